@@ -503,6 +503,138 @@ vp_status vp_unpack_combine(const void* recv, int64_t recv_capacity, int64_t row
                             const int64_t* bytes, const int32_t* recv_src, int32_t k_max, void* combined,
                             int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------- layer: routing, experts
+ *
+ * What stands before, between and after the two exchanges of a
+ * mixture-of-experts layer.  Element types: */
+typedef enum { VP_F32 = 0, VP_BF16 = 1, VP_F16 = 2 } vp_dtype;
+
+enum { VP_SCORE_SOFTMAX = 0, VP_SCORE_SIGMOID = 1 };
+
+/* How a token's experts follow from its logits (vp_route). */
+typedef struct {
+  int32_t score;       /* VP_SCORE_SOFTMAX over the row, or VP_SCORE_SIGMOID of each logit */
+  int32_t top_k;       /* experts of a token, 1..64 */
+  int32_t n_groups;    /* groups of E / n_groups neighbouring experts, 1..64 (1: none) */
+  int32_t top_groups;  /* groups that are kept */
+  int32_t group_top;   /* a group's score: its best key (1) or the sum of its best two (2) */
+  int32_t renorm;      /* divide the weights by the sum of the chosen scores */
+  float scale;         /* factor of the weights, positive */
+} vp_route_params;
+
+/* Routing: the experts of every token and their weights.
+ *   logits  device [T, E], rows logits_stride elements apart, vp_dtype
+ *   bias    device float32 [E] or NULL: added to the scores for the choice
+ *           only (load balance), not to the weights
+ *   ids     device int32 [T, k]   in order of falling key; the routing of
+ *           vp_demand
+ *   weights device float32 [T, k] scale * score (/ the chosen scores' sum)
+ * Keys are score + bias (without a bias the logits' own order); ties go to the
+ * lowest index.  A logit of minus infinity masks its expert: masked experts,
+ * and those outside the kept groups, are chosen only when nothing else is
+ * left, with weight 0; a row with nothing left has k distinct ids and all
+ * weights 0.  NaN logits are chosen last too, and the formulas carry them
+ * into the weights.  Sums are in 32 bits.  E <= 4096, top_k <= min(64, E) and
+ * <= the experts of the kept groups, T * top_k < 2^31. */
+vp_status vp_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t logits_stride,
+                   const vp_route_params* p, const float* bias, int32_t* ids, float* weights, void* stream);
+
+/* Gradient of the weights by the logits: d_weights device float32 [T, k],
+ * ids and weights as vp_route gave them for the same logits and params; writes
+ * d_logits device [T, E] of the logits' type.  The choice and the bias have no
+ * gradient; a weight of 0 passes none on.  An id outside [0, E) sets
+ * VP_ERR_INVALID_ARGUMENT in dev_status. */
+vp_status vp_route_grad(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t logits_stride,
+                        const vp_route_params* p, const int32_t* ids, const float* weights, const float* d_weights,
+                        void* d_logits, int32_t* dev_status, void* stream);
+
+/* First row of every local expert in the expert-major output of
+ * vp_unpack_rows: counts device int32 [N, E] as there; offsets device int64
+ * [E/N + 1], the last entry the number of rows.  A negative count sets
+ * VP_ERR_INVALID_ARGUMENT. */
+vp_status vp_expert_offsets(const int32_t* counts, int32_t n_ranks, int32_t E, int32_t self_rank, int64_t* offsets,
+                            int32_t* dev_status, void* stream);
+
+/* The experts' products over expert-major rows (rows offsets[e] up to
+ * offsets[e + 1] are expert e's; only the device knows them):
+ *   x       device [R, K] bf16 or fp16, rows x_stride bytes apart
+ *   w       device [L, N, K] of the same type, contiguous
+ *   offsets device int64 [L + 1], nondecreasing, within [0, R]
+ *   y       device [R, N]: x W_e^T; gated: [R, N/2], silu(x G^T) * (x U^T)
+ *           with G the first and U the second N/2 rows of W_e
+ *   pre     gated: device [R, N], x G^T and x U^T (rounded), or NULL
+ * Sums are in 32 bits and rounded once.  Rows outside the experts' are neither
+ * read nor written.  K and N are multiples of 8 (gated: N of 16), strides of 16
+ * bytes and at most 4 MiB, addresses 16-byte aligned, R < 2^31, L <= 4096.
+ * Offsets that decrease or leave [0, R] set VP_ERR_INVALID_ARGUMENT in
+ * dev_status. */
+vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const void* w, const int64_t* offsets,
+                           int64_t R, int32_t L, int32_t N, int32_t K, int32_t gated, void* y, int64_t y_stride,
+                           void* pre, int64_t pre_stride, int32_t* dev_status, void* stream);
+
+/* dx = dy W_e for every expert's rows: dy device [R, N], dx device [R, K]. */
+vp_status vp_expert_matmul_grad_x(const void* dy, int64_t dy_stride, int32_t dtype, const void* w,
+                                  const int64_t* offsets, int64_t R, int32_t L, int32_t N, int32_t K, void* dx,
+                                  int64_t dx_stride, int32_t* dev_status, void* stream);
+
+/* dW_e = dy^T x over the expert's rows: dw device float32 [L, N, K],
+ * contiguous; 0 for an expert without rows. */
+vp_status vp_expert_matmul_grad_w(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int32_t dtype,
+                                  const int64_t* offsets, int64_t R, int32_t L, int32_t N, int32_t K, float* dw,
+                                  int32_t* dev_status, void* stream);
+
+/* Gradient of the gated product by x G^T and x U^T: dh device [R, I], pre as
+ * vp_expert_matmul left it (I = N/2), dpre device [R, 2 I]; the products'
+ * gradients then follow from dpre. */
+vp_status vp_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride, int32_t dtype,
+                              const int64_t* offsets, int64_t R, int32_t L, int32_t I, void* dpre,
+                              int64_t dpre_stride, int32_t* dev_status, void* stream);
+
+/* The layer's output from the rows that vp_unpack_combine put at (token,
+ * slot): out[t] = residual[t] + sum_j weights[t, j] * rows[t * k + j].
+ *   rows    device [T * k, H] of any vp_dtype, row_stride bytes apart
+ *   weights device float32 [T, k]
+ *   residual, out  device [T, H] of the same type; residual may be NULL, or
+ *           out itself
+ * A slot of weight 0 adds nothing whatever its row holds.  Sums are in 32
+ * bits, in slot order.  H elements fill whole 16-byte vectors; strides are
+ * multiples of 16 bytes, addresses 16-byte aligned; k <= 255, T < 2^31. */
+vp_status vp_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, int64_t H, int64_t row_stride,
+                   const float* weights, const void* residual, int64_t residual_stride, void* out, int64_t out_stride,
+                   void* stream);
+
+/* Its gradient: d_rows[t * k + j] = weights[t, j] * d_out[t] and d_weights[t,
+ * j] = <d_out[t], rows[t * k + j]> (float32); both 0 for a slot of weight 0. */
+vp_status vp_merge_grad(const void* d_out, int32_t dtype, int64_t T, int32_t k, int64_t H, int64_t d_out_stride,
+                        const void* rows, int64_t row_stride, const float* weights, void* d_rows,
+                        int64_t d_rows_stride, float* d_weights, void* stream);
+
+/* Bytes of a row of K values in 4-bit blocks (OCP MXFP4): K/2 bytes of E2M1
+ * codes, two a byte with the lower index in the low bits; K/32 bytes of
+ * exponents (E8M0, one for 32 neighbouring values); zeros up to a multiple of
+ * 16.  Such a row can be packed and unpacked like any other.  0 unless K is a
+ * positive multiple of 32. */
+int64_t vp_mx_row_bytes(int64_t K);
+
+/* Rows to 4-bit blocks: x device [rows, K] of any vp_dtype; q device, rows
+ * q_stride bytes apart.  A block's power of two is that of its largest
+ * magnitude over 4 (never below 2^-127); values are rounded to nearest, ties
+ * to the even code, and end at 6 times that power.  A block with an infinity
+ * or NaN gets exponent 255 and reads back as NaN.  Strides are multiples of
+ * 16 bytes, addresses 16-byte aligned. */
+vp_status vp_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t K, int64_t x_stride, void* q,
+                         int64_t q_stride, void* stream);
+vp_status vp_mx_dequantize(const void* q, int64_t rows, int64_t K, int64_t q_stride, void* out, int32_t dtype,
+                           int64_t out_stride, void* stream);
+
+/* vp_expert_matmul with both operands in 4-bit blocks along K: xq device [R]
+ * rows xq_stride bytes apart, wq device [L, N] rows vp_mx_row_bytes(K) bytes
+ * apart; y device [R, N] (gated [R, N/2]) bf16 or fp16.  K is a multiple of 32;
+ * otherwise as vp_expert_matmul. */
+vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq, const int64_t* offsets, int64_t R,
+                              int32_t L, int32_t N, int32_t K, int32_t gated, void* y, int32_t dtype,
+                              int64_t y_stride, int32_t* dev_status, void* stream);
+
 /* --------------------------------------------------------------- helpers */
 
 /* Modeled completion time of a schedule, Eq. (2), as the exact fraction

@@ -112,6 +112,7 @@ def lib():
     L.vp_status_string.restype = C.c_char_p
     L.vp_last_error.argtypes = []
     L.vp_last_error.restype = C.c_char_p
+    layer.declare(L)
     _lib = L
     return L
 
@@ -730,3 +731,11 @@ class Pipeline:
         self.words_stage(stream)
         self.plan_stage(stream)
         return self.pack_stage(tokens, head_lo, send, stream)
+
+
+# ----------------------------------------------------------------- layer
+
+from . import layer  # noqa: E402
+from .layer import (expert_gate_grad, expert_matmul, expert_matmul_grad_w, expert_matmul_grad_x,  # noqa: E402,F401
+                    expert_matmul_mx, expert_offsets, merge, merge_grad, mx_dequantize, mx_quantize, mx_row_bytes,
+                    route, route_grad)

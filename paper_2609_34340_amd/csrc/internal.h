@@ -194,4 +194,44 @@ size_t unpack_lds_bytes(int mode, int32_t N, int32_t eloc);
 vp_status launch_unpack(const UnpackLaunch& a, void* stream);
 vp_status launch_transpose(const int64_t* D, int32_t N, int64_t* DT, void* stream);
 
+// The layer around the exchanges: routing, the experts' products, the merge
+// of the returned rows, rows in 4-bit blocks.  Strides are bytes between rows
+// (the logits' in elements).
+vp_status launch_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t stride,
+                       const vp_route_params& p, const float* bias, int32_t* ids, float* weights, void* stream);
+vp_status launch_route_grad(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t stride,
+                            const vp_route_params& p, const int32_t* ids, const float* weights,
+                            const float* d_weights, void* d_logits, int32_t* status, void* stream);
+vp_status launch_expert_offsets(const int32_t* counts, int32_t N, int32_t E, int32_t self, int64_t* offsets,
+                                int32_t* status, void* stream);
+enum { kExpertForward = 0, kExpertGradX = 1, kExpertGradW = 2 };
+struct ExpertLaunch {
+  int mode;
+  bool gated, mx;
+  int32_t dtype;
+  const void *a, *b;       // rows and weights; grad w: dy and x
+  int64_t a_stride, b_stride;
+  const int64_t* offsets;
+  int64_t R;
+  int32_t L, N, K;
+  void *out, *pre;
+  int64_t out_stride, pre_stride;
+  int32_t* status;
+};
+vp_status launch_expert_product(const ExpertLaunch& p, void* stream);
+vp_status launch_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride,
+                                  int32_t dtype, int64_t R, int32_t half, const int64_t* offsets, int32_t L, void* out,
+                                  int64_t out_stride, int32_t* status, void* stream);
+vp_status launch_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, int64_t H, int64_t row_stride,
+                       const float* weights, const void* residual, int64_t residual_stride, void* out,
+                       int64_t out_stride, void* stream);
+vp_status launch_merge_grad(const void* d_out, int32_t dtype, int64_t T, int32_t k, int64_t H, int64_t d_out_stride,
+                            const void* rows, int64_t row_stride, const float* weights, void* d_rows,
+                            int64_t d_rows_stride, float* d_weights, void* stream);
+int64_t mx_row_bytes(int64_t K);
+vp_status launch_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t K, int64_t x_stride, void* q,
+                             int64_t q_stride, void* stream);
+vp_status launch_mx_dequantize(const void* q, int64_t rows, int64_t K, int64_t q_stride, void* out, int32_t dtype,
+                               int64_t out_stride, void* stream);
+
 }  // namespace vp

@@ -1,0 +1,60 @@
+// 16-bit and 32-bit element types of the layer operators, in registers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/vp.h"
+
+namespace vp {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 { uint16_t u; };
+struct F16 { uint16_t u; };
+
+__device__ inline float to_f32(float x) { return x; }
+__device__ inline float to_f32(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
+__device__ inline float to_f32(F16 x) { return (float)__builtin_bit_cast(_Float16, x.u); }
+
+// Round to nearest, ties to even; NaN stays NaN.
+template <typename T> __device__ inline T from_f32(float x);
+template <> __device__ inline float from_f32<float>(float x) { return x; }
+template <> __device__ inline Bf16 from_f32<Bf16>(float x) { return {__builtin_bit_cast(uint16_t, (__bf16)x)}; }
+template <> __device__ inline F16 from_f32<F16>(float x) { return {__builtin_bit_cast(uint16_t, (_Float16)x)}; }
+
+// 16 bytes of T as floats and back.
+template <typename T> struct Vec { static constexpr int n = 8; };
+template <> struct Vec<float> { static constexpr int n = 4; };
+
+template <typename T> __device__ inline void unpack16(u32x4 v, float* f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = to_f32(T{(uint16_t)(v[i] & 0xffffu)});
+    f[2 * i + 1] = to_f32(T{(uint16_t)(v[i] >> 16)});
+  }
+}
+template <> __device__ inline void unpack16<float>(u32x4 v, float* f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+}
+template <typename T> __device__ inline u32x4 pack16(const float* f) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(f[2 * i]).u | (uint32_t)from_f32<T>(f[2 * i + 1]).u << 16;
+  return v;
+}
+template <> __device__ inline u32x4 pack16<float>(const float* f) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+  return v;
+}
+
+inline int64_t dtype_size(int32_t d) { return d == VP_F32 ? 4 : 2; }
+inline bool is_dtype(int32_t d) { return d == VP_F32 || d == VP_BF16 || d == VP_F16; }
+
+}  // namespace vp
