@@ -565,7 +565,8 @@ vp_status vp_expert_offsets(const int32_t* counts, int32_t n_ranks, int32_t E, i
  *   pre     gated: device [R, N], x G^T and x U^T (rounded), or NULL
  * Sums are in 32 bits and rounded once.  Rows outside the experts' are neither
  * read nor written.  K and N are multiples of 8 (gated: N of 16), strides of 16
- * bytes and at most 4 MiB, addresses 16-byte aligned, R < 2^31, L <= 4096.
+ * bytes and at most 4 MiB, addresses 16-byte aligned, R < 2^31, L <= 4096, half
+ * of a gated expert's weights below 1 GiB.
  * Offsets that decrease or leave [0, R] set VP_ERR_INVALID_ARGUMENT in
  * dev_status. */
 vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const void* w, const int64_t* offsets,

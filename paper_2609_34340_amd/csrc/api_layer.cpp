@@ -49,6 +49,15 @@ vp_status check_experts(int32_t dtype, const int64_t* offsets, int64_t R, int32_
   return VP_OK;
 }
 
+// A tile of a gated product spans both halves of an expert's weights.
+vp_status check_gated(int32_t gated, int32_t N, int64_t row_bytes) {
+  if (gated != 0 && gated != 1) return set_error(VP_ERR_INVALID_ARGUMENT, "gated is 0 or 1");
+  if (gated && N % 16 != 0) return set_error(VP_ERR_UNSUPPORTED, "a gated product's N must be a multiple of 16");
+  if (gated && ((int64_t)N / 2 + 256) * row_bytes >= int64_t(1) << 30)
+    return set_error(VP_ERR_UNSUPPORTED, "half of a gated expert's weights must be below 1 GiB");
+  return VP_OK;
+}
+
 // One operand of a product: `width` bytes of each row.
 vp_status check_rows(const void* p, int64_t width, int64_t stride, int64_t R, const char* name) {
   if (R > 0 && !p) return set_error(VP_ERR_INVALID_ARGUMENT, std::string("null ") + name);
@@ -97,8 +106,7 @@ vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const
                            void* pre, int64_t pre_stride, int32_t* dev_status, void* stream) {
   vp_status st = check_experts(dtype, offsets, R, L, N, K, dev_status);
   if (st != VP_OK) return st;
-  if (gated != 0 && gated != 1) return set_error(VP_ERR_INVALID_ARGUMENT, "gated is 0 or 1");
-  if (gated && N % 16 != 0) return set_error(VP_ERR_UNSUPPORTED, "a gated product's N must be a multiple of 16");
+  if ((st = check_gated(gated, N, (int64_t)K * 2)) != VP_OK) return st;
   if (!gated && pre) return set_error(VP_ERR_INVALID_ARGUMENT, "pre belongs to a gated product");
   if ((st = check_rows(x, (int64_t)K * 2, x_stride, R, "x")) != VP_OK) return st;
   if ((st = check_rows(w, (int64_t)K * 2, (int64_t)K * 2, 1, "w")) != VP_OK) return st;
@@ -230,10 +238,9 @@ vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq,
                               int64_t y_stride, int32_t* dev_status, void* stream) {
   vp_status st = check_experts(dtype, offsets, R, L, N, K, dev_status);
   if (st != VP_OK) return st;
-  if (gated != 0 && gated != 1) return set_error(VP_ERR_INVALID_ARGUMENT, "gated is 0 or 1");
-  if (K % 32 != 0 || (gated && N % 16 != 0))
-    return set_error(VP_ERR_UNSUPPORTED, "K must be a multiple of 32, a gated product's N of 16");
+  if (K % 32 != 0) return set_error(VP_ERR_UNSUPPORTED, "K must be a multiple of 32");
   const int64_t rb = vp::mx_row_bytes(K);
+  if ((st = check_gated(gated, N, rb)) != VP_OK) return st;
   if ((st = check_rows(xq, rb, xq_stride, R, "xq")) != VP_OK) return st;
   if ((st = check_rows(wq, rb, rb, 1, "wq")) != VP_OK) return st;
   if ((st = check_rows(y, (int64_t)(gated ? N / 2 : N) * 2, y_stride, R, "y")) != VP_OK) return st;

@@ -9,7 +9,30 @@
 // in bf16 or fp16 with 32-bit sums, and the forward product also with both
 // operands in 4-bit blocks (mx.hip) on the scaled matrix instruction, which
 // multiplies the values and applies the blocks' powers of two itself.
+//
+// A workgroup makes one tile of BM rows by BN columns of one expert.  Tiles
+// are numbered without a count of any expert's: expert e owns the slots from
+// floor(offsets[e] / BM) + e on, at least as many as its rows need, and a
+// slot past its rows is empty.  So the grid follows from the buffer's size,
+// and a tile finds its expert by counting the experts whose first slot is at
+// or below its own.
+//
+// Each step of the contraction brings 128 bytes of every row of both operands
+// to LDS (64 16-bit values, or 256 4-bit ones) by direct loads, double
+// buffered.  Both operands are read through buffer descriptors that end with
+// the expert's last row: what lies outside reads as zero, so no neighbour's
+// row (which may hold anything) enters a sum.  The places in LDS are permuted
+// so that the matrix fragments' reads meet no bank twice:
+//   rows by contraction   16-byte chunk c of row r at place c ^ (r & 7); a
+//                         fragment lane reads its row's chunk whole
+//   contraction by rows   (grad x's weights, both operands of grad w) 32-byte
+//                         piece p of contraction row c at place p ^ f(c), read
+//                         through the transposing LDS load
+// The product is computed as its transpose, so that a lane's four results are
+// neighbours in the output row.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "internal.h"
 #include "numeric.h"
@@ -17,6 +40,7 @@
 namespace vp {
 namespace {
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -79,116 +103,299 @@ template <> struct Frag<F16> { using type = f16x8; using elem = _Float16; };
 
 __device__ inline float silu(float g) { return g / (1.0f + expf(-g)); }
 
-// A simple product: one wavefront a 16 x 16 tile, fragments straight from memory.
-template <typename T, int MODE, bool GATED>
-__global__ void __launch_bounds__(64) product_simple(ProductArgs a) {
-  const int lane = threadIdx.x, r = lane % 16, q = lane / 16;
-  if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets(a);
+// ---------------------------------------------------------------- tiled products
+
+constexpr int kStep = 128;   // bytes of a row that one step of the contraction takes
+
+// Address of the permuted place of 32-byte piece p of contraction row c.
+__device__ inline int piece_place(int p, int c) { return p ^ ((c & 3) | ((c >> 3) & 1) << 2); }
+
+// One operand of a tile: ROWS rows (columns of the output, or its rows) in LDS.
+// COLS: the buffer's rows are the contraction, ROWS neighbouring elements of
+// each; otherwise a buffer row is an operand row, 128 bytes of it per step.
+template <int ROWS, bool COLS, int WAVES> struct Operand {
+  static constexpr int kLoads = ROWS * kStep / 1024 / WAVES;   // direct loads of 64 x 16 bytes by each wavefront
+  static constexpr int kSlots = ROWS / 8;                      // COLS: 16-byte slots of a contraction row
+  const unsigned char* base;   // of the current step, in the wavefront's registers
+  int64_t left;                // rows by contraction: bytes to the end of the last valid row; COLS: rows left
+  int64_t stride;
+  int width;                   // rows by contraction: bytes of a row left; COLS: bytes of a row from the tile's first column
+  uint32_t off[kLoads];
+
+  // For rows by contraction `row_of(i)` gives the buffer row of operand row i, relative to `base`.
+  template <typename F> __device__ void init(int wave, int lane, F row_of) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      if (COLS) {
+        const int c = (wave * kLoads + j) * (64 / kSlots) + lane / kSlots, slot = lane % kSlots;
+        off[j] = (uint32_t)(c * stride) + piece_place(slot / 2, c) * 32 + (slot & 1) * 16;
+      } else {
+        const int i = (wave * kLoads + j) * 8 + lane / 8;
+        off[j] = (uint32_t)(row_of(i) * stride) + ((lane & 7) ^ (i & 7)) * 16;
+      }
+    }
+  }
+  // Starts the step's loads to `lds` and moves on.
+  __device__ void load(unsigned char* lds, int wave, int lane) {
+    int64_t bytes = COLS ? (left < 64 ? left - 1 : 63) * stride + width : left;
+    if (bytes < 0) bytes = 0;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+    // chunks past a row's end read outside the buffer, as zero
+    const uint32_t past = !COLS && (((lane & 7) ^ (lane >> 3)) * 16 >= width) ? 0x60000000u : 0u;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + j) * 1024),
+                                               16, off[j] + past, 0, 0, 0);
+    if (COLS) {
+      base += 64 * stride;
+      left -= 64;
+    } else {
+      base += kStep;
+      left -= kStep;
+      width -= kStep;
+    }
+  }
+};
+
+template <typename T> struct Mx { using out = T; };   // both operands in 4-bit blocks, results of type T
+template <typename T> struct Elem { using out = T; static constexpr bool mx = false; };
+template <typename T> struct Elem<Mx<T>> { using out = T; static constexpr bool mx = true; };
+
+// WM x WN wavefronts, each with MT x NT fragments of 16 x 16 results.
+template <typename T, int MODE, bool GATED, int WM, int WN, int MT, int NT>
+__global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host's pass knows none of the builtins below
+  using Out = typename Elem<T>::out;
+  constexpr bool kMx = Elem<T>::mx, kColsA = MODE == kGradW, kColsB = MODE != kForward;
+  constexpr int BM = WM * MT * 16, BN = WN * NT * 16, kWaves = WM * WN;
+  constexpr int kTileN = GATED ? BN / 2 : BN;   // output columns
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2][(BM + BN) * kStep];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 16, q = lane / 16;
+  if (blockIdx.x == 0) check_offsets(a);
+
+  // which tile: XCD x (block % 8) takes a contiguous eighth of the tiles (of
+  // every expert's, for grad w), in blocks of eight row tiles by all columns
+  const int nt = (a.N + kTileN - 1) / kTileN;
+  const int xcd = blockIdx.x & 7;
+  const int64_t idx = blockIdx.x >> 3;
+  constexpr int kBand = 8;
   Group g;
-  int64_t m0;
+  int64_t m0, slot;
+  int ni;
   if (MODE == kGradW) {
-    g = group_of(a, blockIdx.z);
-    m0 = (int64_t)blockIdx.x * 16;
+    const int mt = (a.M + BM - 1) / BM;
+    const int64_t per = ((int64_t)mt * nt + 7) / 8;
+    const int64_t e = idx / per, t = xcd * per + idx % per;
+    if (e >= a.L || t >= (int64_t)mt * nt) return;
+    const int band = (int)(t / (kBand * nt)), in = (int)(t % (kBand * nt));
+    const int high = min(kBand, mt - band * kBand);
+    slot = band * kBand + in % high;
+    ni = in / high;
+    g = group_of(a, (int)e);
+    m0 = slot * BM;
   } else {
-    const int e = expert_of_slot<16>(a, blockIdx.x);
+    int64_t rows = a.offsets[a.L];
+    rows = rows < 0 ? 0 : rows > a.R ? a.R : rows;
+    const int64_t slots = rows / BM + a.L, total = slots * nt, per = (total + 7) / 8, t = xcd * per + idx;
+    if (idx >= per || t >= total) return;
+    const int64_t band = t / (kBand * nt);
+    const int in = (int)(t % (kBand * nt));
+    const int high = (int)min((int64_t)kBand, slots - band * kBand);
+    slot = band * kBand + in % high;
+    ni = in / high;
+    const int e = expert_of_slot<BM>(a, slot);
     if (e < 0) return;
     g = group_of(a, e);
-    m0 = g.lo + ((int64_t)blockIdx.x - (a.offsets[e] / 16 + e)) * 16;
-    if (m0 >= g.hi) return;
+    m0 = g.lo + (slot - (a.offsets[e] / BM + e)) * BM;
+    if (m0 < g.lo || m0 >= g.hi) return;
   }
-  const int n0 = blockIdx.y * 16;
-  const int rows = (int)(g.hi - g.lo);
-  constexpr int kSteps = GATED ? 2 : 1;
-  f32x4 acc[kSteps] = {};
-  const int C = MODE == kGradW ? rows : a.C;
-  for (int c0 = 0; c0 < C; c0 += 32) {
-    typename Frag<T>::type fa, fb[kSteps];
-    using E = typename Frag<T>::elem;
-    for (int i = 0; i < 8; ++i) {
-      const int c = c0 + q * 8 + i;
-      uint16_t va = 0, vb[2] = {0, 0};
-      if (c < C) {
-        const int n = n0 + r;
-        if (MODE == kGradW) {
-          if (m0 + r < a.M) va = ((const uint16_t*)(a.a + (g.lo + c) * a.a_stride))[m0 + r];
-          if (n < a.N) vb[0] = ((const uint16_t*)(a.b + (g.lo + c) * a.b_stride))[n];
-        } else {
-          if (m0 + r < g.hi) va = ((const uint16_t*)(a.a + (m0 + r) * a.a_stride))[c];
-          for (int s = 0; s < kSteps; ++s)
-            if (n < a.N)
-              vb[s] = MODE == kForward ? ((const uint16_t*)(a.b + g.e * a.b_expert + (int64_t)(n + s * a.half) * a.b_stride))[c]
-                                       : ((const uint16_t*)(a.b + g.e * a.b_expert + (int64_t)c * a.b_stride))[n];
-        }
-      }
-      fa[i] = __builtin_bit_cast(E, va);
-      for (int s = 0; s < kSteps; ++s)
-        fb[s][i] = __builtin_bit_cast(E, vb[s]);
+  const int n0 = ni * kTileN;
+
+  // operands and the steps of the contraction
+  const int64_t rows = g.hi - g.lo;
+  const int64_t C = MODE == kGradW ? rows : a.C;               // elements
+  const int row_bytes = kMx ? a.C / 2 : a.C * 2;
+  const int64_t steps = MODE == kGradW || MODE == kGradX ? (C + 63) / 64 : (row_bytes + kStep - 1) / kStep;
+  Operand<BM, kColsA, kWaves> oa;
+  Operand<BN, kColsB, kWaves> ob;
+  oa.stride = a.a_stride;
+  ob.stride = a.b_stride;
+  if (kColsA) {
+    oa.base = a.a + g.lo * a.a_stride + m0 * 2;
+    oa.left = rows;
+    oa.width = (int)((a.M - m0) * 2);
+  } else {
+    oa.base = a.a + m0 * a.a_stride;
+    const int64_t valid = min((int64_t)BM, g.hi - m0);
+    oa.left = (valid - 1) * a.a_stride + row_bytes;
+    oa.width = row_bytes;
+  }
+  oa.init(wave, lane, [](int i) { return (int64_t)i; });
+  if (MODE == kGradW) {
+    ob.base = a.b + g.lo * a.b_stride + n0 * 2;
+    ob.left = rows;
+    ob.width = (a.N - n0) * 2;
+  } else if (MODE == kGradX) {
+    ob.base = a.b + g.e * a.b_expert + n0 * 2;
+    ob.left = a.C;
+    ob.width = (a.N - n0) * 2;
+  } else {
+    // gated: of every 64 operand rows the first 32 are gate rows, the others the same up rows
+    ob.base = a.b + g.e * a.b_expert + (int64_t)n0 * a.b_stride;
+    ob.left = ((int64_t)(GATED ? a.half + a.N : a.N) - n0 - 1) * a.b_stride + row_bytes;
+    const int64_t most = (int64_t)(GATED ? a.half + kTileN : BN) * a.b_stride;
+    if (ob.left > most) ob.left = most;
+    ob.width = row_bytes;
+  }
+  const int half = a.half;
+  ob.init(wave, lane, [=](int i) { return GATED ? (int64_t)(i / 64 * 32 + i % 32 + (i & 32 ? half : 0)) : (int64_t)i; });
+
+  // places of this lane's fragments in LDS
+  const int wm = wave / WN, wn = wave % WN;
+  const auto chunk = [=](int kk) { return kMx ? 2 * q + kk : 4 * kk + q; };
+  uint32_t pa[kColsA ? MT : 1], pb[kColsB ? NT : 1];
+  if (kColsA) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) pa[i] = (q * 8 + r / 4) * (BM * 2) + piece_place(wm * MT + i, q * 8 + r / 4) * 32 + (r & 3) * 8;
+  } else {
+    pa[0] = (wm * MT * 16 + r) * kStep;
+  }
+  if (kColsB) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) pb[i] = (q * 8 + r / 4) * (BN * 2) + piece_place(wn * NT + i, q * 8 + r / 4) * 32 + (r & 3) * 8;
+  } else {
+    pb[0] = (wn * NT * 16 + r) * kStep;
+  }
+  const auto frag = [&](const unsigned char* p, auto cols, auto width, uint32_t place, int i, int kk) -> i32x4 {
+    if constexpr (decltype(cols)::value) {
+      constexpr int kRow = decltype(width)::value * 2;
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const unsigned char* at = p + place + kk * 32 * kRow;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRow));
+      const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
+      return i32x4{(int)l.x, (int)l.y, (int)h.x, (int)h.y};
+    } else {
+      return *(const i32x4*)(p + place + i * 16 * kStep + (chunk(kk) ^ (r & 7)) * 16);
     }
-    for (int s = 0; s < kSteps; ++s) acc[s] = mma(fb[s], fa, acc[s]);
+  };
+
+  // 4-bit blocks: the powers of two of this lane's rows, two blocks per step
+  int sa[kMx ? MT : 1] = {}, sb[kMx ? NT : 1] = {};
+  const unsigned char *qa[kMx ? MT : 1], *qb[kMx ? NT : 1];
+  if constexpr (kMx) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t m = m0 + wm * MT * 16 + i * 16 + r;
+      qa[i] = a.a + (m < g.hi ? m : m0) * a.a_stride + row_bytes + 2 * q;
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int j = wn * NT * 16 + i * 16 + r;
+      const int n = n0 + (GATED ? j / 64 * 32 + j % 32 : j);
+      qb[i] = a.b + g.e * a.b_expert + (int64_t)((n < a.N ? n : 0) + (GATED && (j & 32) ? half : 0)) * a.b_stride + row_bytes + 2 * q;
+    }
   }
-  for (int i = 0; i < 4; ++i) {
-    const int n = n0 + q * 4 + i;
-    const int64_t m = m0 + r;
-    if (n >= a.N || m >= (MODE == kGradW ? a.M : g.hi)) continue;
-    if (MODE == kGradW) {
-      ((float*)(a.out + g.e * a.b_expert + m * a.out_stride))[n] = acc[0][i];
-    } else if (GATED) {
-      ((T*)(a.out + m * a.out_stride))[n] = from_f32<T>(silu(acc[0][i]) * acc[1][i]);
-      if (a.pre) {
-        ((T*)(a.pre + m * a.pre_stride))[n] = from_f32<T>(acc[0][i]);
-        ((T*)(a.pre + m * a.pre_stride))[n + a.half] = from_f32<T>(acc[1][i]);
+  int sa1[kMx ? MT : 1] = {}, sb1[kMx ? NT : 1] = {};   // the next step's
+  const auto scales = [&](int64_t s) {
+    if constexpr (kMx) {
+      // blocks past the row's last read as 2^-127 (their codes are zero)
+      const int left = a.C / 32 - (int)s * 8 - 2 * q;
+      const int mask = left >= 2 ? 0xffff : left == 1 ? 0xff : 0;
+      const int64_t at = left > 0 ? s * 8 : 0;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sa1[i] = left > 0 ? *(const uint16_t*)(qa[i] + at) & mask : 0;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) sb1[i] = left > 0 ? *(const uint16_t*)(qb[i] + at) & mask : 0;
+    }
+  };
+
+  f32x4 acc[MT][NT] = {};
+  oa.load(lds[0], wave, lane);
+  ob.load(lds[0] + BM * kStep, wave, lane);
+  scales(0);
+  for (int64_t s = 0; s < steps; ++s) {
+    // this step's bytes are there, and no wavefront reads the other half any more
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (s + 1 < steps) {
+      oa.load(lds[(s + 1) & 1], wave, lane);
+      ob.load(lds[(s + 1) & 1] + BM * kStep, wave, lane);
+    }
+    if constexpr (kMx) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sa[i] = sa1[i];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) sb[i] = sb1[i];
+      scales(s + 1);
+    }
+    const unsigned char *la = lds[s & 1], *lb = la + BM * kStep;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      i32x4 fa[MT], fb[NT];
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        fb[i] = frag(lb, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        fa[i] = frag(la, std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          if constexpr (kMx) {
+            const i32x8 wa = {fa[i][0], fa[i][1], fa[i][2], fa[i][3], 0, 0, 0, 0};
+            const i32x8 wb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
+            acc[i][j] = kk == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, 0, sb[j], 0, sa[i])
+                                : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, 1, sb[j], 1, sa[i]);
+          } else {
+            using F = typename Frag<T>::type;
+            acc[i][j] = mma(__builtin_bit_cast(F, fb[j]), __builtin_bit_cast(F, fa[i]), acc[i][j]);
+          }
+        }
+    }
+  }
+
+  const auto put = [&](unsigned char* at, f32x4 v) {
+    u32x2 o;
+    o.x = from_f32<Out>(v[0]).u | (uint32_t)from_f32<Out>(v[1]).u << 16;
+    o.y = from_f32<Out>(v[2]).u | (uint32_t)from_f32<Out>(v[3]).u << 16;
+    *(u32x2*)at = o;
+  };
+  const int64_t end = MODE == kGradW ? a.M : g.hi;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + (wm * MT + i) * 16 + r;
+    if (m >= end) continue;
+    unsigned char* out = a.out + (MODE == kGradW ? g.e * a.b_expert : 0) + m * a.out_stride;
+    if constexpr (GATED) {
+#pragma unroll
+      for (int j = 0; j < NT / 2; ++j) {
+        const int n = n0 + wn * NT * 8 + j * 16 + q * 4;
+        if (n >= a.N) continue;
+        const f32x4 gate = acc[i][j], up = acc[i][j + NT / 2];
+        f32x4 h;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) h[v] = silu(gate[v]) * up[v];
+        put(out + n * 2, h);
+        if (a.pre) {
+          put(a.pre + m * a.pre_stride + n * 2, gate);
+          put(a.pre + m * a.pre_stride + (int64_t)(n + a.half) * 2, up);
+        }
       }
     } else {
-      ((T*)(a.out + m * a.out_stride))[n] = from_f32<T>(acc[0][i]);
-    }
-  }
-}
-
-// 4-bit blocks, the simple way: the scaled instruction takes 128 values of a
-// row, 32 per lane with that lane's scale.
-template <typename T, bool GATED>
-__global__ void __launch_bounds__(64) product_simple_mx(ProductArgs a) {
-  const int lane = threadIdx.x, r = lane % 16, q = lane / 16;
-  if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets(a);
-  const int e = expert_of_slot<16>(a, blockIdx.x);
-  if (e < 0) return;
-  const Group g = group_of(a, e);
-  const int64_t m0 = g.lo + ((int64_t)blockIdx.x - (a.offsets[e] / 16 + e)) * 16;
-  if (m0 >= g.hi) return;
-  const int n0 = blockIdx.y * 16;
-  constexpr int kSteps = GATED ? 2 : 1;
-  f32x4 acc[kSteps] = {};
-  const int blocks = a.C / 32;
-  for (int b0 = 0; b0 < blocks; b0 += 4) {
-    const int b = b0 + q;
-    i32x4 va = {0, 0, 0, 0}, vb[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    int sa = 0, sb[2] = {0, 0};
-    if (b < blocks) {
-      if (m0 + r < g.hi) {
-        const unsigned char* p = a.a + (m0 + r) * a.a_stride;
-        va = *(const i32x4*)(p + b * 16);
-        sa = p[a.C / 2 + b];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int n = n0 + (wn * NT + j) * 16 + q * 4;
+        if (n >= a.N) continue;
+        if constexpr (MODE == kGradW) *(f32x4*)(out + (int64_t)n * 4) = acc[i][j];
+        else put(out + (int64_t)n * 2, acc[i][j]);
       }
-      for (int s = 0; s < kSteps; ++s)
-        if (n0 + r < a.N) {
-          const unsigned char* p = a.b + e * a.b_expert + (int64_t)(n0 + r + s * a.half) * a.b_stride;
-          vb[s] = *(const i32x4*)(p + b * 16);
-          sb[s] = p[a.C / 2 + b];
-        }
-    }
-    const i32x8 fa = {va[0], va[1], va[2], va[3], 0, 0, 0, 0};
-    for (int s = 0; s < kSteps; ++s) {
-      const i32x8 fb = {vb[s][0], vb[s][1], vb[s][2], vb[s][3], 0, 0, 0, 0};
-      acc[s] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa, acc[s], 4, 4, 0, sb[s], 0, sa);
     }
   }
-  for (int i = 0; i < 4; ++i) {
-    const int n = n0 + q * 4 + i;
-    const int64_t m = m0 + r;
-    if (n >= a.N || m >= g.hi) continue;
-    const float z = GATED ? silu(acc[0][i]) * acc[kSteps - 1][i] : acc[0][i];
-    ((T*)(a.out + m * a.out_stride))[n] = from_f32<T>(z);
-  }
+#endif
 }
 
 // Gradient of the gate: with s = 1 / (1 + exp(-g)),
@@ -232,6 +439,26 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(GateArgs a) {
 
 }  // namespace
 
+namespace {
+
+// Grids cover the buffer's tiles for any offsets, rounded up to the eight XCDs.
+template <typename T, int MODE, bool GATED, int WM, int WN, int MT, int NT>
+vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
+  constexpr int BM = WM * MT * 16, kTileN = WN * NT * 16 / (GATED ? 2 : 1);
+  const int64_t nt = (a.N + kTileN - 1) / kTileN;
+  const int64_t per = MODE == kGradW ? (((a.M + BM - 1) / BM) * nt + 7) / 8 * a.L : ((a.R / BM + a.L) * nt + 7) / 8;
+  if (per * 8 >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
+  hipLaunchKernelGGL((product_tiled<T, MODE, GATED, WM, WN, MT, NT>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
+  if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
+  return VP_OK;
+}
+
+template <typename T, int MODE, bool GATED> vp_status launch_product_as(const ProductArgs& a, hipStream_t s) {
+  return launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
+}
+
+}  // namespace
+
 vp_status launch_expert_product(const ExpertLaunch& p, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   ProductArgs a{};
@@ -247,41 +474,36 @@ vp_status launch_expert_product(const ExpertLaunch& p, void* stream) {
   a.out_stride = p.out_stride;
   a.pre_stride = p.pre_stride;
   a.status = p.status;
-  const int64_t slots = p.R / 16 + p.L;
+  const bool bf = p.dtype == VP_BF16;
   if (p.mode == kExpertForward) {
     a.C = p.K;
     a.N = p.gated ? p.N / 2 : p.N;
     a.half = p.N / 2;
     a.b_expert = p.N * p.b_stride;
-    const dim3 grid((unsigned)slots, (unsigned)((a.N + 15) / 16));
     if (p.mx) {
-      if (p.dtype == VP_BF16 && p.gated) hipLaunchKernelGGL((product_simple_mx<Bf16, true>), grid, dim3(64), 0, s, a);
-      else if (p.dtype == VP_BF16) hipLaunchKernelGGL((product_simple_mx<Bf16, false>), grid, dim3(64), 0, s, a);
-      else if (p.gated) hipLaunchKernelGGL((product_simple_mx<F16, true>), grid, dim3(64), 0, s, a);
-      else hipLaunchKernelGGL((product_simple_mx<F16, false>), grid, dim3(64), 0, s, a);
+      if (bf && p.gated) return launch_product_as<Mx<Bf16>, kForward, true>(a, s);
+      if (bf) return launch_product_as<Mx<Bf16>, kForward, false>(a, s);
+      if (p.gated) return launch_product_as<Mx<F16>, kForward, true>(a, s);
+      return launch_product_as<Mx<F16>, kForward, false>(a, s);
     } else {
-      if (p.dtype == VP_BF16 && p.gated) hipLaunchKernelGGL((product_simple<Bf16, kForward, true>), grid, dim3(64), 0, s, a);
-      else if (p.dtype == VP_BF16) hipLaunchKernelGGL((product_simple<Bf16, kForward, false>), grid, dim3(64), 0, s, a);
-      else if (p.gated) hipLaunchKernelGGL((product_simple<F16, kForward, true>), grid, dim3(64), 0, s, a);
-      else hipLaunchKernelGGL((product_simple<F16, kForward, false>), grid, dim3(64), 0, s, a);
+      if (bf && p.gated) return launch_product_as<Bf16, kForward, true>(a, s);
+      if (bf) return launch_product_as<Bf16, kForward, false>(a, s);
+      if (p.gated) return launch_product_as<F16, kForward, true>(a, s);
+      return launch_product_as<F16, kForward, false>(a, s);
     }
   } else if (p.mode == kExpertGradX) {
     a.C = p.N;
     a.N = p.K;
     a.b_expert = p.N * p.b_stride;
-    const dim3 grid((unsigned)slots, (unsigned)((a.N + 15) / 16));
-    if (p.dtype == VP_BF16) hipLaunchKernelGGL((product_simple<Bf16, kGradX, false>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((product_simple<F16, kGradX, false>), grid, dim3(64), 0, s, a);
+    if (bf) return launch_product_as<Bf16, kGradX, false>(a, s);
+    return launch_product_as<F16, kGradX, false>(a, s);
   } else {
     a.M = p.N;
     a.N = p.K;
     a.b_expert = (int64_t)p.N * p.out_stride;
-    const dim3 grid((unsigned)((a.M + 15) / 16), (unsigned)((a.N + 15) / 16), (unsigned)p.L);
-    if (p.dtype == VP_BF16) hipLaunchKernelGGL((product_simple<Bf16, kGradW, false>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((product_simple<F16, kGradW, false>), grid, dim3(64), 0, s, a);
+    if (bf) return launch_product_as<Bf16, kGradW, false>(a, s);
+    return launch_product_as<F16, kGradW, false>(a, s);
   }
-  if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
-  return VP_OK;
 }
 
 vp_status launch_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride,
