@@ -107,6 +107,21 @@ __device__ inline float silu(float g) { return g / (1.0f + expf(-g)); }
 
 constexpr int kStep = 128;   // bytes of a row that one step of the contraction takes
 
+// Starts a direct load of 16 bytes per lane from `off` of `bytes` bytes at
+// `base` to 1 KB of LDS at `lds` (both the same for the whole wavefront).  It
+// returns nothing in registers, and the loops below wait for it themselves:
+// through the builtin the compiler puts a wait for all loads before every
+// transposing LDS read.
+__device__ inline void direct_load(const unsigned char* base, int bytes, uint32_t off, unsigned char* lds) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const uint64_t b = (uint64_t)base;
+  const i32x4 rsrc = {(int)(uint32_t)b, (int)((b >> 32) & 0xffff), bytes, 0x00020000};
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(at), "v"(off), "s"(rsrc) : "memory", "m0");
+#endif
+}
+
 // Address of the permuted place of 32-byte piece p of contraction row c.
 __device__ inline int piece_place(int p, int c) { return p ^ ((c & 3) | ((c >> 3) & 1) << 2); }
 
@@ -116,10 +131,12 @@ __device__ inline int piece_place(int p, int c) { return p ^ ((c & 3) | ((c >> 3
 template <int ROWS, bool COLS, int WAVES> struct Operand {
   static constexpr int kLoads = ROWS * kStep / 1024 / WAVES;   // direct loads of 64 x 16 bytes by each wavefront
   static constexpr int kSlots = ROWS / 8;                      // COLS: 16-byte slots of a contraction row
-  const unsigned char* base;   // of the current step, in the wavefront's registers
-  int64_t left;                // rows by contraction: bytes to the end of the last valid row; COLS: rows left
-  int64_t stride;
+  const unsigned char* base;   // of the current step
+  int stride;                  // bytes, at most 4 MiB
+  int left;                    // rows by contraction: bytes to the end of the last valid row; COLS: rows left
   int width;                   // rows by contraction: bytes of a row left; COLS: bytes of a row from the tile's first column
+  int bytes;                   // what the step may read from its base on
+  uint32_t past;               // rows by contraction: added where the lane's chunk lies past the row's end
   uint32_t off[kLoads];
 
   // For rows by contraction `row_of(i)` gives the buffer row of operand row i, relative to `base`.
@@ -134,18 +151,18 @@ template <int ROWS, bool COLS, int WAVES> struct Operand {
         off[j] = (uint32_t)(row_of(i) * stride) + ((lane & 7) ^ (i & 7)) * 16;
       }
     }
+    bounds(lane);
   }
-  // Starts the step's loads to `lds` and moves on.
-  __device__ void load(unsigned char* lds, int wave, int lane) {
-    int64_t bytes = COLS ? (left < 64 ? left - 1 : 63) * stride + width : left;
-    if (bytes < 0) bytes = 0;
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+  __device__ void bounds(int lane) {
+    bytes = max(COLS ? (min(left, 64) - 1) * stride + width : left, 0);
     // chunks past a row's end read outside the buffer, as zero
-    const uint32_t past = !COLS && (((lane & 7) ^ (lane >> 3)) * 16 >= width) ? 0x60000000u : 0u;
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + j) * 1024),
-                                               16, off[j] + past, 0, 0, 0);
+    past = !COLS && ((lane & 7) ^ (lane >> 3)) * 16 >= width ? 0x60000000u : 0u;
+  }
+  // Starts the j-th of the step's loads.
+  __device__ void issue(unsigned char* lds, int wave, int j) const {
+    direct_load(base, bytes, off[j] + past, lds + (wave * kLoads + j) * 1024);
+  }
+  __device__ void next(int lane) {
     if (COLS) {
       base += 64 * stride;
       left -= 64;
@@ -154,6 +171,7 @@ template <int ROWS, bool COLS, int WAVES> struct Operand {
       left -= kStep;
       width -= kStep;
     }
+    bounds(lane);
   }
 };
 
@@ -170,6 +188,8 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   constexpr int BM = WM * MT * 16, BN = WN * NT * 16, kWaves = WM * WN;
   constexpr int kTileN = GATED ? BN / 2 : BN;   // output columns
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2][(BM + BN) * kStep];
+  // 4-bit blocks: the powers of two of four steps, 32 bytes a row, double buffered
+  __shared__ __attribute__((aligned(1024))) unsigned char powers[kMx ? 2 : 1][kMx ? (BM + BN) * 32 : 16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, q = lane / 16;
   if (blockIdx.x == 0) check_offsets(a);
@@ -219,22 +239,22 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   const int64_t steps = MODE == kGradW || MODE == kGradX ? (C + 63) / 64 : (row_bytes + kStep - 1) / kStep;
   Operand<BM, kColsA, kWaves> oa;
   Operand<BN, kColsB, kWaves> ob;
-  oa.stride = a.a_stride;
-  ob.stride = a.b_stride;
+  oa.stride = (int)a.a_stride;
+  ob.stride = (int)a.b_stride;
   if (kColsA) {
     oa.base = a.a + g.lo * a.a_stride + m0 * 2;
-    oa.left = rows;
+    oa.left = (int)rows;
     oa.width = (int)((a.M - m0) * 2);
   } else {
     oa.base = a.a + m0 * a.a_stride;
     const int64_t valid = min((int64_t)BM, g.hi - m0);
-    oa.left = (valid - 1) * a.a_stride + row_bytes;
+    oa.left = (int)((valid - 1) * a.a_stride) + row_bytes;
     oa.width = row_bytes;
   }
-  oa.init(wave, lane, [](int i) { return (int64_t)i; });
+  oa.init(wave, lane, [](int i) { return i; });
   if (MODE == kGradW) {
     ob.base = a.b + g.lo * a.b_stride + n0 * 2;
-    ob.left = rows;
+    ob.left = (int)rows;
     ob.width = (a.N - n0) * 2;
   } else if (MODE == kGradX) {
     ob.base = a.b + g.e * a.b_expert + n0 * 2;
@@ -243,13 +263,12 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   } else {
     // gated: of every 64 operand rows the first 32 are gate rows, the others the same up rows
     ob.base = a.b + g.e * a.b_expert + (int64_t)n0 * a.b_stride;
-    ob.left = ((int64_t)(GATED ? a.half + a.N : a.N) - n0 - 1) * a.b_stride + row_bytes;
-    const int64_t most = (int64_t)(GATED ? a.half + kTileN : BN) * a.b_stride;
-    if (ob.left > most) ob.left = most;
+    const int64_t end = ((int64_t)(GATED ? a.half + a.N : a.N) - n0 - 1) * a.b_stride + row_bytes;
+    ob.left = (int)min(end, (int64_t)(GATED ? a.half + kTileN : BN) * a.b_stride);
     ob.width = row_bytes;
   }
   const int half = a.half;
-  ob.init(wave, lane, [=](int i) { return GATED ? (int64_t)(i / 64 * 32 + i % 32 + (i & 32 ? half : 0)) : (int64_t)i; });
+  ob.init(wave, lane, [=](int i) { return GATED ? i / 64 * 32 + i % 32 + (i & 32 ? half : 0) : i; });
 
   // places of this lane's fragments in LDS
   const int wm = wave / WN, wn = wave % WN;
@@ -281,82 +300,140 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     }
   };
 
-  // 4-bit blocks: the powers of two of this lane's rows, two blocks per step
-  int sa[kMx ? MT : 1] = {}, sb[kMx ? NT : 1] = {};
-  const unsigned char *qa[kMx ? MT : 1], *qb[kMx ? NT : 1];
+  // 4-bit blocks: a load covers 32 rows' powers of four steps, first their
+  // first 16 bytes (two steps), then the others; a lane's two blocks of a step
+  // are neighbouring bytes
+  constexpr int kPowerLoads = kMx ? (BM + BN) / 32 / kWaves : 1;
+  static_assert(!kMx || (BM + BN) / 32 % kWaves == 0, "whole loads");
+  uint32_t power_off[kPowerLoads] = {};
   if constexpr (kMx) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int64_t m = m0 + wm * MT * 16 + i * 16 + r;
-      qa[i] = a.a + (m < g.hi ? m : m0) * a.a_stride + row_bytes + 2 * q;
-    }
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const int j = wn * NT * 16 + i * 16 + r;
-      const int n = n0 + (GATED ? j / 64 * 32 + j % 32 : j);
-      qb[i] = a.b + g.e * a.b_expert + (int64_t)((n < a.N ? n : 0) + (GATED && (j & 32) ? half : 0)) * a.b_stride + row_bytes + 2 * q;
+    for (int j = 0; j < kPowerLoads; ++j) {
+      const int i = (wave * kPowerLoads + j) * 32 + lane % 32;
+      const int64_t row = i < BM ? i : GATED ? (i - BM) / 64 * 32 + (i - BM) % 32 + ((i - BM) & 32 ? half : 0) : i - BM;
+      power_off[j] = (uint32_t)(row * (i < BM ? a.a_stride : a.b_stride)) + row_bytes + lane / 32 * 16;
     }
   }
-  int sa1[kMx ? MT : 1] = {}, sb1[kMx ? NT : 1] = {};   // the next step's
-  const auto scales = [&](int64_t s) {
+  const unsigned char *power_a = oa.base, *power_b = ob.base;
+  const int power_end_a = oa.left - row_bytes, power_end_b = ob.left - row_bytes;   // the last row's first byte
+  const auto load_powers = [&](int64_t s) {   // of steps s .. s + 3
     if constexpr (kMx) {
-      // blocks past the row's last read as 2^-127 (their codes are zero)
+      const int whole = (row_bytes + a.C / 32 + 15) / 16 * 16;   // bytes of a packed row
+#pragma unroll
+      for (int j = 0; j < kPowerLoads; ++j) {
+        const int i0 = (wave * kPowerLoads + j) * 32;
+        const bool is_a = i0 < BM;
+        direct_load(is_a ? power_a : power_b, (is_a ? power_end_a : power_end_b) + whole, power_off[j] + (uint32_t)(s * 8),
+                    powers[(s / 4) & 1] + i0 * 32);
+      }
+    }
+  };
+  // The two powers of fragment row `row` + r in step s; blocks past the row's
+  // last count as 2^-127 (their codes are zero).
+  const auto read_power = [&](int64_t s, int row) -> int {
+    if constexpr (kMx) {
       const int left = a.C / 32 - (int)s * 8 - 2 * q;
       const int mask = left >= 2 ? 0xffff : left == 1 ? 0xff : 0;
-      const int64_t at = left > 0 ? s * 8 : 0;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) sa1[i] = left > 0 ? *(const uint16_t*)(qa[i] + at) & mask : 0;
-#pragma unroll
-      for (int i = 0; i < NT; ++i) sb1[i] = left > 0 ? *(const uint16_t*)(qb[i] + at) & mask : 0;
+      const unsigned char* at = powers[(s / 4) & 1] + ((s & 2) << 8) + (s & 1) * 8 + 2 * q + r * 16;
+      return *(const uint16_t*)(at + row / 32 * 1024 + row % 32 * 16) & mask;
     }
+    return 0;
+  };
+  const auto read_a = [&](int64_t s, int kk, int i) {
+    return frag(lds[s & 1], std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
+  };
+  const auto read_b = [&](int64_t s, int kk, int i) {
+    return frag(lds[s & 1] + BM * kStep, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
+  };
+  static_assert(NT <= MT && decltype(oa)::kLoads + decltype(ob)::kLoads == MT, "one load and at most one fragment of each operand per row of products");
+  constexpr int kLoadsA = decltype(oa)::kLoads, kLoads = MT;
+  const auto issue = [&](int64_t s, int j) {
+    if (j < kLoadsA) oa.issue(lds[s & 1], wave, j);
+    else ob.issue(lds[s & 1] + BM * kStep, wave, j - kLoadsA);
+  };
+  const auto load = [&](int64_t s) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) issue(s, j);
+    oa.next(lane);
+    ob.next(lane);
   };
 
   f32x4 acc[MT][NT] = {};
-  oa.load(lds[0], wave, lane);
-  ob.load(lds[0] + BM * kStep, wave, lane);
-  scales(0);
+  // One row of fragments: i of the rows' by all of the columns'.
+  const auto multiply = [&](auto half_step, int i, const i32x4& fa, const i32x4 (&fb)[NT], int sa, const int (&sb)[NT]) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      if constexpr (kMx) {
+        constexpr int kk = decltype(half_step)::value;
+        const i32x8 wa = {fa[0], fa[1], fa[2], fa[3], 0, 0, 0, 0};
+        const i32x8 wb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, kk, sb[j], kk, sa);
+      } else {
+        using F = typename Frag<T>::type;
+        acc[i][j] = mma(__builtin_bit_cast(F, fb[j]), __builtin_bit_cast(F, fa), acc[i][j]);
+      }
+    }
+  };
+
+  // A step is two halves of 32 16-bit (128 4-bit) values.  While one half is
+  // multiplied the next one's fragments are read; in the middle of a step its
+  // LDS half has been read by all and takes the loads of the step after next.
+  // Steps past the last load zeros that nothing multiplies.
+  i32x4 fa0[MT], fb0[NT], fa1[MT], fb1[NT];
+  int sa[MT] = {}, sb[NT] = {};
+  if (steps > 0) {
+    load_powers(0);
+    load(0);
+    load(1);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa0[i] = read_a(0, 0, i);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) fb0[i] = read_b(0, 0, i);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sa[kMx ? i : 0] = read_power(0, (wm * MT + i) * 16);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sb[kMx ? i : 0] = read_power(0, BM + (wn * NT + i) * 16);
+  }
   for (int64_t s = 0; s < steps; ++s) {
-    // this step's bytes are there, and no wavefront reads the other half any more
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      fa1[i] = read_a(s, 1, i);
+      if (i < NT) fb1[i] = read_b(s, 1, i);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(std::integral_constant<int, 0>{}, i, fa0[i], fb0, sa[kMx ? i : 0], sb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (s + 1 < steps) {
-      oa.load(lds[(s + 1) & 1], wave, lane);
-      ob.load(lds[(s + 1) & 1] + BM * kStep, wave, lane);
+    if (kMx && ((s + 2) & 3) == 0) load_powers(s + 2);
+    // one load between rows of products: issued together they would hold up
+    // every wavefront's matrix instructions behind the CU's one load path
+    int sb1[NT] = {};
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      issue(s + 2, i);
+      fa0[i] = read_a(s + 1, 0, i);
+      if (i < NT) {
+        fb0[i] = read_b(s + 1, 0, i);
+        if (kMx) sb1[i] = read_power(s + 1, BM + (wn * NT + i) * 16);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(std::integral_constant<int, 1>{}, i, fa1[i], fb1, sa[kMx ? i : 0], sb);
+      __builtin_amdgcn_sched_barrier(0);
+      if (kMx) sa[i] = read_power(s + 1, (wm * MT + i) * 16);
     }
+    oa.next(lane);
+    ob.next(lane);
     if constexpr (kMx) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) sa[i] = sa1[i];
-#pragma unroll
       for (int i = 0; i < NT; ++i) sb[i] = sb1[i];
-      scales(s + 1);
-    }
-    const unsigned char *la = lds[s & 1], *lb = la + BM * kStep;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      i32x4 fa[MT], fb[NT];
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-        fb[i] = frag(lb, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-        fa[i] = frag(la, std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          if constexpr (kMx) {
-            const i32x8 wa = {fa[i][0], fa[i][1], fa[i][2], fa[i][3], 0, 0, 0, 0};
-            const i32x8 wb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
-            acc[i][j] = kk == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, 0, sb[j], 0, sa[i])
-                                : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, 1, sb[j], 1, sa[i]);
-          } else {
-            using F = typename Frag<T>::type;
-            acc[i][j] = mma(__builtin_bit_cast(F, fb[j]), __builtin_bit_cast(F, fa[i]), acc[i][j]);
-          }
-        }
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last loads end before the LDS is another workgroup's
 
   const auto put = [&](unsigned char* at, f32x4 v) {
     u32x2 o;
@@ -375,7 +452,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
       for (int j = 0; j < NT / 2; ++j) {
         const int n = n0 + wn * NT * 8 + j * 16 + q * 4;
         if (n >= a.N) continue;
-        const f32x4 gate = acc[i][j], up = acc[i][j + NT / 2];
+        const f32x4 gate = acc[i][j / 2 * 4 + j % 2], up = acc[i][j / 2 * 4 + j % 2 + 2];
         f32x4 h;
 #pragma unroll
         for (int v = 0; v < 4; ++v) h[v] = silu(gate[v]) * up[v];
