@@ -10,12 +10,9 @@
 // operands in 4-bit blocks (mx.hip) on the scaled matrix instruction, which
 // multiplies the values and applies the blocks' powers of two itself.
 //
-// A workgroup makes one tile of BM rows by BN columns of one expert.  Tiles
-// are numbered without a count of any expert's: expert e owns the slots from
-// floor(offsets[e] / BM) + e on, at least as many as its rows need, and a
-// slot past its rows is empty.  So the grid follows from the buffer's size,
-// and a tile finds its expert by counting the experts whose first slot is at
-// or below its own.
+// A workgroup makes tiles of BM rows by BN columns of one expert.  Row tiles
+// are numbered expert after expert from the offsets, by every wavefront for
+// itself; the grid follows from the buffer's size.
 //
 // Each step of the contraction brings 128 bytes of every row of both operands
 // to LDS (64 16-bit values, or 256 4-bit ones) by direct loads, double
@@ -32,6 +29,7 @@
 // neighbours in the output row.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "internal.h"
@@ -63,28 +61,65 @@ struct ProductArgs {
   int32_t* status;
 };
 
+// The offsets do not change while a kernel runs: they are read by scalar loads,
+// which a wavefront need not wait for behind its loads to LDS.
+__device__ inline int64_t offset_at(const ProductArgs& a, int e) {
+  return ((const __attribute__((address_space(4))) int64_t*)a.offsets)[e];
+}
+
 struct Group { int e; int64_t lo, hi; };   // an expert and its rows, inside the buffer
 
-__device__ inline Group group_of(const ProductArgs& a, int e) {
-  Group g{e, a.offsets[e], a.offsets[e + 1]};
+__device__ inline void clamp(const ProductArgs& a, Group& g) {
   g.lo = g.lo < 0 ? 0 : g.lo > a.R ? a.R : g.lo;
   g.hi = g.hi < g.lo ? g.lo : g.hi > a.R ? a.R : g.hi;
+}
+__device__ inline Group group_of(const ProductArgs& a, int e) {
+  Group g{e, offset_at(a, e), offset_at(a, e + 1)};
+  clamp(a, g);
   return g;
 }
 
-// The expert that owns tile slot `slot` of `BM` rows, or -1.
-template <int BM> __device__ inline int expert_of_slot(const ProductArgs& a, int64_t slot) {
-  const int lane = threadIdx.x % 64;
-  int n = 0;
-  for (int e0 = 0; e0 < a.L; e0 += 64) {
-    const int e = e0 + lane;
-    const bool in = e < a.L && a.offsets[e] / BM + e <= slot;
-    const unsigned long long m = __ballot(in);
-    n += __popcll(m);
-    if (m != ~0ull) break;
+// Row tiles of BM rows, expert after expert.  Lane l of every wavefront holds
+// the first tile of its run of experts (one each up to 64 experts).
+template <int BM> struct RowTiles {
+  int run;         // experts of a lane
+  int64_t first;   // this lane's first tile
+  int64_t total;
+
+  __device__ static int64_t of(const Group& g) { return (g.hi - g.lo + BM - 1) / BM; }
+  __device__ void init(const ProductArgs& a, int lane) {
+    run = (a.L + 63) / 64;
+    int64_t sum = 0;
+    for (int e = lane * run; e < min((lane + 1) * run, a.L); ++e) {
+      Group g{e, a.offsets[e], a.offsets[e + 1]};
+      clamp(a, g);
+      sum += of(g);
+    }
+    int64_t incl = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t v = __shfl_up(incl, d);
+      incl += lane >= d ? v : 0;
+    }
+    first = incl - sum;
+    total = __shfl(incl, 63);
+    total = (int64_t)((uint64_t)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32 |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((int)total));
   }
-  return __builtin_amdgcn_readfirstlane(n) - 1;
-}
+  // The expert of tile `t` (below the total) and the first row of the tile.
+  __device__ Group find(const ProductArgs& a, int64_t t, int64_t* m0) const {
+    const int l = __popcll(__ballot(first <= t)) - 1;
+    t -= (int64_t)((uint64_t)__builtin_amdgcn_readlane((int)(first >> 32), l) << 32 |
+                   (uint32_t)__builtin_amdgcn_readlane((int)first, l));
+    Group g = group_of(a, l * run);
+    while (t >= of(g) && g.e + 1 < min((l + 1) * run, a.L)) {
+      t -= of(g);
+      g = group_of(a, g.e + 1);
+    }
+    *m0 = g.lo + t * BM;
+    return g;
+  }
+};
 
 // Offsets that decrease or pass the buffer are the caller's error; products
 // stay inside the buffers all the same.
@@ -106,6 +141,7 @@ __device__ inline float silu(float g) { return g / (1.0f + expf(-g)); }
 // ---------------------------------------------------------------- tiled products
 
 constexpr int kStep = 128;   // bytes of a row that one step of the contraction takes
+constexpr int kCus = 256;
 
 // Starts a direct load of 16 bytes per lane from `off` of `bytes` bytes at
 // `base` to 1 KB of LDS at `lds` (both the same for the whole wavefront).  It
@@ -115,10 +151,11 @@ constexpr int kStep = 128;   // bytes of a row that one step of the contraction 
 __device__ inline void direct_load(const unsigned char* base, int bytes, uint32_t off, unsigned char* lds) {
 #ifdef __HIP_DEVICE_COMPILE__
   const uint64_t b = (uint64_t)base;
-  const i32x4 rsrc = {(int)(uint32_t)b, (int)((b >> 32) & 0xffff), bytes, 0x00020000};
-  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+  const auto same = [](uint32_t v) { return __builtin_amdgcn_readfirstlane((int)v); };   // in scalar registers
+  const i32x4 rsrc = {same((uint32_t)b), same((uint32_t)(b >> 32) & 0xffff), same(bytes), 0x00020000};
+  const int at = same((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(at), "v"(off), "s"(rsrc) : "memory", "m0");
+               :: "s"(at), "v"(off), "s"(rsrc) : "memory");   // nothing else in these kernels uses m0
 #endif
 }
 
@@ -139,7 +176,8 @@ template <int ROWS, bool COLS, int WAVES> struct Operand {
   uint32_t past;               // rows by contraction: added where the lane's chunk lies past the row's end
   uint32_t off[kLoads];
 
-  // For rows by contraction `row_of(i)` gives the buffer row of operand row i, relative to `base`.
+  // Once: this lane's offsets.  For rows by contraction `row_of(i)` gives the
+  // buffer row of operand row i, relative to `base`.
   template <typename F> __device__ void init(int wave, int lane, F row_of) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
@@ -151,6 +189,11 @@ template <int ROWS, bool COLS, int WAVES> struct Operand {
         off[j] = (uint32_t)(row_of(i) * stride) + ((lane & 7) ^ (i & 7)) * 16;
       }
     }
+  }
+  __device__ void start(const unsigned char* at, int left_, int width_, int lane) {
+    base = at;
+    left = left_;
+    width = width_;
     bounds(lane);
   }
   __device__ void bounds(int lane) {
@@ -179,7 +222,19 @@ template <typename T> struct Mx { using out = T; };   // both operands in 4-bit 
 template <typename T> struct Elem { using out = T; static constexpr bool mx = false; };
 template <typename T> struct Elem<Mx<T>> { using out = T; static constexpr bool mx = true; };
 
-// WM x WN wavefronts, each with MT x NT fragments of 16 x 16 results.
+// Where a tile's operands begin and how much of them there is (see Operand),
+// and its results.
+struct TileAt {
+  const unsigned char *a, *b;
+  int a_left, a_width, b_left, b_width, steps;
+  unsigned char *out, *pre;
+  int rows, cols;   // of the tile, inside the output
+};
+
+// WM x WN wavefronts, each with MT x NT fragments of 16 x 16 results.  A
+// workgroup takes every gridDim / 8-th tile of its XCD's and runs through
+// their steps as one stream: the loads are two steps ahead, so that the next
+// tile's first steps arrive while this one's results are written.
 template <typename T, int MODE, bool GATED, int WM, int WN, int MT, int NT>
 __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host's pass knows none of the builtins below
@@ -187,91 +242,120 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   constexpr bool kMx = Elem<T>::mx, kColsA = MODE == kGradW, kColsB = MODE != kForward;
   constexpr int BM = WM * MT * 16, BN = WN * NT * 16, kWaves = WM * WN;
   constexpr int kTileN = GATED ? BN / 2 : BN;   // output columns
+  constexpr int kSize = MODE == kGradW ? 4 : 2;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2][(BM + BN) * kStep];
   // 4-bit blocks: the powers of two of four steps, 32 bytes a row, double buffered
   __shared__ __attribute__((aligned(1024))) unsigned char powers[kMx ? 2 : 1][kMx ? (BM + BN) * 32 : 16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, q = lane / 16;
+  const int wm = wave / WN, wn = wave % WN;
+  const int half = a.half;
+  const int row_bytes = kMx ? a.C / 2 : a.C * 2;
   if (blockIdx.x == 0) check_offsets(a);
 
-  // which tile: XCD x (block % 8) takes a contiguous eighth of the tiles (of
-  // every expert's, for grad w), in blocks of eight row tiles by all columns
-  const int nt = (a.N + kTileN - 1) / kTileN;
-  const int xcd = blockIdx.x & 7;
-  const int64_t idx = blockIdx.x >> 3;
-  constexpr int kBand = 8;
-  Group g;
-  int64_t m0, slot;
-  int ni;
-  if (MODE == kGradW) {
-    const int mt = (a.M + BM - 1) / BM;
-    const int64_t per = ((int64_t)mt * nt + 7) / 8;
-    const int64_t e = idx / per, t = xcd * per + idx % per;
-    if (e >= a.L || t >= (int64_t)mt * nt) return;
-    const int band = (int)(t / (kBand * nt)), in = (int)(t % (kBand * nt));
-    const int high = min(kBand, mt - band * kBand);
-    slot = band * kBand + in % high;
-    ni = in / high;
-    g = group_of(a, (int)e);
-    m0 = slot * BM;
-  } else {
-    int64_t rows = a.offsets[a.L];
-    rows = rows < 0 ? 0 : rows > a.R ? a.R : rows;
-    const int64_t slots = rows / BM + a.L, total = slots * nt, per = (total + 7) / 8, t = xcd * per + idx;
-    if (idx >= per || t >= total) return;
-    const int64_t band = t / (kBand * nt);
-    const int in = (int)(t % (kBand * nt));
-    const int high = (int)min((int64_t)kBand, slots - band * kBand);
-    slot = band * kBand + in % high;
-    ni = in / high;
-    const int e = expert_of_slot<BM>(a, slot);
-    if (e < 0) return;
-    g = group_of(a, e);
-    m0 = g.lo + (slot - (a.offsets[e] / BM + e)) * BM;
-    if (m0 < g.lo || m0 >= g.hi) return;
+  // Tiles: XCD x (block % 8) takes a contiguous eighth of them (of every
+  // expert's, for grad w), in bands of four row tiles by all columns: what 32
+  // workgroups hold at a time (4 by 8 tiles) shares most of its bytes in the
+  // XCD's L2 (bands of 4, 8, 16, 32: 1.21, 1.18, 1.15, 1.11 PFLOP/s, 32768
+  // rows, 4096 x 4096, gated).
+  constexpr int kBand = 4;
+  const int nt = (a.N + kTileN - 1) / kTileN, mt = MODE == kGradW ? (a.M + BM - 1) / BM : 0;
+  RowTiles<BM> row_tiles;
+  int64_t slots = mt;   // row tiles
+  if (MODE != kGradW) {
+    row_tiles.init(a, lane);
+    slots = row_tiles.total;
   }
-  const int n0 = ni * kTileN;
+  const int64_t per = (slots * nt + 7) / 8;   // this XCD's tiles
+  const int64_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW ? per * a.L : per;
+  const auto tile_at = [&](int64_t idx, TileAt& t) -> bool {
+    const int64_t in_xcd = MODE == kGradW ? idx % per : idx, at = (blockIdx.x & 7) * per + in_xcd;
+    if (at >= slots * nt) return false;
+    const int64_t band = at / (kBand * nt);
+    const int in = (int)(at - band * (kBand * nt)), high = (int)min((int64_t)kBand, slots - band * kBand);
+    const int64_t slot = band * kBand + in % high;
+    const int n0 = in / high * kTileN;
+    Group g;
+    int64_t m0;
+    if (MODE == kGradW) {
+      g = group_of(a, (int)(idx / per));
+      m0 = slot * BM;
+      t.rows = (int)min((int64_t)BM, a.M - m0);
+    } else {
+      g = row_tiles.find(a, slot, &m0);
+      t.rows = (int)min((int64_t)BM, g.hi - m0);
+    }
+    const int rows = (int)(g.hi - g.lo);
+    if (MODE == kGradW) {
+      t.a = a.a + g.lo * a.a_stride + m0 * 2;
+      t.b = a.b + g.lo * a.b_stride + n0 * 2;
+      t.a_left = t.b_left = rows;
+      t.a_width = (int)(a.M - m0) * 2;
+      t.b_width = (a.N - n0) * 2;
+      t.steps = max((rows + 63) / 64, 1);   // an expert without rows: zeros
+    } else {
+      t.a = a.a + m0 * a.a_stride;
+      t.a_left = (t.rows - 1) * (int)a.a_stride + row_bytes;
+      t.a_width = row_bytes;
+      t.steps = (row_bytes + kStep - 1) / kStep;
+      if (MODE == kGradX) {
+        t.b = a.b + g.e * a.b_expert + n0 * 2;
+        t.b_left = a.C;
+        t.b_width = (a.N - n0) * 2;
+      } else {
+        // gated: of every 64 operand rows the first 32 are gate rows, the others the same up rows
+        t.b = a.b + g.e * a.b_expert + n0 * a.b_stride;
+        const int64_t end = ((int64_t)(GATED ? half + a.N : a.N) - n0 - 1) * a.b_stride + row_bytes;
+        t.b_left = (int)min(end, (int64_t)(GATED ? half + kTileN : BN) * a.b_stride);
+        t.b_width = row_bytes;
+      }
+    }
+    t.cols = min(kTileN, a.N - n0);
+    t.out = a.out + (MODE == kGradW ? g.e * a.b_expert : 0) + m0 * a.out_stride + (int64_t)n0 * kSize;
+    t.pre = GATED && a.pre ? a.pre + m0 * a.pre_stride + (int64_t)n0 * 2 : nullptr;
+    return true;
+  };
+  const auto find = [&](int64_t& idx, TileAt& t) {   // the first tile at or after idx
+    for (; idx < last; idx += stride)
+      if (tile_at(idx, t)) return true;
+    return false;
+  };
 
-  // operands and the steps of the contraction
-  const int64_t rows = g.hi - g.lo;
-  const int64_t C = MODE == kGradW ? rows : a.C;               // elements
-  const int row_bytes = kMx ? a.C / 2 : a.C * 2;
-  const int64_t steps = MODE == kGradW || MODE == kGradX ? (C + 63) / 64 : (row_bytes + kStep - 1) / kStep;
+  // what is loaded, two steps ahead of what is multiplied
   Operand<BM, kColsA, kWaves> oa;
   Operand<BN, kColsB, kWaves> ob;
+  TileAt ahead;
+  int64_t load_idx = first;
+  int load_step = 0, load_group = 0;
+  if (!find(load_idx, ahead)) return;
+  int64_t idx = load_idx;
+  const auto begin = [&] {
+    oa.start(ahead.a, ahead.a_left, ahead.a_width, lane);
+    ob.start(ahead.b, ahead.b_left, ahead.b_width, lane);
+  };
   oa.stride = (int)a.a_stride;
   ob.stride = (int)a.b_stride;
-  if (kColsA) {
-    oa.base = a.a + g.lo * a.a_stride + m0 * 2;
-    oa.left = (int)rows;
-    oa.width = (int)((a.M - m0) * 2);
-  } else {
-    oa.base = a.a + m0 * a.a_stride;
-    const int64_t valid = min((int64_t)BM, g.hi - m0);
-    oa.left = (int)((valid - 1) * a.a_stride) + row_bytes;
-    oa.width = row_bytes;
-  }
   oa.init(wave, lane, [](int i) { return i; });
-  if (MODE == kGradW) {
-    ob.base = a.b + g.lo * a.b_stride + n0 * 2;
-    ob.left = (int)rows;
-    ob.width = (a.N - n0) * 2;
-  } else if (MODE == kGradX) {
-    ob.base = a.b + g.e * a.b_expert + n0 * 2;
-    ob.left = a.C;
-    ob.width = (a.N - n0) * 2;
-  } else {
-    // gated: of every 64 operand rows the first 32 are gate rows, the others the same up rows
-    ob.base = a.b + g.e * a.b_expert + (int64_t)n0 * a.b_stride;
-    const int64_t end = ((int64_t)(GATED ? a.half + a.N : a.N) - n0 - 1) * a.b_stride + row_bytes;
-    ob.left = (int)min(end, (int64_t)(GATED ? a.half + kTileN : BN) * a.b_stride);
-    ob.width = row_bytes;
-  }
-  const int half = a.half;
   ob.init(wave, lane, [=](int i) { return GATED ? i / 64 * 32 + i % 32 + (i & 32 ? half : 0) : i; });
+  begin();
+  const auto advance = [&] {
+    if (++load_step < ahead.steps) {
+      oa.next(lane);
+      ob.next(lane);
+      return;
+    }
+    load_idx += stride;
+    load_step = 0;
+    if (find(load_idx, ahead)) {
+      begin();
+    } else {   // nothing is left: the loads bring zeros that nothing multiplies
+      ahead.steps = 0x7fffffff;
+      oa.start(ahead.a, 0, 0, lane);
+      ob.start(ahead.b, 0, 0, lane);
+    }
+  };
 
   // places of this lane's fragments in LDS
-  const int wm = wave / WN, wn = wave % WN;
   const auto chunk = [=](int kk) { return kMx ? 2 * q + kk : 4 * kk + q; };
   uint32_t pa[kColsA ? MT : 1], pb[kColsB ? NT : 1];
   if (kColsA) {
@@ -299,6 +383,12 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
       return *(const i32x4*)(p + place + i * 16 * kStep + (chunk(kk) ^ (r & 7)) * 16);
     }
   };
+  const auto read_a = [&](int pos, int kk, int i) {
+    return frag(lds[pos & 1], std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
+  };
+  const auto read_b = [&](int pos, int kk, int i) {
+    return frag(lds[pos & 1] + BM * kStep, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
+  };
 
   // 4-bit blocks: a load covers 32 rows' powers of four steps, first their
   // first 16 bytes (two steps), then the others; a lane's two blocks of a step
@@ -309,58 +399,55 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   if constexpr (kMx) {
 #pragma unroll
     for (int j = 0; j < kPowerLoads; ++j) {
-      const int i = (wave * kPowerLoads + j) * 32 + lane % 32;
-      const int64_t row = i < BM ? i : GATED ? (i - BM) / 64 * 32 + (i - BM) % 32 + ((i - BM) & 32 ? half : 0) : i - BM;
-      power_off[j] = (uint32_t)(row * (i < BM ? a.a_stride : a.b_stride)) + row_bytes + lane / 32 * 16;
+      const int i = (wave * kPowerLoads + j) * 32 + lane % 32, n = i - BM;
+      const int row = i < BM ? i : GATED ? n / 64 * 32 + n % 32 + (n & 32 ? half : 0) : n;
+      power_off[j] = (uint32_t)(row * (i < BM ? oa.stride : ob.stride)) + row_bytes + lane / 32 * 16;
     }
   }
-  const unsigned char *power_a = oa.base, *power_b = ob.base;
-  const int power_end_a = oa.left - row_bytes, power_end_b = ob.left - row_bytes;   // the last row's first byte
-  const auto load_powers = [&](int64_t s) {   // of steps s .. s + 3
+  const auto load_powers = [&] {   // of the next four steps to load
     if constexpr (kMx) {
-      const int whole = (row_bytes + a.C / 32 + 15) / 16 * 16;   // bytes of a packed row
+      if (load_step % 4 != 0) return;
+      const int tail = (row_bytes + a.C / 32 + 15) / 16 * 16 - row_bytes;   // a packed row's bytes after the codes
 #pragma unroll
       for (int j = 0; j < kPowerLoads; ++j) {
         const int i0 = (wave * kPowerLoads + j) * 32;
         const bool is_a = i0 < BM;
-        direct_load(is_a ? power_a : power_b, (is_a ? power_end_a : power_end_b) + whole, power_off[j] + (uint32_t)(s * 8),
-                    powers[(s / 4) & 1] + i0 * 32);
+        direct_load(is_a ? ahead.a : ahead.b, (is_a ? ahead.a_left : ahead.b_left) + tail,
+                    power_off[j] + (uint32_t)(load_step * 8), powers[load_group & 1] + i0 * 32);
       }
+      ++load_group;
     }
   };
-  // The two powers of fragment row `row` + r in step s; blocks past the row's
+  // The two powers of fragment row `row` + r in a step; blocks past the row's
   // last count as 2^-127 (their codes are zero).
-  const auto read_power = [&](int64_t s, int row) -> int {
+  const auto read_power = [&](int group, int step, int row) -> int {
     if constexpr (kMx) {
-      const int left = a.C / 32 - (int)s * 8 - 2 * q;
+      const int left = a.C / 32 - step * 8 - 2 * q;
       const int mask = left >= 2 ? 0xffff : left == 1 ? 0xff : 0;
-      const unsigned char* at = powers[(s / 4) & 1] + ((s & 2) << 8) + (s & 1) * 8 + 2 * q + r * 16;
+      const unsigned char* at = powers[group & 1] + ((step & 2) << 8) + (step & 1) * 8 + 2 * q + r * 16;
       return *(const uint16_t*)(at + row / 32 * 1024 + row % 32 * 16) & mask;
     }
     return 0;
   };
-  const auto read_a = [&](int64_t s, int kk, int i) {
-    return frag(lds[s & 1], std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
-  };
-  const auto read_b = [&](int64_t s, int kk, int i) {
-    return frag(lds[s & 1] + BM * kStep, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
-  };
-  static_assert(NT <= MT && decltype(oa)::kLoads + decltype(ob)::kLoads == MT, "one load and at most one fragment of each operand per row of products");
-  constexpr int kLoadsA = decltype(oa)::kLoads, kLoads = MT;
-  const auto issue = [&](int64_t s, int j) {
-    if (j < kLoadsA) oa.issue(lds[s & 1], wave, j);
-    else ob.issue(lds[s & 1] + BM * kStep, wave, j - kLoadsA);
-  };
-  const auto load = [&](int64_t s) {
+
+  constexpr int kLoadsA = decltype(oa)::kLoads, kLoadsB = decltype(ob)::kLoads;
+  static_assert(NT + 4 == MT && kLoadsA == 4 && kLoadsB == 4, "the loads' places among the rows of products");
+  const auto issue_a = [&](int pos, int j) { oa.issue(lds[pos & 1], wave, j); };
+  const auto issue_b = [&](int pos, int j) { ob.issue(lds[pos & 1] + BM * kStep, wave, j); };
+  const auto load = [&](int pos) {
+    load_powers();
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) issue(s, j);
-    oa.next(lane);
-    ob.next(lane);
+    for (int j = 0; j < 4; ++j) issue_b(pos, j);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) issue_a(pos, j);
+    advance();
   };
 
   f32x4 acc[MT][NT] = {};
   // One row of fragments: i of the rows' by all of the columns'.
   const auto multiply = [&](auto half_step, int i, const i32x4& fa, const i32x4 (&fb)[NT], int sa, const int (&sb)[NT]) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       if constexpr (kMx) {
@@ -373,105 +460,163 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
         acc[i][j] = mma(__builtin_bit_cast(F, fb[j]), __builtin_bit_cast(F, fa), acc[i][j]);
       }
     }
+    // the compiler would move these pure instructions past the barriers, to where the sums are next used
+#pragma unroll
+    for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
   };
 
-  // A step is two halves of 32 16-bit (128 4-bit) values.  While one half is
-  // multiplied the next one's fragments are read; in the middle of a step its
-  // LDS half has been read by all and takes the loads of the step after next.
-  // Steps past the last load zeros that nothing multiplies.
-  i32x4 fa0[MT], fb0[NT], fa1[MT], fb1[NT];
-  int sa[MT] = {}, sb[NT] = {};
-  if (steps > 0) {
-    load_powers(0);
-    load(0);
-    load(1);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < MT; ++i) fa0[i] = read_a(0, 0, i);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) fb0[i] = read_b(0, 0, i);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sa[kMx ? i : 0] = read_power(0, (wm * MT + i) * 16);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) sb[kMx ? i : 0] = read_power(0, BM + (wn * NT + i) * 16);
-  }
-  for (int64_t s = 0; s < steps; ++s) {
+  // Results go through a descriptor of the tile's rows inside the output; what
+  // lies outside is dropped there, so every wavefront issues the same number
+  // of stores.  Neighbouring 16-lane rows exchange halves of two fragments,
+  // after which a lane holds eight neighbouring 16-bit results.
+  constexpr int kStores = MODE == kGradW ? MT * NT : GATED ? MT * NT / 4 : MT * NT / 2;
+  const auto put = [&](unsigned char* base, int64_t row_stride, int rows, int cols, auto value) {
+    const int bytes = rows > 0 ? (rows - 1) * (int)row_stride + cols * kSize : 0;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(base, 0, bytes, 0x00020000);
+    constexpr int kCols = GATED ? NT / 2 : NT;   // output fragments of a wavefront's row
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      fa1[i] = read_a(s, 1, i);
-      if (i < NT) fb1[i] = read_b(s, 1, i);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(std::integral_constant<int, 0>{}, i, fa0[i], fb0, sa[kMx ? i : 0], sb);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (kMx && ((s + 2) & 3) == 0) load_powers(s + 2);
-    // one load between rows of products: issued together they would hold up
-    // every wavefront's matrix instructions behind the CU's one load path
-    int sb1[NT] = {};
+      const uint32_t row = (uint32_t)(((wm * MT + i) * 16 + r) * (int)row_stride);
+      if constexpr (MODE == kGradW) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      issue(s + 2, i);
-      fa0[i] = read_a(s + 1, 0, i);
-      if (i < NT) {
-        fb0[i] = read_b(s + 1, 0, i);
-        if (kMx) sb1[i] = read_power(s + 1, BM + (wn * NT + i) * 16);
+        for (int j = 0; j < kCols; ++j) {
+          const int n = (wn * kCols + j) * 16 + q * 4;
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, value(i, j)), rsrc,
+                                                     n < cols ? row + n * 4 : 0x60000000u, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kCols; j += 2) {
+          u32x2 p[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const f32x4 v = value(i, j + u);
+            p[u].x = from_f32<Out>(v[0]).u | (uint32_t)from_f32<Out>(v[1]).u << 16;
+            p[u].y = from_f32<Out>(v[2]).u | (uint32_t)from_f32<Out>(v[3]).u << 16;
+          }
+          const auto x = __builtin_amdgcn_permlane16_swap(p[0].x, p[1].x, false, false);
+          const auto y = __builtin_amdgcn_permlane16_swap(p[0].y, p[1].y, false, false);
+          const u32x4 o = {x[0], y[0], x[1], y[1]};
+          const int n = (wn * kCols + j + (q & 1)) * 16 + (q >> 1) * 8;
+          __builtin_amdgcn_raw_buffer_store_b128(o, rsrc, n < cols ? row + n * 2 : 0x60000000u, 0, 0);
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(std::integral_constant<int, 1>{}, i, fa1[i], fb1, sa[kMx ? i : 0], sb);
-      __builtin_amdgcn_sched_barrier(0);
-      if (kMx) sa[i] = read_power(s + 1, (wm * MT + i) * 16);
     }
-    oa.next(lane);
-    ob.next(lane);
-    if constexpr (kMx) {
+  };
+  const auto write = [&](const TileAt& t) {
+    if constexpr (GATED) {
+      // a wavefront's columns: of every four fragments two of the gate, then the same two of the up half
+      const auto gate = [&](int i, int j) { return acc[i][j / 2 * 4 + j % 2]; };
+      const auto up = [&](int i, int j) { return acc[i][j / 2 * 4 + j % 2 + 2]; };
+      if (t.pre) {
+        put(t.pre, a.pre_stride, t.rows, t.cols, gate);
+        put(t.pre + (int64_t)half * 2, a.pre_stride, t.rows, t.cols, up);
+      }
+      put(t.out, a.out_stride, t.rows, t.cols, [&](int i, int j) {
+        const f32x4 g = gate(i, j), u = up(i, j);
+        f32x4 h;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) sb[i] = sb1[i];
+        for (int v = 0; v < 4; ++v) h[v] = silu(g[v]) * u[v];
+        return h;
+      });
+    } else {
+      put(t.out, a.out_stride, t.rows, t.cols, [&](int i, int j) { return acc[i][j]; });
+    }
+  };
+
+  // A step is two halves of 32 16-bit (128 4-bit) values, each eight rows of
+  // products.  A row's fragment is replaced by its next half's as soon as the
+  // row is done, so one set of them is enough; the columns' are read half a
+  // step ahead.  Once every wavefront has read a step's columns (in its first
+  // half) or rows (after the second half's first row) their place takes the
+  // loads of the step after next.  These are spread between the rows of
+  // products: issued together they hold up every wavefront's matrix
+  // instructions behind the CU's one load path.
+  constexpr std::integral_constant<int, 0> kFirst{};
+  constexpr std::integral_constant<int, 1> kSecond{};
+  i32x4 fa[MT], fb0[NT], fb1[NT];
+  int sa[MT] = {}, sb[NT] = {};
+  int steps = ahead.steps, step = 0, group = 0;
+  load(0);
+  load(1);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < MT; ++i) fa[i] = read_a(0, 0, i);
+#pragma unroll
+  for (int i = 0; i < NT; ++i) fb0[i] = read_b(0, 0, i);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) sa[i] = read_power(0, 0, (wm * MT + i) * 16);
+#pragma unroll
+  for (int i = 0; i < NT; ++i) sb[i] = read_power(0, 0, BM + (wn * NT + i) * 16);
+  bool stored = false;
+  for (int pos = 0;; ++pos) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      if (i < NT) fb1[i] = read_b(pos, 1, i);
+      if (i == NT + 1) {
+        issue_b(pos + 2, 0);
+        issue_b(pos + 2, 1);
+      } else if (i > NT + 1) {
+        issue_b(pos + 2, i - NT);
+      }
+      multiply(kFirst, i, fa[i], fb0, sa[i], sb);
+      if (i == NT) {   // every wavefront has read the step's columns
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      fa[i] = read_a(pos, 1, i);
+    }
+    multiply(kSecond, 0, fa[0], fb1, sa[0], sb);
+    // the next step has arrived (the stores of the tile before may be on
+    // their way), and no wavefront reads this step's half any more
+    if (stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kStores + kLoadsB) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoadsB) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const bool end = step + 1 == steps;
+    const int next_step = end ? 0 : step + 1;
+    if (next_step % 4 == 0) ++group;
+    load_powers();
+    int sb1[NT] = {};
+    fa[0] = read_a(pos + 1, 0, 0);
+    sa[0] = read_power(group, next_step, wm * MT * 16);
+#pragma unroll
+    for (int i = 1; i < MT; ++i) {
+      if (i % 2) issue_a(pos + 2, i / 2);
+      if (i <= NT) {
+        fb0[i - 1] = read_b(pos + 1, 0, i - 1);
+        sb1[i - 1] = read_power(group, next_step, BM + (wn * NT + i - 1) * 16);
+      }
+      multiply(kSecond, i, fa[i], fb1, sa[i], sb);
+      fa[i] = read_a(pos + 1, 0, i);
+      sa[i] = read_power(group, next_step, (wm * MT + i) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sb[i] = sb1[i];
+    advance();
+    stored = false;
+    ++step;
+    if (end) {
+      TileAt t;
+      tile_at(idx, t);
+      write(t);
+      stored = !t.pre;
+      idx += stride;
+      if (!find(idx, t)) break;
+      steps = t.steps;
+      step = 0;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last loads end before the LDS is another workgroup's
-
-  const auto put = [&](unsigned char* at, f32x4 v) {
-    u32x2 o;
-    o.x = from_f32<Out>(v[0]).u | (uint32_t)from_f32<Out>(v[1]).u << 16;
-    o.y = from_f32<Out>(v[2]).u | (uint32_t)from_f32<Out>(v[3]).u << 16;
-    *(u32x2*)at = o;
-  };
-  const int64_t end = MODE == kGradW ? a.M : g.hi;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t m = m0 + (wm * MT + i) * 16 + r;
-    if (m >= end) continue;
-    unsigned char* out = a.out + (MODE == kGradW ? g.e * a.b_expert : 0) + m * a.out_stride;
-    if constexpr (GATED) {
-#pragma unroll
-      for (int j = 0; j < NT / 2; ++j) {
-        const int n = n0 + wn * NT * 8 + j * 16 + q * 4;
-        if (n >= a.N) continue;
-        const f32x4 gate = acc[i][j / 2 * 4 + j % 2], up = acc[i][j / 2 * 4 + j % 2 + 2];
-        f32x4 h;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) h[v] = silu(gate[v]) * up[v];
-        put(out + n * 2, h);
-        if (a.pre) {
-          put(a.pre + m * a.pre_stride + n * 2, gate);
-          put(a.pre + m * a.pre_stride + (int64_t)(n + a.half) * 2, up);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int n = n0 + (wn * NT + j) * 16 + q * 4;
-        if (n >= a.N) continue;
-        if constexpr (MODE == kGradW) *(f32x4*)(out + (int64_t)n * 4) = acc[i][j];
-        else put(out + (int64_t)n * 2, acc[i][j]);
-      }
-    }
-  }
 #endif
 }
 
@@ -518,12 +663,15 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(GateArgs a) {
 
 namespace {
 
-// Grids cover the buffer's tiles for any offsets, rounded up to the eight XCDs.
+// One workgroup per CU runs through its share of the tiles; grad w's tiles have
+// their experts' lengths, so there every tile is a workgroup of its own and
+// the hardware hands them out.
 template <typename T, int MODE, bool GATED, int WM, int WN, int MT, int NT>
 vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
   constexpr int BM = WM * MT * 16, kTileN = WN * NT * 16 / (GATED ? 2 : 1);
   const int64_t nt = (a.N + kTileN - 1) / kTileN;
-  const int64_t per = MODE == kGradW ? (((a.M + BM - 1) / BM) * nt + 7) / 8 * a.L : ((a.R / BM + a.L) * nt + 7) / 8;
+  int64_t per = MODE == kGradW ? (((a.M + BM - 1) / BM) * nt + 7) / 8 * a.L : ((a.R / BM + a.L) * nt + 7) / 8;
+  if (MODE != kGradW) per = std::min<int64_t>(per, kCus / 8);
   if (per * 8 >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
   hipLaunchKernelGGL((product_tiled<T, MODE, GATED, WM, WN, MT, NT>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
