@@ -620,6 +620,145 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
 #endif
 }
 
+// ----------------------------------------------------------- few rows
+
+// Up to 64 rows of an expert by 32 of its weight rows (gated: 16 of the gate
+// and the same 16 of the up half).  The weights' bytes bound it, so they go
+// straight to registers, each read once with no LDS between: the four
+// wavefronts take turns on 256-byte pieces of the rows (two steps), loads one
+// piece ahead, and their sums are added in LDS in the wavefronts' order.  The
+// rows of x come from the L2.
+constexpr int kFewRows = 64, kFewCols = 32, kPiece = 256;
+
+template <typename T, bool GATED, int MT>
+__device__ inline void few_rows(const ProductArgs& a, const Group& g, int64_t m0, int n0, float* sums) {
+#ifdef __HIP_DEVICE_COMPILE__
+  using Out = typename Elem<T>::out;
+  constexpr bool kMx = Elem<T>::mx;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 16, q = lane / 16;
+  const int code_bytes = kMx ? a.C / 2 : a.C * 2;
+  const int row_bytes = kMx ? (code_bytes + a.C / 32 + 15) / 16 * 16 : code_bytes;
+  const int rows = (int)min((int64_t)(MT * 16), g.hi - m0);
+  const int sx = (int)a.a_stride, sw = (int)a.b_stride;
+  const auto rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_stride), 0, (rows - 1) * sx + row_bytes, 0x00020000);
+  const auto weights = [&](int u) {
+    const int n = GATED ? n0 : n0 + u * 16, valid = max(min(16, a.N - n), 0);
+    const unsigned char* base = a.b + g.e * a.b_expert + (int64_t)(n + (GATED ? u * a.half : 0)) * a.b_stride;
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, valid > 0 ? (valid - 1) * sw + row_bytes : 0, 0x00020000);
+  };
+  const auto rw0 = weights(0), rw1 = weights(1);
+
+  struct Piece {
+    u32x4 w[2][4], x[MT][4];
+    u32x4 ws[2], xs[MT];   // 4-bit blocks: sixteen powers of the row
+  };
+  const auto load = [&](Piece& p, int at) {   // `at`: the piece's first byte
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int byte = at + c * 64 + q * 16;
+      const uint32_t off = byte < code_bytes ? (uint32_t)byte : 0x60000000u;   // past the row: zero
+      p.w[0][c] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 2);   // not to be kept in caches
+      p.w[1][c] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 2);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) p.x[i][c] = __builtin_amdgcn_raw_buffer_load_b128(rx, off + (i * 16 + r) * sx, 0, 0);
+    }
+    if constexpr (kMx) {
+      const uint32_t off = at < code_bytes ? code_bytes + at / 16 : 0x60000000u;
+      p.ws[0] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 0);
+      p.ws[1] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 0);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) p.xs[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, off + (i * 16 + r) * sx, 0, 0);
+    }
+  };
+  f32x4 acc[2][MT] = {};
+  const auto multiply = [&](const Piece& p, int at) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if constexpr (kMx) {
+        const bool in = at + c * 64 + q * 16 < code_bytes;   // powers past the row: 2^-127, of zeros
+        const auto power = [&](const u32x4& v) { return in ? (int)(v[c] >> (8 * q) & 0xff) : 0; };
+        const auto wide = [](const u32x4& v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            acc[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(p.w[u][c]), wide(p.x[i][c]), acc[u][i], 4, 4, 0,
+                                                                         power(p.ws[u]), 0, power(p.xs[i]));
+      } else {
+        using F = typename Frag<T>::type;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) acc[u][i] = mma(__builtin_bit_cast(F, p.w[u][c]), __builtin_bit_cast(F, p.x[i][c]), acc[u][i]);
+      }
+    }
+  };
+  constexpr int kTurn = 4 * kPiece;
+  Piece p0, p1;
+  load(p0, wave * kPiece);
+  for (int at = wave * kPiece; at < code_bytes; at += 2 * kTurn) {
+    load(p1, at + kTurn);
+    multiply(p0, at);
+    load(p0, at + 2 * kTurn);
+    multiply(p1, at + kTurn);
+  }
+
+  f32x4* part = (f32x4*)sums;   // [wavefront][column tile][row tile][lane]
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) part[((wave * 2 + u) * MT + i) * 64 + lane] = acc[u][i];
+  __syncthreads();
+  for (int i = wave; i < MT; i += 4) {   // a row tile to a wavefront
+    const int64_t m = m0 + i * 16 + r;
+    f32x4 z[2] = {};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) z[u] += part[((w * 2 + u) * MT + i) * 64 + lane];
+    if (m >= g.hi) continue;
+    const auto put = [&](unsigned char* row, int n, f32x4 v) {
+      u32x2 o;
+      o.x = from_f32<Out>(v[0]).u | (uint32_t)from_f32<Out>(v[1]).u << 16;
+      o.y = from_f32<Out>(v[2]).u | (uint32_t)from_f32<Out>(v[3]).u << 16;
+      *(u32x2*)(row + (int64_t)n * 2) = o;
+    };
+    unsigned char* out = a.out + m * a.out_stride;
+    const int n = n0 + q * 4;
+    if constexpr (GATED) {
+      if (n >= a.N) continue;
+      if (a.pre) {
+        put(a.pre + m * a.pre_stride, n, z[0]);
+        put(a.pre + m * a.pre_stride, n + a.half, z[1]);
+      }
+      f32x4 h;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) h[v] = silu(z[0][v]) * z[1][v];
+      put(out, n, h);
+    } else {
+      if (n < a.N) put(out, n, z[0]);
+      if (n + 16 < a.N) put(out, n + 16, z[1]);
+    }
+  }
+#endif
+}
+
+template <typename T, bool GATED> __global__ void __launch_bounds__(256) product_few(ProductArgs a) {
+  __shared__ float sums[4 * 2 * (kFewRows / 16) * 64 * 4];
+  if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets(a);
+  RowTiles<kFewRows> tiles;
+  tiles.init(a, threadIdx.x % 64);
+  if (blockIdx.y >= tiles.total) return;
+  int64_t m0;
+  const Group g = tiles.find(a, blockIdx.y, &m0);
+  const int n0 = blockIdx.x * (GATED ? kFewCols / 2 : kFewCols);
+  const int64_t rows = g.hi - m0;
+  if (rows <= 16) few_rows<T, GATED, 1>(a, g, m0, n0, sums);
+  else if (rows <= 32) few_rows<T, GATED, 2>(a, g, m0, n0, sums);
+  else few_rows<T, GATED, 4>(a, g, m0, n0, sums);
+}
+
 // Gradient of the gate: with s = 1 / (1 + exp(-g)),
 //   dg = dh u s (1 + g (1 - s)),   du = dh g s
 // for every row of the experts; 16 bytes a thread, bound by HBM.
@@ -679,6 +818,15 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
 }
 
 template <typename T, int MODE, bool GATED> vp_status launch_product_as(const ProductArgs& a, hipStream_t s) {
+  if constexpr (MODE == kForward) {
+    const int64_t tiles = a.R / kFewRows + a.L;
+    if (a.R <= (int64_t)kFewRows * a.L && tiles < 65536) {
+      const unsigned cols = GATED ? kFewCols / 2 : kFewCols;
+      hipLaunchKernelGGL((product_few<T, GATED>), dim3((a.N + cols - 1) / cols, (unsigned)tiles), dim3(256), 0, s, a);
+      if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
+      return VP_OK;
+    }
+  }
   return launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
 }
 
