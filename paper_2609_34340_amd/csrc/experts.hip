@@ -431,7 +431,10 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   };
 
   constexpr int kLoadsA = decltype(oa)::kLoads, kLoadsB = decltype(ob)::kLoads;
-  static_assert(NT + 4 == MT && kLoadsA == 4 && kLoadsB == 4, "the loads' places among the rows of products");
+  // where the loads go among the rows of products: the columns' before the
+  // middle of the step if there are rows enough, else all after it
+  constexpr bool kEarly = MT == NT + 4;
+  static_assert((kEarly || MT == 4) && kLoadsA == 4 && kLoadsB == 4, "the loads' places among the rows of products");
   const auto issue_a = [&](int pos, int j) { oa.issue(lds[pos & 1], wave, j); };
   const auto issue_b = [&](int pos, int j) { ob.issue(lds[pos & 1] + BM * kStep, wave, j); };
   const auto load = [&](int pos) {
@@ -557,14 +560,14 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if (i < NT) fb1[i] = read_b(pos, 1, i);
-      if (i == NT + 1) {
+      if (kEarly && i == NT + 1) {
         issue_b(pos + 2, 0);
         issue_b(pos + 2, 1);
-      } else if (i > NT + 1) {
+      } else if (kEarly && i > NT + 1) {
         issue_b(pos + 2, i - NT);
       }
       multiply(kFirst, i, fa[i], fb0, sa[i], sb);
-      if (i == NT) {   // every wavefront has read the step's columns
+      if (kEarly && i == NT) {   // every wavefront has read the step's columns
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -574,8 +577,8 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     multiply(kSecond, 0, fa[0], fb1, sa[0], sb);
     // the next step has arrived (the stores of the tile before may be on
     // their way), and no wavefront reads this step's half any more
-    if (stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kStores + kLoadsB) : "memory");
-    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoadsB) : "memory");
+    if (stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kStores + (kEarly ? kLoadsB : 0)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kEarly ? kLoadsB : 0) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const bool end = step + 1 == steps;
@@ -585,13 +588,29 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     int sb1[NT] = {};
     fa[0] = read_a(pos + 1, 0, 0);
     sa[0] = read_power(group, next_step, wm * MT * 16);
+    if (!kEarly) {
+      issue_b(pos + 2, 0);
+      issue_b(pos + 2, 1);
+    }
 #pragma unroll
     for (int i = 1; i < MT; ++i) {
-      if (i % 2) issue_a(pos + 2, i / 2);
-      if (i <= NT) {
-        fb0[i - 1] = read_b(pos + 1, 0, i - 1);
-        sb1[i - 1] = read_power(group, next_step, BM + (wn * NT + i - 1) * 16);
+      if (kEarly) {
+        if (i % 2) issue_a(pos + 2, i / 2);
+      } else {
+        if (i == 1) {
+          issue_b(pos + 2, 2);
+          issue_b(pos + 2, 3);
+        } else {
+          issue_a(pos + 2, 2 * i - 4);
+          issue_a(pos + 2, 2 * i - 3);
+        }
       }
+      const auto column = [&](int j) {
+        fb0[j] = read_b(pos + 1, 0, j);
+        sb1[j] = read_power(group, next_step, BM + (wn * NT + j) * 16);
+      };
+      if (i <= NT) column(i - 1);
+      if (!kEarly && i == MT - 1) column(NT - 1);
       multiply(kSecond, i, fa[i], fb1, sa[i], sb);
       fa[i] = read_a(pos + 1, 0, i);
       sa[i] = read_power(group, next_step, (wm * MT + i) * 16);
@@ -658,8 +677,8 @@ __device__ inline void few_rows(const ProductArgs& a, const Group& g, int64_t m0
     for (int c = 0; c < 4; ++c) {
       const int byte = at + c * 64 + q * 16;
       const uint32_t off = byte < code_bytes ? (uint32_t)byte : 0x60000000u;   // past the row: zero
-      p.w[0][c] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 2);   // not to be kept in caches
-      p.w[1][c] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 2);
+      p.w[0][c] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 0);
+      p.w[1][c] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 0);
 #pragma unroll
       for (int i = 0; i < MT; ++i) p.x[i][c] = __builtin_amdgcn_raw_buffer_load_b128(rx, off + (i * 16 + r) * sx, 0, 0);
     }
@@ -810,22 +829,49 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
   constexpr int BM = WM * MT * 16, kTileN = WN * NT * 16 / (GATED ? 2 : 1);
   const int64_t nt = (a.N + kTileN - 1) / kTileN;
   int64_t per = MODE == kGradW ? (((a.M + BM - 1) / BM) * nt + 7) / 8 * a.L : ((a.R / BM + a.L) * nt + 7) / 8;
-  if (MODE != kGradW) per = std::min<int64_t>(per, kCus / 8);
+  if (MODE != kGradW) per = std::min<int64_t>(per, kCus / 8 * (BM == 128 ? 2 : 1));
   if (per * 8 >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
   hipLaunchKernelGGL((product_tiled<T, MODE, GATED, WM, WN, MT, NT>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
   return VP_OK;
 }
 
+// Which kernel, from the sizes the host knows (R rows at most, spread over L
+// experts).  Few rows: the weights are read again for every 64 rows, at about
+// 3 TB/s (2.5 in 4-bit blocks); tiles take 1.1 us a step of the contraction
+// and 6 us around it for each round of workgroups, and read all weights at
+// 4.5 TB/s or less.  Measured, few rows against tiles, us: 64 rows at 4 experts
+// of 4096 x 4096 35 / 76, 256 at 4 50 / 76, 256 at 1 48 / 77, 512 at 1 91 / 79,
+// 768 at 8 of 2048 x 2048 52 / 45; in 4-bit blocks 256 at 1 19 / 27, 512 at 1
+// 34 / 28.
+template <typename T> bool few_rows_win(const ProductArgs& a, int64_t weight_rows) {
+  constexpr bool kMx = Elem<T>::mx;
+  const int64_t tiles = a.R / kFewRows + a.L;
+  if (tiles >= 65536) return false;   // the grid's second dimension
+  const double expert = (double)weight_rows * (double)a.b_stride;   // bytes
+  const double few = ((double)a.R / kFewRows + 0.5 * a.L) * expert / (kMx ? 2500.0 : 3000.0);   // ns
+  const double rounds = std::max(1.0, ((double)a.R / 256 + 0.5 * a.L) * ((double)weight_rows / 256) / kCus);
+  const double steps = (double)a.C / (kMx ? 256 : 64);
+  return few < std::max((6000.0 + 1100.0 * steps) * rounds, a.L * expert / 4500.0);
+}
+
+// 128 x 128 tiles where they are at most one and a half for each CU, else 256
+// x 256.  Measured, 128 against 256, us: 2048 rows, one expert, 2048 x 2048 43 /
+// 48, 2048 rows at 8 of them 46 / 48, 4096 rows at 8 54 / 52, 32768 rows, 4096
+// x 4096 1605 / 851.  Grad w has 256 x 256 always: 1024 rows at 8 of 2048 x 2048
+// 41 / 35.
 template <typename T, int MODE, bool GATED> vp_status launch_product_as(const ProductArgs& a, hipStream_t s) {
+  const int64_t columns = GATED ? 2 * (int64_t)a.N : a.N;
   if constexpr (MODE == kForward) {
-    const int64_t tiles = a.R / kFewRows + a.L;
-    if (a.R <= (int64_t)kFewRows * a.L && tiles < 65536) {
+    if (few_rows_win<T>(a, columns)) {
       const unsigned cols = GATED ? kFewCols / 2 : kFewCols;
-      hipLaunchKernelGGL((product_few<T, GATED>), dim3((a.N + cols - 1) / cols, (unsigned)tiles), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((product_few<T, GATED>), dim3((a.N + cols - 1) / cols, (unsigned)(a.R / kFewRows + a.L)), dim3(256), 0, s, a);
       if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
       return VP_OK;
     }
+  }
+  if constexpr (MODE != kGradW) {
+    if ((a.R / 128 + a.L / 2 + 1) * ((columns + 127) / 128) <= kCus * 3 / 2) return launch_tiled<T, MODE, GATED, 2, 2, 4, 4>(a, s);
   }
   return launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
 }

@@ -235,6 +235,9 @@ PRODUCTS = [
     ([300, 7, 257], 272, 128),
     ([5] * 70, 64, 104),
     ([640], 528, 264),
+    ([2048, 0, 700, 1349], 2056, 72),     # rows and columns enough for the largest tiles
+    ([2048, 0, 700, 1349], 72, 2056),
+    ([1] * 100 + [700] + [0] * 99, 136, 136),
 ]
 
 
@@ -487,7 +490,7 @@ def test_mx_blocks_with_infinity_or_nan_are_nan(vp):
 
 
 MX_PRODUCTS = [([1], 8, 32), ([0, 3, 0], 16, 64), ([17, 16, 15], 136, 96), ([130, 1, 0, 64], 80, 544), ([300, 7, 257], 272, 1056),
-               ([5] * 70, 64, 128), ([640], 528, 288)]
+               ([5] * 70, 64, 128), ([640], 528, 288), ([2048, 0, 700, 1349], 2056, 1312), ([1] * 100 + [700] + [0] * 99, 136, 160)]
 
 
 @pytest.mark.parametrize("counts,N,K", MX_PRODUCTS, ids=lambda v: str(v) if not isinstance(v, list) else "e%dr%d" % (len(v), sum(v)))
