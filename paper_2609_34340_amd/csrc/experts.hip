@@ -121,6 +121,25 @@ template <int BM> struct RowTiles {
   }
 };
 
+// The expert with the n-th most rows (ties: the lower index first), of at most
+// 64; of more, the n-th.
+__device__ inline int nth_largest(const ProductArgs& a, int n, int lane) {
+  if (a.L > 64) return n;
+  Group g{lane, 0, 0};
+  if (lane < a.L) {
+    g.lo = a.offsets[lane];
+    g.hi = a.offsets[lane + 1];
+    clamp(a, g);
+  }
+  const int rows = (int)(g.hi - g.lo);
+  int before = 0;
+  for (int e = 0; e < a.L; ++e) {
+    const int other = __builtin_amdgcn_readlane(rows, e);
+    before += other > rows || (other == rows && e < lane);
+  }
+  return __builtin_ctzll(__ballot(lane < a.L && before == n));
+}
+
 // Offsets that decrease or pass the buffer are the caller's error; products
 // stay inside the buffers all the same.
 __device__ inline void check_offsets(const ProductArgs& a) {
@@ -278,7 +297,8 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     Group g;
     int64_t m0;
     if (MODE == kGradW) {
-      g = group_of(a, (int)(idx / per));
+      // the longest contractions first: the tiles are handed out as workgroups end
+      g = group_of(a, nth_largest(a, (int)(idx / per), lane));
       m0 = slot * BM;
       t.rows = (int)min((int64_t)BM, a.M - m0);
     } else {
@@ -839,7 +859,7 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
 // Which kernel, from the sizes the host knows (R rows at most, spread over L
 // experts).  Few rows: the weights are read again for every 64 rows, at about
 // 3 TB/s (2.5 in 4-bit blocks); tiles take 1.1 us a step of the contraction
-// and 6 us around it for each round of workgroups, and read all weights at
+// (1.5) and 6 us around it for each round of workgroups, and read all weights at
 // 4.5 TB/s or less.  Measured, few rows against tiles, us: 64 rows at 4 experts
 // of 4096 x 4096 35 / 76, 256 at 4 50 / 76, 256 at 1 48 / 77, 512 at 1 91 / 79,
 // 768 at 8 of 2048 x 2048 52 / 45; in 4-bit blocks 256 at 1 19 / 27, 512 at 1
@@ -852,7 +872,7 @@ template <typename T> bool few_rows_win(const ProductArgs& a, int64_t weight_row
   const double few = ((double)a.R / kFewRows + 0.5 * a.L) * expert / (kMx ? 2500.0 : 3000.0);   // ns
   const double rounds = std::max(1.0, ((double)a.R / 256 + 0.5 * a.L) * ((double)weight_rows / 256) / kCus);
   const double steps = (double)a.C / (kMx ? 256 : 64);
-  return few < std::max((6000.0 + 1100.0 * steps) * rounds, a.L * expert / 4500.0);
+  return few < std::max((6000.0 + (kMx ? 1500.0 : 1100.0) * steps) * rounds, a.L * expert / 4500.0);
 }
 
 // 128 x 128 tiles where they are at most one and a half for each CU, else 256

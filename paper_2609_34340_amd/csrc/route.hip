@@ -12,10 +12,16 @@
 // 16-bit logits: 8.4 MB, 1.6 us), so the work is the choice itself: k rounds
 // of a maximum over E.  LPT lanes share a token, V keys each in registers: a
 // round is V/2 three-way maxima, log2(LPT) cross-lane steps for the value, the
-// same for the lowest index that has it, and V steps that strike it out.
-// Sixteen lanes per token (four tokens side by side in a wavefront) up to 256
-// experts, a whole wavefront above: fewer lanes take fewer cross-lane steps
-// and share each instruction among more tokens.
+// same for the lowest index that has it, and V steps that strike it out.  The
+// cross-lane steps stay in the vector unit (inside rows of 16 lanes by data
+// movement in the operand, across them by row swaps): through LDS permutes
+// 16,384 tokens of 256 take 13.7 us, this way 13.2, and 96 tokens 14 and 8 (sigmoid,
+// bias, eight groups).
+//
+// Sixteen lanes per token (four tokens side by side in a wavefront) where there
+// are tokens to fill the CUs: fewer lanes take fewer cross-lane steps and share
+// each instruction among more tokens.  A whole wavefront for few tokens, whose
+// call is one token's latency, and above 256 experts.
 //
 // Keys are unsigned integers in the order of the floats, so that a struck-out
 // key (0), one that may not be chosen (1) and every number are comparable.
@@ -37,9 +43,25 @@ __device__ inline uint32_t ordered(float x) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
+// f over the LPT lanes of a token, in every one of them.
+template <int CTRL, typename T> __device__ inline T moved(T v) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
 template <int LPT, typename T, typename F> __device__ inline T across(T v, F f) {
-#pragma unroll
-  for (int d = 1; d < LPT; d <<= 1) v = f(v, __shfl_xor(v, d, LPT));
+#ifdef __HIP_DEVICE_COMPILE__
+  v = f(v, moved<0xB1>(v));    // within pairs
+  v = f(v, moved<0x4E>(v));    // fours
+  v = f(v, moved<0x141>(v));   // eights: each half row mirrored
+  v = f(v, moved<0x140>(v));   // rows of 16, mirrored
+  if constexpr (LPT == 64) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);   // even rows, odd rows
+    v = f(__builtin_bit_cast(T, (unsigned)a[0]), __builtin_bit_cast(T, (unsigned)a[1]));
+    const unsigned w = __builtin_bit_cast(unsigned, v);
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);   // halves
+    v = f(__builtin_bit_cast(T, (unsigned)b[0]), __builtin_bit_cast(T, (unsigned)b[1]));
+  }
+#endif
   return v;
 }
 
@@ -149,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteArgs a) {
     best = across<LPT>(best, [](uint32_t p, uint32_t q) { return max(p, q); });
     uint32_t at = ~0u;
 #pragma unroll
-    for (int v = V - 1; v >= 0; --v) at = key[v] == best ? (uint32_t)expert_of<LPT>(v, sub) : at;
+    for (int v = 0; v < V; ++v) at = min(at, key[v] == best ? (uint32_t)expert_of<LPT>(v, sub) : ~0u);
     at = across<LPT>(at, [](uint32_t p, uint32_t q) { return min(p, q); });
 #pragma unroll
     for (int v = 0; v < V; ++v) key[v] = (uint32_t)expert_of<LPT>(v, sub) == at ? kTaken : key[v];
@@ -286,7 +308,12 @@ template <typename T> void launch_route_as(const RouteArgs& a, hipStream_t s) {
     const size_t lds = 4 * (size_t)tok * (a.k + 1 + (a.n_groups > 1 ? a.E + 1 + 2 * a.n_groups : 0));
     hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + tok - 1) / tok)), dim3(threads), lds, s, a);
   };
-  if (a.E <= 64) go(route_kernel<T, 16, 4>, 16, kThreads);
+  // a wavefront per token against sixteen lanes, us: 96 tokens of 256 experts
+  // 5.2 / 7.7, 4096 7.5 / 8.2, 8192 11.3 / 9.3; of 128 experts 2048 5.3 / 5.3, 4096 7.2 / 5.4
+  const bool few = a.T <= (a.E <= 128 ? 2048 : 4096);
+  if (few && a.E <= 64) go(route_kernel<T, 64, 1>, 64, kThreads);
+  else if (few && a.E <= 256) go(route_kernel<T, 64, 4>, 64, kThreads);
+  else if (a.E <= 64) go(route_kernel<T, 16, 4>, 16, kThreads);
   else if (a.E <= 128) go(route_kernel<T, 16, 8>, 16, kThreads);
   else if (a.E <= 256) go(route_kernel<T, 16, 16>, 16, kThreads);
   else if (a.E <= 1024) go(route_kernel<T, 64, 16>, 64, kThreads);

@@ -10,6 +10,7 @@ by default) and returns; outputs may be given to reuse buffers.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Optional
 
 import torch
@@ -46,47 +47,58 @@ def declare(L) -> None:
     L.vp_expert_matmul_mx.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, vp, i32, i64, vp, vp]
 
 
+# The checks are written for their cost: a small call is bound by the host (a decode step's merge 10 us a pass, of which
+# the kernel takes 4), and every tensor attribute is a call.
+
 def _matrix(t: torch.Tensor, name: str, cols: Optional[int] = None, dtype=None, rows: Optional[int] = None) -> int:
     """Checks a [rows, cols] GPU matrix whose elements are neighbours; its row stride in elements."""
-    if not t.is_cuda or t.dim() != 2 or t.dtype not in _DTYPES and t.dtype != torch.uint8:
-        raise ValueError("%s must be a floating or byte matrix on the GPU" % name)
+    shape = t.shape
+    if not t.is_cuda or len(shape) != 2:
+        raise ValueError("%s must be a matrix on the GPU" % name)
+    n, m = shape
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s must be %s" % (name, dtype))
-    if (cols is not None and t.shape[1] != cols) or (rows is not None and t.shape[0] != rows):
-        raise ValueError("%s must be [%s, %s], is %s" % (name, rows if rows is not None else "rows", cols, tuple(t.shape)))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if (cols is not None and m != cols) or (rows is not None and n != rows):
+        raise ValueError("%s must be [%s, %s], is %s" % (name, "rows" if rows is None else rows,
+                                                         "columns" if cols is None else cols, tuple(shape)))
+    ld, one = t.stride()
+    if one != 1 and m > 1:
         raise ValueError("%s must have neighbouring elements in a row" % name)
-    if t.shape[0] <= 1:
-        return t.shape[1]
-    if t.stride(0) < t.shape[1]:
+    if n <= 1:
+        return m
+    if ld < m:
         raise ValueError("%s has overlapping rows" % name)
-    return t.stride(0)
+    return ld
 
 
 def _whole(t: torch.Tensor, dtype, shape, name: str) -> torch.Tensor:
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor %s on the GPU" % (name, dtype, tuple(shape)))
     return t
 
 
 def _float_dtype(t: torch.Tensor, name: str, halves: bool = False) -> int:
-    if t.dtype not in _DTYPES or (halves and t.dtype == torch.float32):
+    code = _DTYPES.get(t.dtype)
+    if code is None or (halves and code == 0):
         raise ValueError("%s must be bf16%s" % (name, " or fp16" if halves else ", fp16 or fp32"))
-    return _DTYPES[t.dtype]
+    return code
 
 
 def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
-    if any(t is not None and t.device != first.device for t in others):
-        raise ValueError("all tensors must be on one device")
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on one device")
 
 
 # --------------------------------------------------------------- routing
 
-def _route_params(score, k, n_groups, top_groups, group_top, renorm, scale) -> RouteParams:
+@functools.lru_cache(maxsize=64)
+def _route_params(score, k, n_groups, top_groups, group_top, renorm, scale):
     if score not in SCORES:
         raise ValueError("score must be one of %s" % sorted(SCORES))
-    return RouteParams(SCORES[score], k, n_groups, n_groups if top_groups is None else top_groups, group_top,
-                       int(bool(renorm)), scale)
+    return C.byref(RouteParams(SCORES[score], k, n_groups, n_groups if top_groups is None else top_groups, group_top,
+                               int(bool(renorm)), scale))
 
 
 def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optional[torch.Tensor] = None,
@@ -106,7 +118,7 @@ def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optiona
     weights = _whole(out["weights"], torch.float32, (T, k), "weights")
     _same_device(logits, bias, ids, weights)
     p = _route_params(score, k, n_groups, top_groups, group_top, renorm, scale)
-    _check(lib().vp_route(_ptr(logits), dt, T, E, ld, C.byref(p), _ptr(bias), _ptr(ids), _ptr(weights),
+    _check(lib().vp_route(_ptr(logits), dt, T, E, ld, p, _ptr(bias), _ptr(ids), _ptr(weights),
                           _stream(stream)), "vp_route")
     return out
 
@@ -131,7 +143,7 @@ def route_grad(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, d
         status = new_status(logits.device)
     _same_device(logits, ids, weights, d_weights, out, status)
     p = _route_params(score, k, 1, 1, 1, renorm, scale)
-    _check(lib().vp_route_grad(_ptr(logits), dt, T, E, ld, C.byref(p), _ptr(ids), _ptr(weights), _ptr(d_weights),
+    _check(lib().vp_route_grad(_ptr(logits), dt, T, E, ld, p, _ptr(ids), _ptr(weights), _ptr(d_weights),
                                _ptr(out), _ptr(status), _stream(stream)), "vp_route_grad")
     return out
 
