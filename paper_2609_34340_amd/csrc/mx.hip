@@ -25,16 +25,18 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPer = 8;   // values of a thread
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-// The 4-bit code of a magnitude below 8: the count of rounding boundaries at
-// or below it; a tie belongs to the even code, so every second boundary is
-// passed only by larger values.
-__device__ inline uint32_t code_of(float v) {
-  const float m = fabsf(v);
-  const uint32_t c = (uint32_t)(m > 0.25f) + (m >= 0.75f) + (m > 1.25f) + (m >= 1.75f) + (m > 2.5f) + (m >= 3.5f) +
-                     (m > 5.0f);
-  return c | (__float_as_uint(v) >> 31) << 3;
+// The codes of eight values below 8, by the conversion instruction (nearest,
+// ties to the even code, ends at 6; low four bits first).
+__device__ inline uint32_t codes_of(const float* f) {
+#ifdef __HIP_DEVICE_COMPILE__
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[0], f[1], 1.0f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[2], f[3], 1.0f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[4], f[5], 1.0f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[6], f[7], 1.0f, 3);
+#else
+  return 0;
+#endif
 }
 
 __device__ inline float value_of(uint32_t code) {
@@ -78,10 +80,9 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(MxArgs a) {
     top = max(top, __shfl_xor(top, 2));
     const int e = (int)(top >> 23);
     const int power = e == 255 ? 255 : max(e - 2, 0);   // the exponent byte
-    uint32_t codes = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) codes |= code_of(ldexpf(f[i], 127 - power)) << (4 * i);
-    *(uint32_t*)(dst + (int64_t)c * 4) = power == 255 ? 0 : codes;
+    for (int i = 0; i < kPer; ++i) f[i] = ldexpf(f[i], 127 - power);
+    *(uint32_t*)(dst + (int64_t)c * 4) = power == 255 ? 0 : codes_of(f);
     if ((c & 3) == 0) dst[a.K / 2 + c / 4] = (unsigned char)power;
   }
   for (int i = a.K / 2 + a.K / 32 + sub; i < a.row_bytes; i += a.per_row) dst[i] = 0;
