@@ -155,7 +155,17 @@ template <typename T> struct Frag;
 template <> struct Frag<Bf16> { using type = bf16x8; using elem = __bf16; };
 template <> struct Frag<F16> { using type = f16x8; using elem = _Float16; };
 
-__device__ inline float silu(float g) { return g / (1.0f + expf(-g)); }
+// To a few units of the last place of 32 bits for |g| in the tens (the product
+// with log2 e is rounded), far inside the 16 bits that the result is rounded
+// to; the library's exponential and divide cost a gated tile 64 times 30
+// instructions a lane.
+__device__ inline float silu(float g) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504089f));
+#else
+  return g;
+#endif
+}
 
 // ---------------------------------------------------------------- tiled products
 
@@ -241,13 +251,16 @@ template <typename T> struct Mx { using out = T; };   // both operands in 4-bit 
 template <typename T> struct Elem { using out = T; static constexpr bool mx = false; };
 template <typename T> struct Elem<Mx<T>> { using out = T; static constexpr bool mx = true; };
 
-// Where a tile's operands begin and how much of them there is (see Operand),
-// and its results.
-struct TileAt {
-  const unsigned char *a, *b;
-  int a_left, a_width, b_left, b_width, steps;
+// A tile's results: where they go, its rows and columns inside the output, and
+// the steps of its contraction.
+struct TileOut {
   unsigned char *out, *pre;
-  int rows, cols;   // of the tile, inside the output
+  int rows, cols, steps;
+};
+// And where its operands begin and how much of them there is (see Operand).
+struct TileAt : TileOut {
+  const unsigned char *a, *b;
+  int a_left, a_width, b_left, b_width;
 };
 
 // WM x WN wavefronts, each with MT x NT fragments of 16 x 16 results.  A
@@ -285,15 +298,15 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     row_tiles.init(a, lane);
     slots = row_tiles.total;
   }
-  const int64_t per = (slots * nt + 7) / 8;   // this XCD's tiles
-  const int64_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW ? per * a.L : per;
-  const auto tile_at = [&](int64_t idx, TileAt& t) -> bool {
-    const int64_t in_xcd = MODE == kGradW ? idx % per : idx, at = (blockIdx.x & 7) * per + in_xcd;
-    if (at >= slots * nt) return false;
-    const int64_t band = at / (kBand * nt);
-    const int in = (int)(at - band * (kBand * nt)), high = (int)min((int64_t)kBand, slots - band * kBand);
+  const uint32_t all = (uint32_t)(slots * nt), per = (all + 7) / 8;   // tiles, below 2^31; this XCD's
+  const uint32_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW ? per * a.L : per;
+  const auto tile_at = [&](uint32_t idx, TileAt& t) -> bool {
+    const uint32_t in_xcd = MODE == kGradW ? idx % per : idx, at = (blockIdx.x & 7) * per + in_xcd;
+    if (at >= all) return false;
+    const uint32_t band = at / (uint32_t)(kBand * nt), in = at - band * (kBand * nt);
+    const uint32_t high = min((uint32_t)kBand, (uint32_t)slots - band * kBand);
     const int64_t slot = band * kBand + in % high;
-    const int n0 = in / high * kTileN;
+    const int n0 = (int)(in / high) * kTileN;
     Group g;
     int64_t m0;
     if (MODE == kGradW) {
@@ -312,7 +325,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
       t.a_left = t.b_left = rows;
       t.a_width = (int)(a.M - m0) * 2;
       t.b_width = (a.N - n0) * 2;
-      t.steps = max((rows + 63) / 64, 1);   // an expert without rows: zeros
+      t.steps = (rows + 63) / 64;   // an expert without rows: zeros
     } else {
       t.a = a.a + m0 * a.a_stride;
       t.a_left = (t.rows - 1) * (int)a.a_stride + row_bytes;
@@ -330,12 +343,13 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
         t.b_width = row_bytes;
       }
     }
+    t.steps = max(t.steps, 2);   // steps past the last add zeros
     t.cols = min(kTileN, a.N - n0);
     t.out = a.out + (MODE == kGradW ? g.e * a.b_expert : 0) + m0 * a.out_stride + (int64_t)n0 * kSize;
     t.pre = GATED && a.pre ? a.pre + m0 * a.pre_stride + (int64_t)n0 * 2 : nullptr;
     return true;
   };
-  const auto find = [&](int64_t& idx, TileAt& t) {   // the first tile at or after idx
+  const auto find = [&](uint32_t& idx, TileAt& t) {   // the first tile at or after idx
     for (; idx < last; idx += stride)
       if (tile_at(idx, t)) return true;
     return false;
@@ -345,10 +359,11 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   Operand<BM, kColsA, kWaves> oa;
   Operand<BN, kColsB, kWaves> ob;
   TileAt ahead;
-  int64_t load_idx = first;
+  uint32_t load_idx = first;
   int load_step = 0, load_group = 0;
   if (!find(load_idx, ahead)) return;
-  int64_t idx = load_idx;
+  TileOut cur = ahead, next = ahead, after = ahead;   // of the multiplied tile and those begun since
+  int begun = 0;   // how many of these: a tile has two steps at least, so at most two
   const auto begin = [&] {
     oa.start(ahead.a, ahead.a_left, ahead.a_width, lane);
     ob.start(ahead.b, ahead.b_left, ahead.b_width, lane);
@@ -368,6 +383,8 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     load_step = 0;
     if (find(load_idx, ahead)) {
       begin();
+      (begun == 0 ? next : after) = ahead;
+      ++begun;
     } else {   // nothing is left: the loads bring zeros that nothing multiplies
       ahead.steps = 0x7fffffff;
       oa.start(ahead.a, 0, 0, lane);
@@ -528,7 +545,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
       }
     }
   };
-  const auto write = [&](const TileAt& t) {
+  const auto write = [&](const TileOut& t) {
     if constexpr (GATED) {
       // a wavefront's columns: of every four fragments two of the gate, then the same two of the up half
       const auto gate = [&](int i, int j) { return acc[i][j / 2 * 4 + j % 2]; };
@@ -561,7 +578,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   constexpr std::integral_constant<int, 1> kSecond{};
   i32x4 fa[MT], fb0[NT], fb1[NT];
   int sa[MT] = {}, sb[NT] = {};
-  int steps = ahead.steps, step = 0, group = 0;
+  int step = 0, group = 0;
   load(0);
   load(1);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -601,7 +618,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kEarly ? kLoadsB : 0) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const bool end = step + 1 == steps;
+    const bool end = step + 1 == cur.steps;
     const int next_step = end ? 0 : step + 1;
     if (next_step % 4 == 0) ++group;
     load_powers();
@@ -641,13 +658,12 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     stored = false;
     ++step;
     if (end) {
-      TileAt t;
-      tile_at(idx, t);
-      write(t);
-      stored = !t.pre;
-      idx += stride;
-      if (!find(idx, t)) break;
-      steps = t.steps;
+      write(cur);
+      stored = !cur.pre;
+      if (begun == 0) break;
+      cur = next;
+      next = after;
+      --begun;
       step = 0;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -849,8 +865,9 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
   constexpr int BM = WM * MT * 16, kTileN = WN * NT * 16 / (GATED ? 2 : 1);
   const int64_t nt = (a.N + kTileN - 1) / kTileN;
   int64_t per = MODE == kGradW ? (((a.M + BM - 1) / BM) * nt + 7) / 8 * a.L : ((a.R / BM + a.L) * nt + 7) / 8;
-  if (MODE != kGradW) per = std::min<int64_t>(per, kCus / 8 * (BM == 128 ? 2 : 1));
   if (per * 8 >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
+  if (MODE != kGradW) per = std::min<int64_t>(per, kCus / 8 * (BM == 128 ? 2 : 1));
+  
   hipLaunchKernelGGL((product_tiled<T, MODE, GATED, WM, WN, MT, NT>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
   return VP_OK;
