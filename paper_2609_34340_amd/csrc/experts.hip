@@ -487,7 +487,6 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   // One row of fragments: i of the rows' by all of the columns'.
   const auto multiply = [&](auto half_step, int i, const i32x4& fa, const i32x4 (&fb)[NT], int sa, const int (&sb)[NT]) {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       if constexpr (kMx) {
@@ -500,10 +499,9 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
         acc[i][j] = mma(__builtin_bit_cast(F, fb[j]), __builtin_bit_cast(F, fa), acc[i][j]);
       }
     }
-    // the compiler would move these pure instructions past the barriers, to where the sums are next used
+    // the compiler would move these pure instructions past the loads' branches, to where the sums are next used
 #pragma unroll
-    for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
-    __builtin_amdgcn_s_setprio(0);
+    for (int j = 0; j < (kMx ? NT : 0); ++j) asm volatile("" : "+v"(acc[i][j]));
     __builtin_amdgcn_sched_barrier(0);
   };
 
@@ -875,28 +873,29 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
 
 // Which kernel, from the sizes the host knows (R rows at most, spread over L
 // experts).  Few rows: the weights are read again for every 64 rows, at about
-// 3 TB/s (2.5 in 4-bit blocks); tiles take 1.1 us a step of the contraction
-// (1.5) and 6 us around it for each round of workgroups, and read all weights at
-// 4.5 TB/s or less.  Measured, few rows against tiles, us: 64 rows at 4 experts
-// of 4096 x 4096 35 / 76, 256 at 4 50 / 76, 256 at 1 48 / 77, 512 at 1 91 / 79,
-// 768 at 8 of 2048 x 2048 52 / 45; in 4-bit blocks 256 at 1 19 / 27, 512 at 1
-// 34 / 28.
+// 3.6 TB/s (2.5 in 4-bit blocks); tiles take 0.85 us a step of the contraction
+// (1.35) and 6 us around it for each round of workgroups, and read all weights
+// at 4.5 TB/s or less.  Measured, few rows against tiles, us: 64 rows at 4
+// experts of 4096 x 4096 35 / 60, 256 at 4 50 / 60, 256 at 1 48 / 60, 512 at 1
+// 91 / 62, 512 at 8 of 2048 x 2048 29 / 33, 768 at 8 52 / 35; in 4-bit blocks 256
+// at 1 of 4096 x 4096 19 / 27, 512 at 1 34 / 27.
 template <typename T> bool few_rows_win(const ProductArgs& a, int64_t weight_rows) {
   constexpr bool kMx = Elem<T>::mx;
   const int64_t tiles = a.R / kFewRows + a.L;
   if (tiles >= 65536) return false;   // the grid's second dimension
   const double expert = (double)weight_rows * (double)a.b_stride;   // bytes
-  const double few = ((double)a.R / kFewRows + 0.5 * a.L) * expert / (kMx ? 2500.0 : 3000.0);   // ns
+  const double few = ((double)a.R / kFewRows + 0.5 * a.L) * expert / (kMx ? 2500.0 : 3600.0);   // ns
   const double rounds = std::max(1.0, ((double)a.R / 256 + 0.5 * a.L) * ((double)weight_rows / 256) / kCus);
   const double steps = (double)a.C / (kMx ? 256 : 64);
-  return few < std::max((6000.0 + (kMx ? 1500.0 : 1100.0) * steps) * rounds, a.L * expert / 4500.0);
+  return few < std::max((6000.0 + (kMx ? 1350.0 : 850.0) * steps) * rounds, a.L * expert / 4500.0);
 }
 
-// 128 x 128 tiles where they are at most one and a half for each CU, else 256
-// x 256.  Measured, 128 against 256, us: 2048 rows, one expert, 2048 x 2048 43 /
-// 48, 2048 rows at 8 of them 46 / 48, 4096 rows at 8 54 / 52, 32768 rows, 4096
-// x 4096 1605 / 851.  Grad w has 256 x 256 always: 1024 rows at 8 of 2048 x 2048
-// 41 / 35.
+// 128 x 128 tiles where they are at most two and a half for each CU, else 256 x
+// 256.  Measured, 128 against 256, us: 2048 rows, one expert, 2048 x 2048 39 / 52,
+// 4096 rows at 8 of them 48 / 54, 2048 rows at 4 of 4096 x 4096 87 / 94, 8192 rows
+// at 8 of 2048 x 2048 93 / 67, 4096 rows, one of 4096 x 4096 185 / 119.  Grad w
+// where 256 x 256 leave half of the CUs without a tile: 2048 rows, one expert,
+// 2048 x 2048 42 / 59, 1024 rows at 8 of them (512 tiles) 40 / 36.
 template <typename T, int MODE, bool GATED> vp_status launch_product_as(const ProductArgs& a, hipStream_t s) {
   const int64_t columns = GATED ? 2 * (int64_t)a.N : a.N;
   if constexpr (MODE == kForward) {
@@ -907,10 +906,9 @@ template <typename T, int MODE, bool GATED> vp_status launch_product_as(const Pr
       return VP_OK;
     }
   }
-  if constexpr (MODE != kGradW) {
-    if ((a.R / 128 + a.L / 2 + 1) * ((columns + 127) / 128) <= kCus * 3 / 2) return launch_tiled<T, MODE, GATED, 2, 2, 4, 4>(a, s);
-  }
-  return launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
+  const bool small = MODE == kGradW ? (int64_t)a.L * ((a.M + 255) / 256) * ((a.N + 255) / 256) <= kCus / 2
+                                    : (a.R / 128 + a.L / 2 + 1) * ((columns + 127) / 128) <= kCus * 5 / 2;
+  return small ? launch_tiled<T, MODE, GATED, 2, 2, 4, 4>(a, s) : launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
 }
 
 }  // namespace

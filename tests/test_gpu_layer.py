@@ -237,6 +237,7 @@ PRODUCTS = [
     ([640], 528, 264),
     ([2048, 0, 700, 1349], 2056, 72),     # rows and columns enough for the largest tiles
     ([2048, 0, 700, 1349], 72, 2056),
+    ([100, 0, 65, 1], 1032, 2312),        # grad w: more than half as many tiles as CUs
     ([1] * 100 + [700] + [0] * 99, 136, 136),
 ]
 
