@@ -506,7 +506,8 @@ vp_status vp_unpack_combine(const void* recv, int64_t recv_capacity, int64_t row
 /* ------------------------------------------------- layer: routing, experts
  *
  * What stands before, between and after the two exchanges of a
- * mixture-of-experts layer.  Element types: */
+ * mixture-of-experts layer.  In these calls dev_status may be NULL: device
+ * errors then stay unreported.  Element types: */
 typedef enum { VP_F32 = 0, VP_BF16 = 1, VP_F16 = 2 } vp_dtype;
 
 enum { VP_SCORE_SOFTMAX = 0, VP_SCORE_SIGMOID = 1 };

@@ -38,11 +38,10 @@ vp_status check_route(int32_t dtype, int64_t T, int32_t E, int64_t stride, const
   return VP_OK;
 }
 
-vp_status check_experts(int32_t dtype, const int64_t* offsets, int64_t R, int32_t L, int32_t N, int32_t K,
-                        const int32_t* dev_status) {
+vp_status check_experts(int32_t dtype, const int64_t* offsets, int64_t R, int32_t L, int32_t N, int32_t K) {
   if (!is_half(dtype)) return set_error(VP_ERR_INVALID_ARGUMENT, "the experts' rows are bf16 or fp16");
   if (R < 0 || L < 1 || N < 1 || K < 1) return set_error(VP_ERR_INVALID_ARGUMENT, "bad product sizes");
-  if (!offsets || !dev_status) return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
+  if (!offsets) return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
   if (N % 8 != 0 || K % 8 != 0) return set_error(VP_ERR_UNSUPPORTED, "N and K must be multiples of 8");
   if (R >= kMaxRows || L > kMaxExperts || N > kMaxWidth || K > kMaxWidth)
     return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 rows, 4096 experts or 2^20 columns");
@@ -85,7 +84,7 @@ vp_status vp_route_grad(const void* logits, int32_t dtype, int64_t T, int32_t E,
                         void* d_logits, int32_t* dev_status, void* stream) {
   vp_status st = check_route(dtype, T, E, logits_stride, p);
   if (st != VP_OK) return st;
-  if (!dev_status || (T > 0 && (!logits || !ids || !weights || !d_weights || !d_logits)))
+  if (T > 0 && (!logits || !ids || !weights || !d_weights || !d_logits))
     return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
   if (T == 0) return VP_OK;
   return vp::launch_route_grad(logits, dtype, T, E, logits_stride, *p, ids, weights, d_weights, d_logits, dev_status,
@@ -97,14 +96,14 @@ vp_status vp_expert_offsets(const int32_t* counts, int32_t n_ranks, int32_t E, i
   if (n_ranks < 1 || n_ranks > vp::kMaxRanks || E < 1 || E % n_ranks != 0 || E > kMaxExperts || self_rank < 0 ||
       self_rank >= n_ranks)
     return set_error(VP_ERR_INVALID_ARGUMENT, "bad offsets sizes (E a multiple of N, <= 4096)");
-  if (!counts || !offsets || !dev_status) return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
+  if (!counts || !offsets) return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
   return vp::launch_expert_offsets(counts, n_ranks, E, self_rank, offsets, dev_status, stream);
 }
 
 vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const void* w, const int64_t* offsets,
                            int64_t R, int32_t L, int32_t N, int32_t K, int32_t gated, void* y, int64_t y_stride,
                            void* pre, int64_t pre_stride, int32_t* dev_status, void* stream) {
-  vp_status st = check_experts(dtype, offsets, R, L, N, K, dev_status);
+  vp_status st = check_experts(dtype, offsets, R, L, N, K);
   if (st != VP_OK) return st;
   if ((st = check_gated(gated, N, (int64_t)K * 2)) != VP_OK) return st;
   if (!gated && pre) return set_error(VP_ERR_INVALID_ARGUMENT, "pre belongs to a gated product");
@@ -121,7 +120,7 @@ vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const
 vp_status vp_expert_matmul_grad_x(const void* dy, int64_t dy_stride, int32_t dtype, const void* w,
                                   const int64_t* offsets, int64_t R, int32_t L, int32_t N, int32_t K, void* dx,
                                   int64_t dx_stride, int32_t* dev_status, void* stream) {
-  vp_status st = check_experts(dtype, offsets, R, L, N, K, dev_status);
+  vp_status st = check_experts(dtype, offsets, R, L, N, K);
   if (st != VP_OK) return st;
   if ((st = check_rows(dy, (int64_t)N * 2, dy_stride, R, "dy")) != VP_OK) return st;
   if ((st = check_rows(w, (int64_t)K * 2, (int64_t)K * 2, 1, "w")) != VP_OK) return st;
@@ -135,7 +134,7 @@ vp_status vp_expert_matmul_grad_x(const void* dy, int64_t dy_stride, int32_t dty
 vp_status vp_expert_matmul_grad_w(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int32_t dtype,
                                   const int64_t* offsets, int64_t R, int32_t L, int32_t N, int32_t K, float* dw,
                                   int32_t* dev_status, void* stream) {
-  vp_status st = check_experts(dtype, offsets, R, L, N, K, dev_status);
+  vp_status st = check_experts(dtype, offsets, R, L, N, K);
   if (st != VP_OK) return st;
   if ((st = check_rows(dy, (int64_t)N * 2, dy_stride, R, "dy")) != VP_OK) return st;
   if ((st = check_rows(x, (int64_t)K * 2, x_stride, R, "x")) != VP_OK) return st;
@@ -148,7 +147,7 @@ vp_status vp_expert_matmul_grad_w(const void* dy, int64_t dy_stride, const void*
 vp_status vp_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride, int32_t dtype,
                               const int64_t* offsets, int64_t R, int32_t L, int32_t I, void* dpre,
                               int64_t dpre_stride, int32_t* dev_status, void* stream) {
-  vp_status st = check_experts(dtype, offsets, R, L, I, 8, dev_status);
+  vp_status st = check_experts(dtype, offsets, R, L, I, 8);
   if (st != VP_OK) return st;
   if ((st = check_rows(dh, (int64_t)I * 2, dh_stride, R, "dh")) != VP_OK) return st;
   if ((st = check_rows(pre, (int64_t)I * 4, pre_stride, R, "pre")) != VP_OK) return st;
@@ -236,7 +235,7 @@ vp_status vp_mx_dequantize(const void* q, int64_t rows, int64_t K, int64_t q_str
 vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq, const int64_t* offsets, int64_t R,
                               int32_t L, int32_t N, int32_t K, int32_t gated, void* y, int32_t dtype,
                               int64_t y_stride, int32_t* dev_status, void* stream) {
-  vp_status st = check_experts(dtype, offsets, R, L, N, K, dev_status);
+  vp_status st = check_experts(dtype, offsets, R, L, N, K);
   if (st != VP_OK) return st;
   if (K % 32 != 0) return set_error(VP_ERR_UNSUPPORTED, "K must be a multiple of 32");
   const int64_t rb = vp::mx_row_bytes(K);

@@ -44,7 +44,10 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-__device__ inline void report(int32_t* status, int code) { atomicCAS(status, 0, code); }
+// A caller without a status does not learn of device errors.
+__device__ inline void report(int32_t* status, int code) {
+  if (status) atomicCAS(status, 0, code);
+}
 
 enum { kForward = 0, kGradX = 1, kGradW = 2 };
 
@@ -85,6 +88,7 @@ template <int BM> struct RowTiles {
   int run;         // experts of a lane
   int64_t first;   // this lane's first tile
   int64_t total;
+  bool in_order;   // false: more tiles than offsets in order can have
 
   __device__ static int64_t of(const Group& g) { return (g.hi - g.lo + BM - 1) / BM; }
   __device__ void init(const ProductArgs& a, int lane) {
@@ -105,6 +109,9 @@ template <int BM> struct RowTiles {
     total = __shfl(incl, 63);
     total = (int64_t)((uint64_t)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32 |
                       (uint32_t)__builtin_amdgcn_readfirstlane((int)total));
+    // others (an error, reported) get no work, instead of any amount
+    in_order = total <= a.R / BM + a.L;
+    if (!in_order) total = 0;
   }
   // The expert of tile `t` (below the total) and the first row of the tile.
   __device__ Group find(const ProductArgs& a, int64_t t, int64_t* m0) const {
@@ -293,10 +300,11 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   constexpr int kBand = 4;
   const int nt = (a.N + kTileN - 1) / kTileN, mt = MODE == kGradW ? (a.M + BM - 1) / BM : 0;
   RowTiles<BM> row_tiles;
-  int64_t slots = mt;   // row tiles
-  if (MODE != kGradW) {
-    row_tiles.init(a, lane);
-    slots = row_tiles.total;
+  row_tiles.init(a, lane);
+  int64_t slots = row_tiles.total;   // row tiles
+  if (MODE == kGradW) {
+    if (!row_tiles.in_order) return;
+    slots = mt;
   }
   const uint32_t all = (uint32_t)(slots * nt), per = (all + 7) / 8;   // tiles, below 2^31; this XCD's
   const uint32_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW ? per * a.L : per;

@@ -36,7 +36,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kTaken = 0, kMasked = 1;   // below the key of every number
 
-__device__ inline void report(int32_t* status, int code) { atomicCAS(status, 0, code); }
+// A caller without a status does not learn of device errors.
+__device__ inline void report(int32_t* status, int code) {
+  if (status) atomicCAS(status, 0, code);
+}
 
 __device__ inline uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);   // -0 counts as +0

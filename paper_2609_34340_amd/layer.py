@@ -5,7 +5,8 @@ these names too.
 
 Matrices may have strided rows (the receive slots' 128-byte stride), their
 elements must be neighbours.  Every call enqueues on `stream` (the current one
-by default) and returns; outputs may be given to reuse buffers.
+by default) and returns; outputs may be given to reuse buffers.  Errors that
+only the device can see go to `status` (new_status()) where one is given.
 """
 from __future__ import annotations
 
@@ -15,7 +16,7 @@ from typing import Optional
 
 import torch
 
-from . import _check, _ptr, _stream, lib, new_status
+from . import _check, _ptr, _stream, lib
 
 SCORES = {"softmax": 0, "sigmoid": 1}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -139,8 +140,6 @@ def route_grad(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, d
     if out is None:
         out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
     _whole(out, logits.dtype, (T, E), "d_logits")
-    if status is None:
-        status = new_status(logits.device)
     _same_device(logits, ids, weights, d_weights, out, status)
     p = _route_params(score, k, 1, 1, 1, renorm, scale)
     _check(lib().vp_route_grad(_ptr(logits), dt, T, E, ld, p, _ptr(ids), _ptr(weights), _ptr(d_weights),
@@ -161,8 +160,6 @@ def expert_offsets(counts: torch.Tensor, self_rank: int, out: Optional[torch.Ten
     if out is None:
         out = torch.empty(n_local + 1, dtype=torch.int64, device=counts.device)
     _whole(out, torch.int64, (n_local + 1,), "offsets")
-    if status is None:
-        status = new_status(counts.device)
     _same_device(counts, out, status)
     _check(lib().vp_expert_offsets(_ptr(counts), N, E, self_rank, _ptr(out), _ptr(status), _stream(stream)),
            "vp_expert_offsets")
@@ -195,8 +192,6 @@ def expert_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, ga
         out = torch.empty((R, width), dtype=x.dtype, device=x.device)
     ldy = _matrix(out, "out", cols=width, dtype=x.dtype, rows=R)
     ldp = 0 if pre is None else _matrix(pre, "pre", cols=N, dtype=x.dtype, rows=R)
-    if status is None:
-        status = new_status(x.device)
     _same_device(x, w, offsets, out, pre, status)
     _check(lib().vp_expert_matmul(_ptr(x), 2 * ldx, dt, _ptr(w), _ptr(offsets), R, L, N, K, int(gated), _ptr(out),
                                   2 * ldy, _ptr(pre), 2 * ldp, _ptr(status), _stream(stream)), "vp_expert_matmul")
@@ -215,8 +210,6 @@ def expert_matmul_grad_x(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tenso
     if out is None:
         out = torch.empty((R, K), dtype=dy.dtype, device=dy.device)
     ldx = _matrix(out, "out", cols=K, dtype=dy.dtype, rows=R)
-    if status is None:
-        status = new_status(dy.device)
     _same_device(dy, w, offsets, out, status)
     _check(lib().vp_expert_matmul_grad_x(_ptr(dy), 2 * ldy, dt, _ptr(w), _ptr(offsets), R, L, N, K, _ptr(out),
                                          2 * ldx, _ptr(status), _stream(stream)), "vp_expert_matmul_grad_x")
@@ -238,8 +231,6 @@ def expert_matmul_grad_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tenso
     if out is None:
         out = torch.empty((L, N, K), dtype=torch.float32, device=dy.device)
     _whole(out, torch.float32, (L, N, K), "out")
-    if status is None:
-        status = new_status(dy.device)
     _same_device(dy, x, offsets, out, status)
     _check(lib().vp_expert_matmul_grad_w(_ptr(dy), 2 * ldy, _ptr(x), 2 * ldx, dt, _ptr(offsets), R, L, N, K,
                                          _ptr(out), _ptr(status), _stream(stream)), "vp_expert_matmul_grad_w")
@@ -259,8 +250,6 @@ def expert_gate_grad(dh: torch.Tensor, pre: torch.Tensor, offsets: torch.Tensor,
     if out is None:
         out = torch.empty((R, 2 * half), dtype=dh.dtype, device=dh.device)
     ldo = _matrix(out, "out", cols=2 * half, dtype=dh.dtype, rows=R)
-    if status is None:
-        status = new_status(dh.device)
     _same_device(dh, pre, offsets, out, status)
     _check(lib().vp_expert_gate_grad(_ptr(dh), 2 * ldh, _ptr(pre), 2 * ldp, dt, _ptr(offsets), R, L, half, _ptr(out),
                                      2 * ldo, _ptr(status), _stream(stream)), "vp_expert_gate_grad")
@@ -371,8 +360,6 @@ def expert_matmul_mx(xq: torch.Tensor, wq: torch.Tensor, offsets: torch.Tensor, 
         out = torch.empty((R, width), dtype=dtype, device=xq.device)
     dt = _float_dtype(out, "out", halves=True)
     ldy = _matrix(out, "out", cols=width, rows=R)
-    if status is None:
-        status = new_status(xq.device)
     _same_device(xq, wq, offsets, out, status)
     _check(lib().vp_expert_matmul_mx(_ptr(xq), ldx, _ptr(wq), _ptr(offsets), R, L, N, K, int(gated), _ptr(out), dt,
                                      2 * ldy, _ptr(status), _stream(stream)), "vp_expert_matmul_mx")

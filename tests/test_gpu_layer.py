@@ -378,6 +378,34 @@ def test_expert_offsets_outside_the_buffer_are_reported(vp):
             assert vp.read_status(st) == vp.INVALID_ARGUMENT, bad
 
 
+def test_experts_without_rows_past_the_first_row(vp):
+    """Offsets need not begin at row 0; a weight gradient over no rows is zero."""
+    x, dy = normal((20, 64), 65, torch.bfloat16).cuda(), normal((20, 32), 66, torch.bfloat16).cuda()
+    w = normal((2, 32, 64), 67, torch.bfloat16).cuda()
+    st = vp.new_status()
+    for cuts in ([5, 5, 5], [3, 3, 17]):
+        off = torch.tensor(cuts).cuda()
+        dw = vp.expert_matmul_grad_w(dy, x, off, out=torch.full((2, 32, 64), 7.0).cuda(), status=st)
+        y = vp.expert_matmul(x, w, off, out=torch.full((20, 32), 7.0, dtype=torch.bfloat16).cuda(), status=st)
+        assert (dw[0] == 0).all() and (y[:cuts[1]] == 7.0).all() and (y[cuts[2]:] == 7.0).all()
+        p, q = dy[cuts[1]:cuts[2]].double().cpu(), x[cuts[1]:cuts[2]].double().cpu()
+        near(dw[1], p.t() @ q, 30 * 2.0 ** -24 * (p.abs().t() @ q.abs()), "dw")
+    assert vp.read_status(st) == 0
+
+
+def test_expert_offsets_that_overlap_end_soon(vp):
+    """Every second expert claims all rows: an error, and no more work than the rows' own."""
+    R, L, N, K = 4096, 64, 64, 64
+    x, w = normal((R, K), 63, torch.bfloat16).cuda(), normal((L, N, K), 64, torch.bfloat16).cuda()
+    off = torch.tensor([0, R] * (L // 2) + [0]).cuda()
+    xq, wq = vp.mx_quantize(x), vp.mx_quantize(w)
+    for call in (lambda st: vp.expert_matmul(x, w, off, status=st), lambda st: vp.expert_matmul_grad_x(x, w, off, status=st),
+                 lambda st: vp.expert_matmul_grad_w(x, x, off, status=st), lambda st: vp.expert_matmul_mx(xq, wq, off, K, status=st)):
+        st = vp.new_status()
+        call(st)
+        assert vp.read_status(st) == vp.INVALID_ARGUMENT
+
+
 # ------------------------------------------------------------------ merge
 
 MERGES = [(1, 1, 8), (1, 8, 2048), (3, 2, 264), (7, 9, 72), (5, 17, 4104), (2, 255, 64), (33, 8, 7168), (96, 8, 4096)]

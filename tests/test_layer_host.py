@@ -51,7 +51,8 @@ def test_route_refuses_sizes_and_pointers(vp):
     assert L.vp_route(P, 0, 4, 256, 256, None, None, P, P, None) == bad
     for args in ((None, P, P), (P, None, P), (P, P, None)):
         assert L.vp_route(args[0], 0, 4, 256, 256, C.byref(p), None, args[1], args[2], None) == bad
-    assert L.vp_route_grad(P, 0, 4, 256, 256, C.byref(p), P, P, P, P, None, None) == bad
+    assert L.vp_route_grad(P, 0, 4, 256, 256, C.byref(p), P, P, P, None, P, None) == bad
+    assert L.vp_route_grad(P, 0, 0, 256, 256, C.byref(p), P, P, P, P, None, None) == vp.OK   # no status, no report
     assert L.vp_expert_offsets(P, 3, 8, 0, P, P, None) == bad
     assert L.vp_expert_offsets(P, 2, 8, 2, P, P, None) == bad
     assert L.vp_expert_offsets(P, 2, 8192, 0, P, P, None) == bad
@@ -68,7 +69,7 @@ def matmul(vp, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=0), 1), (dict(dtype=7), 1), (dict(R=-1), 1), (dict(L=0), 1), (dict(L=4097), 5), (dict(N=12), 5),
     (dict(K=60), 5), (dict(N=0), 1), (dict(K=0), 1), (dict(x=None), 1), (dict(w=None), 1), (dict(y=None), 1),
-    (dict(off=None), 1), (dict(st=None), 1), (dict(x=P + 8), 1), (dict(w=P + 2), 1), (dict(y=P + 4), 1),
+    (dict(off=None), 1), (dict(x=P + 8), 1), (dict(w=P + 2), 1), (dict(y=P + 4), 1),
     (dict(x_stride=120), 1), (dict(x_stride=136), 1), (dict(y_stride=48), 1), (dict(x_stride=(1 << 22) + 16), 5),
     (dict(gated=2), 1), (dict(gated=1, N=24), 5), (dict(pre=P, pre_stride=64), 1), (dict(gated=1, pre=P, pre_stride=32), 1),
     (dict(R=1 << 31), 5), (dict(K=1 << 21, x_stride=1 << 22), 5)])
@@ -78,6 +79,7 @@ def test_expert_matmul_refuses(vp, kw, status):
 
 def test_no_rows_is_no_error(vp):
     assert matmul(vp, R=0, x=None, y=None) == vp.OK
+    assert matmul(vp, R=0, x=None, y=None, st=None) == vp.OK
     assert vp.lib().vp_expert_matmul_grad_x(None, 64, 1, P, P, 0, 2, 32, 64, None, 128, P, None) == vp.OK
 
 
