@@ -54,6 +54,29 @@ template <> __device__ inline u32x4 pack16<float>(const float* f) {
   return v;
 }
 
+// f over groups of LPT neighbouring lanes (16 or 64), the result in every one of
+// them, by data movement in the vector unit.
+template <int CTRL, typename T> __device__ inline T moved(T v) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int LPT, typename T, typename F> __device__ inline T across(T v, F f) {
+#ifdef __HIP_DEVICE_COMPILE__
+  v = f(v, moved<0xB1>(v));    // within pairs
+  v = f(v, moved<0x4E>(v));    // fours
+  v = f(v, moved<0x141>(v));   // eights: each half row mirrored
+  v = f(v, moved<0x140>(v));   // rows of 16, mirrored
+  if constexpr (LPT == 64) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);   // even rows, odd rows
+    v = f(__builtin_bit_cast(T, (unsigned)a[0]), __builtin_bit_cast(T, (unsigned)a[1]));
+    const unsigned w = __builtin_bit_cast(unsigned, v);
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);   // halves
+    v = f(__builtin_bit_cast(T, (unsigned)b[0]), __builtin_bit_cast(T, (unsigned)b[1]));
+  }
+#endif
+  return v;
+}
+
 inline int64_t dtype_size(int32_t d) { return d == VP_F32 ? 4 : 2; }
 inline bool is_dtype(int32_t d) { return d == VP_F32 || d == VP_BF16 || d == VP_F16; }
 
