@@ -6,7 +6,9 @@
  *   (3) channel-ordered send buffers            (Sec. 5 "Device-resident buffer layout"),
  * against an offline catalog of contention-free channel families
  * (Sec. 4.1, Alg. 1), and unpacks received buffers into the output layout,
- * for the dispatch and for the combine that returns the rows.
+ * for the dispatch and for the combine that returns the rows.  Around these
+ * stand the calls of the layer itself: routing to experts, the experts'
+ * products, the merge of the returned rows, and rows in 4-bit blocks.
  *
  * Conventions shared by every entry point
  * ---------------------------------------

@@ -1,4 +1,4 @@
-"""Python binding of libvp: the VarioPath demand -> plan -> pack hot path on MI355X.
+"""Python binding of libvp: the VarioPath demand -> plan -> pack hot path on MI355X, and the layer around it (layer.py).
 
 Argument marshalling only: every step runs in the HIP library's kernels
 (``libvp.so`` next to this file, built by ``paper_2609_34340_amd.build``).
