@@ -19,7 +19,8 @@
 // buffered.  Both operands are read through buffer descriptors that end with
 // the expert's last row: what lies outside reads as zero, so no neighbour's
 // row (which may hold anything) enters a sum.  The places in LDS are permuted
-// so that the matrix fragments' reads meet no bank twice:
+// so that the matrix fragments' reads meet no bank twice (in 4-bit blocks, whose
+// lanes take neighbouring chunks, some do):
 //   rows by contraction   16-byte chunk c of row r at place c ^ (r & 7); a
 //                         fragment lane reads its row's chunk whole
 //   contraction by rows   (grad x's weights, both operands of grad w) 32-byte
@@ -159,8 +160,8 @@ __device__ inline void check_offsets(const ProductArgs& a) {
 __device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 template <typename T> struct Frag;
-template <> struct Frag<Bf16> { using type = bf16x8; using elem = __bf16; };
-template <> struct Frag<F16> { using type = f16x8; using elem = _Float16; };
+template <> struct Frag<Bf16> { using type = bf16x8; };
+template <> struct Frag<F16> { using type = f16x8; };
 
 // To a few units of the last place of 32 bits for |g| in the tens (the product
 // with log2 e is rounded), far inside the 16 bits that the result is rounded
@@ -189,10 +190,17 @@ __device__ inline void direct_load(const unsigned char* base, int bytes, uint32_
 #ifdef __HIP_DEVICE_COMPILE__
   const uint64_t b = (uint64_t)base;
   const auto same = [](uint32_t v) { return __builtin_amdgcn_readfirstlane((int)v); };   // in scalar registers
-  const i32x4 rsrc = {same((uint32_t)b), same((uint32_t)(b >> 32) & 0xffff), same(bytes), 0x00020000};
+  const uint64_t words01 = (uint64_t)(uint32_t)same((uint32_t)(b >> 32) & 0xffff) << 32 | (uint32_t)same((uint32_t)b);
+  const uint64_t words23 = 0x00020000ull << 32 | (uint32_t)same(bytes);
   const int at = same((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(at), "v"(off), "s"(rsrc) : "memory");   // nothing else in these kernels uses m0
+  // A memory instruction may read a scalar register only five wait states after a vector instruction wrote it (the
+  // read of a lane, or a spilled register's return, which the compiler may put right before this block); a scalar
+  // instruction waits by itself, so the descriptor is moved by those.  They are also the wait state that m0 needs.
+  // (No-operations in their place took up to 2% more of the smaller products.)
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 s[96:97], %2\n\ts_mov_b64 s[98:99], %3\n\t"
+               "buffer_load_dwordx4 %1, s[96:99], 0 offen lds"
+               :: "s"(at), "v"(off), "s"(words01), "s"(words23)
+               : "memory", "s96", "s97", "s98", "s99");   // nothing else in these kernels uses m0
 #endif
 }
 
@@ -582,7 +590,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
     }
   };
 
-  // A step is two halves of 32 16-bit (128 4-bit) values, each eight rows of
+  // A step is two halves of 32 16-bit (128 4-bit) values, each MT rows of
   // products.  A row's fragment is replaced by its next half's as soon as the
   // row is done, so one set of them is enough; the columns' are read half a
   // step ahead.  Once every wavefront has read a step's columns (in its first
