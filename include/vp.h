@@ -639,6 +639,17 @@ vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq,
                               int32_t L, int32_t N, int32_t K, int32_t gated, void* y, int32_t dtype,
                               int64_t y_stride, int32_t* dev_status, void* stream);
 
+/* Which kernel the sizes of a layer call select, for tests and profiles (host
+ * only; a negative value for sizes that the call refuses).  The products' rules
+ * take R, the rows of the buffer: a buffer much larger than the rows in use
+ * selects the kernel of many rows.
+ *   vp_expert_kernel  a vp_expert_kind; `direction` 0 forward, 1 grad x, 2 grad w;
+ *                     mx: both operands in 4-bit blocks (forward only)
+ *   vp_route_lanes    lanes that share a token: 64 or 16 */
+typedef enum { VP_EXPERT_FEW_ROWS = 0, VP_EXPERT_TILES_128 = 1, VP_EXPERT_TILES_256 = 2 } vp_expert_kind;
+int32_t vp_expert_kernel(int32_t direction, int32_t mx, int32_t gated, int64_t R, int32_t L, int32_t N, int32_t K);
+int32_t vp_route_lanes(int64_t T, int32_t E);
+
 /* --------------------------------------------------------------- helpers */
 
 /* Modeled completion time of a schedule, Eq. (2), as the exact fraction

@@ -249,4 +249,28 @@ vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq,
   return vp::launch_expert_product(a, stream);
 }
 
+int32_t vp_expert_kernel(int32_t direction, int32_t mx, int32_t gated, int64_t R, int32_t L, int32_t N, int32_t K) {
+  static const int64_t some_offsets = 0;   // only for the check
+  if (direction < 0 || direction > 2 || (mx != 0 && mx != 1) || (gated != 0 && gated != 1)) return -1;
+  if (direction != vp::kExpertForward && (mx || gated)) return -1;
+  if (check_experts(VP_BF16, &some_offsets, R, L, N, K) != VP_OK || (mx && K % 32 != 0)) return -1;
+  const int64_t w_row = mx ? vp::mx_row_bytes(K) : (int64_t)K * 2;
+  if (check_gated(gated, N, w_row) != VP_OK) return -1;
+  vp::ExpertLaunch a{};
+  a.mode = direction;
+  a.gated = gated != 0;
+  a.mx = mx != 0;
+  a.dtype = VP_BF16;
+  a.b_stride = w_row;
+  a.R = R;
+  a.L = L;
+  a.N = N;
+  a.K = K;
+  return vp::expert_kind(a);
+}
+
+int32_t vp_route_lanes(int64_t T, int32_t E) {
+  return T < 0 || E < 1 || E > kMaxExperts ? -1 : vp::route_lanes(T, E);
+}
+
 }  // extern "C"

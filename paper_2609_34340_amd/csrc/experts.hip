@@ -922,25 +922,45 @@ template <typename T> bool few_rows_win(const ProductArgs& a, int64_t weight_row
 // at 8 of 2048 x 2048 93 / 67, 4096 rows, one of 4096 x 4096 185 / 119.  Grad w
 // where 256 x 256 leave half of the CUs without a tile: 2048 rows, one expert,
 // 2048 x 2048 42 / 59, 1024 rows at 8 of them (512 tiles) 40 / 36.
-template <typename T, int MODE, bool GATED> vp_status launch_product_as(const ProductArgs& a, hipStream_t s) {
+template <typename T, int MODE, bool GATED> vp_expert_kind kind_of(const ProductArgs& a) {
   const int64_t columns = GATED ? 2 * (int64_t)a.N : a.N;
   if constexpr (MODE == kForward) {
-    if (few_rows_win<T>(a, columns)) {
+    if (few_rows_win<T>(a, columns)) return VP_EXPERT_FEW_ROWS;
+  }
+  const bool small = MODE == kGradW ? (int64_t)a.L * ((a.M + 255) / 256) * ((a.N + 255) / 256) <= kCus / 2
+                                    : (a.R / 128 + a.L / 2 + 1) * ((columns + 127) / 128) <= kCus * 5 / 2;
+  return small ? VP_EXPERT_TILES_128 : VP_EXPERT_TILES_256;
+}
+
+template <typename T, int MODE, bool GATED> vp_status launch_product_as(const ProductArgs& a, hipStream_t s) {
+  const vp_expert_kind kind = kind_of<T, MODE, GATED>(a);
+  if constexpr (MODE == kForward) {
+    if (kind == VP_EXPERT_FEW_ROWS) {
       const unsigned cols = GATED ? kFewCols / 2 : kFewCols;
       hipLaunchKernelGGL((product_few<T, GATED>), dim3((a.N + cols - 1) / cols, (unsigned)(a.R / kFewRows + a.L)), dim3(256), 0, s, a);
       if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
       return VP_OK;
     }
   }
-  const bool small = MODE == kGradW ? (int64_t)a.L * ((a.M + 255) / 256) * ((a.N + 255) / 256) <= kCus / 2
-                                    : (a.R / 128 + a.L / 2 + 1) * ((columns + 127) / 128) <= kCus * 5 / 2;
-  return small ? launch_tiled<T, MODE, GATED, 2, 2, 4, 4>(a, s) : launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
+  return kind == VP_EXPERT_TILES_128 ? launch_tiled<T, MODE, GATED, 2, 2, 4, 4>(a, s)
+                                     : launch_tiled<T, MODE, GATED, 2, 4, 8, 4>(a, s);
 }
 
-}  // namespace
+// Calls f with the product's element type, direction and gate as types.
+template <typename F> auto as_types(const ExpertLaunch& p, F f) {
+  const bool bf = p.dtype == VP_BF16;
+  const auto typed = [&](auto mode, auto gated) {
+    return bf ? f(Bf16{}, mode, gated) : f(F16{}, mode, gated);
+  };
+  if (p.mode == kExpertGradX) return typed(std::integral_constant<int, kGradX>{}, std::false_type{});
+  if (p.mode == kExpertGradW) return typed(std::integral_constant<int, kGradW>{}, std::false_type{});
+  constexpr std::integral_constant<int, kForward> forward{};
+  if (!p.mx) return p.gated ? typed(forward, std::true_type{}) : typed(forward, std::false_type{});
+  if (p.gated) return bf ? f(Mx<Bf16>{}, forward, std::true_type{}) : f(Mx<F16>{}, forward, std::true_type{});
+  return bf ? f(Mx<Bf16>{}, forward, std::false_type{}) : f(Mx<F16>{}, forward, std::false_type{});
+}
 
-vp_status launch_expert_product(const ExpertLaunch& p, void* stream) {
-  hipStream_t s = (hipStream_t)stream;
+ProductArgs product_args(const ExpertLaunch& p) {
   ProductArgs a{};
   a.a = (const unsigned char*)p.a;
   a.b = (const unsigned char*)p.b;
@@ -954,36 +974,37 @@ vp_status launch_expert_product(const ExpertLaunch& p, void* stream) {
   a.out_stride = p.out_stride;
   a.pre_stride = p.pre_stride;
   a.status = p.status;
-  const bool bf = p.dtype == VP_BF16;
   if (p.mode == kExpertForward) {
     a.C = p.K;
     a.N = p.gated ? p.N / 2 : p.N;
     a.half = p.N / 2;
     a.b_expert = p.N * p.b_stride;
-    if (p.mx) {
-      if (bf && p.gated) return launch_product_as<Mx<Bf16>, kForward, true>(a, s);
-      if (bf) return launch_product_as<Mx<Bf16>, kForward, false>(a, s);
-      if (p.gated) return launch_product_as<Mx<F16>, kForward, true>(a, s);
-      return launch_product_as<Mx<F16>, kForward, false>(a, s);
-    } else {
-      if (bf && p.gated) return launch_product_as<Bf16, kForward, true>(a, s);
-      if (bf) return launch_product_as<Bf16, kForward, false>(a, s);
-      if (p.gated) return launch_product_as<F16, kForward, true>(a, s);
-      return launch_product_as<F16, kForward, false>(a, s);
-    }
   } else if (p.mode == kExpertGradX) {
     a.C = p.N;
     a.N = p.K;
     a.b_expert = p.N * p.b_stride;
-    if (bf) return launch_product_as<Bf16, kGradX, false>(a, s);
-    return launch_product_as<F16, kGradX, false>(a, s);
   } else {
     a.M = p.N;
     a.N = p.K;
     a.b_expert = (int64_t)p.N * p.out_stride;
-    if (bf) return launch_product_as<Bf16, kGradW, false>(a, s);
-    return launch_product_as<F16, kGradW, false>(a, s);
   }
+  return a;
+}
+
+}  // namespace
+
+vp_status launch_expert_product(const ExpertLaunch& p, void* stream) {
+  const ProductArgs a = product_args(p);
+  return as_types(p, [&](auto type, auto mode, auto gated) {
+    return launch_product_as<decltype(type), decltype(mode)::value, decltype(gated)::value>(a, (hipStream_t)stream);
+  });
+}
+
+vp_expert_kind expert_kind(const ExpertLaunch& p) {
+  const ProductArgs a = product_args(p);
+  return as_types(p, [&](auto type, auto mode, auto gated) {
+    return kind_of<decltype(type), decltype(mode)::value, decltype(gated)::value>(a);
+  });
 }
 
 vp_status launch_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride,

@@ -199,6 +199,7 @@ vp_status launch_transpose(const int64_t* D, int32_t N, int64_t* DT, void* strea
 // (the logits' in elements).
 vp_status launch_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t stride,
                        const vp_route_params& p, const float* bias, int32_t* ids, float* weights, void* stream);
+int32_t route_lanes(int64_t T, int32_t E);
 vp_status launch_route_grad(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t stride,
                             const vp_route_params& p, const int32_t* ids, const float* weights,
                             const float* d_weights, void* d_logits, int32_t* status, void* stream);
@@ -219,6 +220,7 @@ struct ExpertLaunch {
   int32_t* status;
 };
 vp_status launch_expert_product(const ExpertLaunch& p, void* stream);
+vp_expert_kind expert_kind(const ExpertLaunch& p);   // of its sizes, strides of the weights and types
 vp_status launch_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride,
                                   int32_t dtype, int64_t R, int32_t half, const int64_t* offsets, int32_t L, void* out,
                                   int64_t out_stride, int32_t* status, void* stream);

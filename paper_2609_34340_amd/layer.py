@@ -46,6 +46,8 @@ def declare(L) -> None:
     L.vp_mx_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp]
     L.vp_mx_dequantize.argtypes = [vp, i64, i64, i64, vp, i32, i64, vp]
     L.vp_expert_matmul_mx.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, vp, i32, i64, vp, vp]
+    L.vp_expert_kernel.argtypes = [i32, i32, i32, i64, i32, i32, i32]
+    L.vp_route_lanes.argtypes = [i64, i32]
 
 
 # The checks are written for their cost: a small call is bound by the host (a decode step's merge 10 us a pass, of which
@@ -364,3 +366,23 @@ def expert_matmul_mx(xq: torch.Tensor, wq: torch.Tensor, offsets: torch.Tensor, 
     _check(lib().vp_expert_matmul_mx(_ptr(xq), ldx, _ptr(wq), _ptr(offsets), R, L, N, K, int(gated), _ptr(out), dt,
                                      2 * ldy, _ptr(status), _stream(stream)), "vp_expert_matmul_mx")
     return out
+
+
+# -------------------------------------------------------- kernels chosen
+
+def expert_kernel(R: int, n_local: int, N: int, K: int, *, mode: str = "forward", gated: bool = False,
+                  mx: bool = False) -> str:
+    """vp_expert_kernel: "few_rows", "tiles_128" or "tiles_256", by which a product of these sizes is computed; mode
+    "forward", "grad_x" or "grad_w"."""
+    kind = lib().vp_expert_kernel(("forward", "grad_x", "grad_w").index(mode), int(mx), int(gated), R, n_local, N, K)
+    if kind < 0:
+        raise ValueError("no product has these sizes")
+    return ("few_rows", "tiles_128", "tiles_256")[kind]
+
+
+def route_lanes(T: int, E: int) -> int:
+    """vp_route_lanes: how many lanes share a token of E experts' logits where T tokens are routed, 64 or 16."""
+    lanes = int(lib().vp_route_lanes(T, E))
+    if lanes < 0:
+        raise ValueError("no routing has these sizes")
+    return lanes

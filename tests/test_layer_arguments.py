@@ -1,0 +1,30 @@
+"""What the layer calls make of their arguments before anything is enqueued (no GPU)."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def vp():
+    import os
+    import paper_2609_34340_amd as vp
+    if not os.path.exists(vp.LIB_PATH):
+        from paper_2609_34340_amd import build
+        build.build()
+    return vp
+
+
+def test_the_kernel_that_sizes_select(vp):
+    L = vp.lib()
+    assert vp.expert_kernel(64, 4, 4096, 4096) == "few_rows" and vp.expert_kernel(32768, 4, 4096, 4096) == "tiles_256"
+    assert vp.expert_kernel(64, 4, 4096, 4096, mode="grad_x") == "tiles_128"
+    assert vp.expert_kernel(0, 1, 8, 8, mode="grad_w") == "tiles_128"
+    assert vp.route_lanes(1, 256) == 64 and vp.route_lanes(16384, 256) == 16 and vp.route_lanes(16384, 257) == 64
+    for args in ((3, 0, 0, 8, 1, 16, 32), (0, 2, 0, 8, 1, 16, 32), (0, 0, 2, 8, 1, 16, 32), (1, 1, 0, 8, 1, 16, 32),
+                 (2, 0, 1, 8, 1, 16, 32), (0, 0, 0, -1, 1, 16, 32), (0, 0, 0, 8, 0, 16, 32), (0, 0, 0, 8, 1, 12, 32),
+                 (0, 0, 1, 8, 1, 24, 32), (0, 1, 0, 8, 1, 16, 48), (0, 0, 0, 1 << 31, 1, 16, 32)):
+        assert L.vp_expert_kernel(*args) < 0, args
+    for args in ((-1, 8), (1, 0), (1, 4097)):
+        assert L.vp_route_lanes(*args) < 0
+    with pytest.raises(ValueError):
+        vp.expert_kernel(8, 1, 12, 32)
+    with pytest.raises(ValueError):
+        vp.route_lanes(1, 4097)
