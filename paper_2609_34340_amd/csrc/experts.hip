@@ -859,7 +859,7 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(GateArgs a) {
     if (threadIdx.x == 0) report(a.status, VP_ERR_INVALID_ARGUMENT);
     return;
   }
-  const int64_t m = blockIdx.x;
+  const int64_t m = block_index();
   if (m < first || m >= last) return;
   for (int c = threadIdx.x; c < a.half / 8; c += 256) {
     float dh[8], g[8], u[8];
@@ -890,8 +890,8 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
   const int64_t nt = (a.N + kTileN - 1) / kTileN;
   int64_t per = MODE == kGradW ? (((a.M + BM - 1) / BM) * nt + 7) / 8 * a.L : ((a.R / BM + a.L) * nt + 7) / 8;
   if (per * 8 >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
-  if (MODE != kGradW) per = std::min<int64_t>(per, kCus / 8 * (BM == 128 ? 2 : 1));
-  
+  // (a dimension of a grid holds fewer than 2^32 threads: grad w's workgroups take more than one of very many tiles)
+  per = std::min<int64_t>(per, MODE == kGradW ? 1 << 19 : kCus / 8 * (BM == 128 ? 2 : 1));
   hipLaunchKernelGGL((product_tiled<T, MODE, GATED, WM, WN, MT, NT>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "expert product launch failed");
   return VP_OK;
@@ -1013,8 +1013,8 @@ vp_status launch_expert_gate_grad(const void* dh, int64_t dh_stride, const void*
   const GateArgs a{(const unsigned char*)dh, (const unsigned char*)pre, (unsigned char*)out, dh_stride, pre_stride,
                    out_stride, offsets, R, L, half, status};
   if (R > 0) {
-    if (dtype == VP_BF16) hipLaunchKernelGGL(gate_grad_kernel<Bf16>, dim3((unsigned)R), dim3(256), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(gate_grad_kernel<F16>, dim3((unsigned)R), dim3(256), 0, (hipStream_t)stream, a);
+    if (dtype == VP_BF16) hipLaunchKernelGGL(gate_grad_kernel<Bf16>, grid_of(R), dim3(256), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(gate_grad_kernel<F16>, grid_of(R), dim3(256), 0, (hipStream_t)stream, a);
   }
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "gate gradient launch failed");
   return VP_OK;

@@ -24,6 +24,7 @@ constexpr int kMaxThreads = 512;
 constexpr int kAhead = 8;   // rows whose loads are issued together
 
 struct MergeArgs {
+  int64_t T;
   const unsigned char* rows;
   int64_t row_stride;   // bytes
   const float* weights;
@@ -38,7 +39,8 @@ struct MergeArgs {
 template <typename T>
 __global__ void __launch_bounds__(kMaxThreads) merge_kernel(MergeArgs a) {
   constexpr int n = Vec<T>::n;
-  const int64_t t = blockIdx.x;
+  const int64_t t = block_index();
+  if (t >= a.T) return;
   const float* w = a.weights + t * a.k;
   for (int c = threadIdx.x; c < a.vecs; c += blockDim.x) {
     float acc[n];
@@ -81,7 +83,8 @@ template <typename T>
 __global__ void __launch_bounds__(kMaxThreads) merge_grad_kernel(MergeArgs a) {
   constexpr int n = Vec<T>::n;
   extern __shared__ float part[];   // [wavefronts][k]
-  const int64_t t = blockIdx.x;
+  const int64_t t = block_index();
+  if (t >= a.T) return;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
   const float* w = a.weights + t * a.k;
   for (int i = threadIdx.x; i < waves * a.k; i += blockDim.x) part[i] = 0.0f;
@@ -151,6 +154,7 @@ vp_status launch_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, in
                        const float* weights, const void* residual, int64_t residual_stride, void* out,
                        int64_t out_stride, void* stream) {
   MergeArgs a{};
+  a.T = T;
   a.rows = (const unsigned char*)rows;
   a.row_stride = row_stride;
   a.weights = weights;
@@ -161,7 +165,7 @@ vp_status launch_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, in
   a.out = (unsigned char*)out;
   a.out_stride = out_stride;
   if (T > 0 && a.vecs > 0) {
-    const dim3 grid((unsigned)T), block(threads_for(a.vecs, kMaxThreads));
+    const dim3 grid = grid_of(T), block(threads_for(a.vecs, kMaxThreads));
     hipStream_t s = (hipStream_t)stream;
     if (dtype == VP_F32) hipLaunchKernelGGL(merge_kernel<float>, grid, block, 0, s, a);
     else if (dtype == VP_BF16) hipLaunchKernelGGL(merge_kernel<Bf16>, grid, block, 0, s, a);
@@ -175,6 +179,7 @@ vp_status launch_merge_grad(const void* d_out, int32_t dtype, int64_t T, int32_t
                             const void* rows, int64_t row_stride, const float* weights, void* d_rows,
                             int64_t d_rows_stride, float* d_weights, void* stream) {
   MergeArgs a{};
+  a.T = T;
   a.rows = (const unsigned char*)rows;
   a.row_stride = row_stride;
   a.weights = weights;
@@ -187,7 +192,7 @@ vp_status launch_merge_grad(const void* d_out, int32_t dtype, int64_t T, int32_t
   a.d_weights = d_weights;
   if (T > 0) {
     const int threads = threads_for((a.vecs + kVecs - 1) / kVecs, kMaxThreads);
-    const dim3 grid((unsigned)T), block(threads);
+    const dim3 grid = grid_of(T), block(threads);
     const size_t lds = (size_t)(threads / 64) * k * 4;
     hipStream_t s = (hipStream_t)stream;
     if (dtype == VP_F32) hipLaunchKernelGGL(merge_grad_kernel<float>, grid, block, lds, s, a);

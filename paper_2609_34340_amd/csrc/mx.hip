@@ -67,7 +67,7 @@ struct MxArgs {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(MxArgs a) {
   const int sub = threadIdx.x & (a.per_row - 1);
-  const int64_t r = (int64_t)blockIdx.x * (kThreads / a.per_row) + threadIdx.x / a.per_row;
+  const int64_t r = block_index() * (kThreads / a.per_row) + threadIdx.x / a.per_row;
   if (r >= a.rows) return;
   const unsigned char* src = a.in + r * a.in_stride;
   unsigned char* dst = a.out + r * a.out_stride;
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(MxArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxArgs a) {
   const int sub = threadIdx.x & (a.per_row - 1);
-  const int64_t r = (int64_t)blockIdx.x * (kThreads / a.per_row) + threadIdx.x / a.per_row;
+  const int64_t r = block_index() * (kThreads / a.per_row) + threadIdx.x / a.per_row;
   if (r >= a.rows) return;
   const unsigned char* src = a.in + r * a.in_stride;
   unsigned char* dst = a.out + r * a.out_stride;
@@ -112,7 +112,7 @@ template <typename F> void launch_rows(F kernel, MxArgs a, hipStream_t s) {
   while (a.per_row < kThreads && a.per_row < a.K / kPer) a.per_row *= 2;
   const int64_t rows = kThreads / a.per_row;
   if (a.rows > 0)
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + rows - 1) / rows)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(kernel, grid_of((a.rows + rows - 1) / rows), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace

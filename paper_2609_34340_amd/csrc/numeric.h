@@ -77,6 +77,14 @@ template <int LPT, typename T, typename F> __device__ inline T across(T v, F f) 
   return v;
 }
 
+// A dimension of a grid holds fewer than 2^32 threads (a launch of more runs some of them, and returns no error): blocks of
+// up to 1,024 threads past the 2^21st go on in the second dimension, whose last line may be part empty.
+constexpr int64_t kGridLine = 1 << 21;
+inline dim3 grid_of(int64_t blocks) {
+  return blocks <= kGridLine ? dim3((unsigned)blocks) : dim3((unsigned)kGridLine, (unsigned)((blocks + kGridLine - 1) / kGridLine));
+}
+__device__ inline int64_t block_index() { return (int64_t)blockIdx.y * kGridLine + blockIdx.x; }
+
 inline int64_t dtype_size(int32_t d) { return d == VP_F32 ? 4 : 2; }
 inline bool is_dtype(int32_t d) { return d == VP_F32 || d == VP_BF16 || d == VP_F16; }
 

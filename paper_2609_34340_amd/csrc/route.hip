@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteArgs a) {
   const int kTok = blockDim.x / LPT;
   extern __shared__ uint32_t lds[];
   const int E = a.E, k = a.k, tok = threadIdx.x / LPT, sub = threadIdx.x % LPT;
-  const int64_t t = (int64_t)blockIdx.x * kTok + tok;
+  const int64_t t = block_index() * kTok + tok;
   const bool live = t < a.T;
   const T* row = (const T*)a.logits + (live ? t : a.T - 1) * a.stride;   // a spare token repeats the last one
 
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteGradArgs a) {
   constexpr int kTok = kThreads / 64;
   extern __shared__ float terms[];
   const int E = a.E, k = a.k, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int64_t t = (int64_t)blockIdx.x * kTok + wave;
+  const int64_t t = block_index() * kTok + wave;
   float* mine = terms + wave * E;
   const bool live = t < a.T;
   const T* row = (const T*)a.logits + (live ? t : a.T - 1) * a.stride;
@@ -297,7 +297,7 @@ template <typename T> void launch_route_as(const RouteArgs& a, hipStream_t s) {
   const auto go = [&](auto kernel, int lpt, int threads) {
     const int tok = threads / lpt;
     const size_t lds = 4 * (size_t)tok * (a.k + 1 + (a.n_groups > 1 ? a.E + 1 + 2 * a.n_groups : 0));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + tok - 1) / tok)), dim3(threads), lds, s, a);
+    hipLaunchKernelGGL(kernel, grid_of((a.T + tok - 1) / tok), dim3(threads), lds, s, a);
   };
   const bool few = route_lanes(a.T, a.E) == 64;
   if (few && a.E <= 64) go(route_kernel<T, 64, 1>, 64, kThreads);
@@ -330,7 +330,7 @@ vp_status launch_route_grad(const void* logits, int32_t dtype, int64_t T, int32_
   const RouteGradArgs a{logits, T, stride, E, p.top_k, p.score == VP_SCORE_SIGMOID, p.renorm, p.scale, ids, weights,
                         d_weights, d_logits, status};
   if (T > 0) {
-    const dim3 grid((unsigned)((T + kThreads / 64 - 1) / (kThreads / 64)));
+    const dim3 grid = grid_of((T + kThreads / 64 - 1) / (kThreads / 64));
     const size_t lds = (size_t)(kThreads / 64) * E * 4;
     hipStream_t s = (hipStream_t)stream;
     if (dtype == VP_F32) hipLaunchKernelGGL(route_grad_kernel<float>, grid, dim3(kThreads), lds, s, a);

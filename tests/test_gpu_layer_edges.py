@@ -1,0 +1,91 @@
+"""The layer calls where an input is out of the ordinary: values that are no numbers, weights of zero, offsets out of
+order, launches of more than 2^32 threads, other streams."""
+import math
+
+import pytest
+import torch
+
+import layer_reference as ref
+from test_gpu_layer import near, normal
+
+pytestmark = pytest.mark.gpu
+
+HALVES = [torch.bfloat16, torch.float16]
+FLOATS = HALVES + [torch.float32]
+
+
+@pytest.fixture(scope="module")
+def vp():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2609_34340_amd as vp
+    return vp
+
+
+# ------------------------------------- more than 2^32 threads, wide strides
+
+@pytest.fixture
+def room():
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+def ends(n, m=4097):
+    """The first and last of n rows, and those around the 2^21st and the middle."""
+    mid = [torch.arange(c - 3, c + 3) for c in (1 << 21, n // 2) if 3 < c < n - 3]
+    return torch.cat([torch.arange(min(n, m)), *mid, torch.arange(n - min(n, m), n)]).unique().cuda()
+
+
+def test_merge_of_two_to_the_26_tokens(vp, room):
+    T, H = (1 << 26) + 5, 8   # 64 threads a token
+    rows = torch.empty((T, H), dtype=torch.bfloat16, device="cuda").normal_()
+    w = torch.full((T, 1), 0.5, device="cuda")
+    assert torch.equal(vp.merge(rows, w), rows * 0.5)
+    g, gw = vp.merge_grad(rows, rows, w)
+    assert torch.equal(g, rows * 0.5)
+    at = ends(T)
+    near(gw[at, 0], (rows[at].double() ** 2).sum(1).cpu(), 2e-6 * (rows[at].double() ** 2).sum(1).cpu())
+    assert (gw > 0).all()
+
+
+def test_gate_gradient_of_two_to_the_24_rows(vp, room):
+    R, I = (1 << 24) + 5, 8   # 256 threads a row
+    pre = torch.empty((R, 2 * I), dtype=torch.bfloat16, device="cuda").normal_()
+    dh = torch.empty((R, I), dtype=torch.bfloat16, device="cuda").normal_()
+    st = vp.new_status()
+    got = vp.expert_gate_grad(dh, pre, torch.tensor([0, R]).cuda(), status=st)
+    assert vp.read_status(st) == 0
+    at = ends(R)
+    small = vp.expert_gate_grad(dh[at], pre[at], torch.tensor([0, len(at)]).cuda())
+    assert torch.equal(got[at], small)
+
+
+def test_four_bit_rows_two_to_the_24(vp, room):
+    R, K = (1 << 24) + 5, 1056   # 256 threads a row
+    x = torch.empty((R, K), dtype=torch.bfloat16, device="cuda")
+    at = ends(R)
+    x[at] = normal((len(at), K), 230, torch.bfloat16).cuda()
+    want = vp.mx_quantize(x[at])
+    q = vp.mx_quantize(x)
+    assert torch.equal(q[at], want)
+    del x
+    assert torch.equal(vp.mx_dequantize(q, K)[at], vp.mx_dequantize(want, K))
+
+
+def test_routes_of_two_to_the_28_tokens(vp, room):
+    T = (1 << 28) + 5   # sixteen threads a token
+    x = torch.empty((T, 2), dtype=torch.bfloat16, device="cuda").normal_()
+    got = vp.route(x, 1, renorm=True)
+    assert torch.equal(got["ids"][:, 0], (x[:, 1] > x[:, 0]).int()) and (got["weights"] == 1).all()
+
+
+def test_route_gradient_of_two_to_the_26_tokens(vp, room):
+    T = (1 << 26) + 5   # 64 threads a token
+    x = torch.empty((T, 2), dtype=torch.bfloat16, device="cuda").normal_()
+    d = torch.ones((T, 1), device="cuda")
+    out = vp.route(x, 1, score="sigmoid", renorm=False)
+    got = vp.route_grad(x, out["ids"], out["weights"], d, score="sigmoid", renorm=False)
+    at = ends(T)
+    small = vp.route_grad(x[at], out["ids"][at], out["weights"][at], d[at], score="sigmoid", renorm=False)
+    assert torch.equal(got[at], small) and ((got != 0).sum(1) == 1).all()
