@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+from operator import index
 from typing import Optional
 
 import torch
@@ -96,12 +97,17 @@ def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
 
 # --------------------------------------------------------------- routing
 
-@functools.lru_cache(maxsize=64)
 def _route_params(score, k, n_groups, top_groups, group_top, renorm, scale):
+    """The parameter block.  Its arguments become plain values first: a tensor or array can change in place."""
     if score not in SCORES:
         raise ValueError("score must be one of %s" % sorted(SCORES))
-    return C.byref(RouteParams(SCORES[score], k, n_groups, n_groups if top_groups is None else top_groups, group_top,
-                               int(bool(renorm)), scale))
+    return _route_block(SCORES[score], index(k), index(n_groups), index(n_groups if top_groups is None else top_groups),
+                        index(group_top), bool(renorm), float(scale))
+
+
+@functools.lru_cache(maxsize=64)
+def _route_block(score, k, n_groups, top_groups, group_top, renorm, scale):
+    return C.byref(RouteParams(score, k, n_groups, top_groups, group_top, int(renorm), scale))
 
 
 def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optional[torch.Tensor] = None,

@@ -21,6 +21,20 @@ def vp():
     return vp
 
 
+# ---------------------------------------------------------------- routing
+
+def test_a_scale_that_changed_in_place(vp):
+    x, scale = normal((4, 16), 200).cuda(), torch.tensor(1.0)
+    one = vp.route(x, 4, scale=scale)
+    scale.fill_(2.5)
+    got = vp.route(x, 4, scale=scale)
+    assert torch.equal(got["ids"], one["ids"])
+    near(got["weights"], 2.5 * one["weights"].double().cpu(), 1e-6 * torch.ones(4, 4))
+    near(vp.route_grad(x, one["ids"], got["weights"], torch.ones(4, 4).cuda(), renorm=False, scale=scale),
+         vp.route_grad(x, one["ids"], got["weights"], torch.ones(4, 4).cuda(), renorm=False, scale=2.5).double().cpu(),
+         torch.zeros(4, 16))
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture

@@ -1,5 +1,6 @@
 """What the layer calls make of their arguments before anything is enqueued (no GPU)."""
 import pytest
+import torch
 
 
 @pytest.fixture(scope="module")
@@ -28,3 +29,15 @@ def test_the_kernel_that_sizes_select(vp):
         vp.expert_kernel(8, 1, 12, 32)
     with pytest.raises(ValueError):
         vp.route_lanes(1, 4097)
+
+
+def test_route_parameters_are_those_of_the_call(vp):
+    from paper_2609_34340_amd.layer import _route_params
+    scale, groups, renorm = torch.tensor(1.0), torch.tensor(2), torch.tensor(True)
+    p = _route_params("softmax", 4, groups, None, 1, renorm, scale)._obj
+    assert (p.scale, p.n_groups, p.top_groups, p.renorm) == (1.0, 2, 2, 1)
+    scale.fill_(2.5)
+    groups.fill_(4)
+    renorm.fill_(False)
+    p = _route_params("softmax", 4, groups, None, 1, renorm, scale)._obj
+    assert (p.scale, p.n_groups, p.top_groups, p.renorm) == (2.5, 4, 4, 0)
