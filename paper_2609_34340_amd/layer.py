@@ -107,6 +107,8 @@ def _route_params(score, k, n_groups, top_groups, group_top, renorm, scale):
 
 @functools.lru_cache(maxsize=64)
 def _route_block(score, k, n_groups, top_groups, group_top, renorm, scale):
+    if max(abs(v) for v in (k, n_groups, top_groups, group_top)) >= 1 << 31:
+        raise ValueError("top_k and the groups must be below 2^31")   # ctypes would keep the low bits
     return C.byref(RouteParams(score, k, n_groups, top_groups, group_top, int(renorm), scale))
 
 

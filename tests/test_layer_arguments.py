@@ -41,3 +41,11 @@ def test_route_parameters_are_those_of_the_call(vp):
     renorm.fill_(False)
     p = _route_params("softmax", 4, groups, None, 1, renorm, scale)._obj
     assert (p.scale, p.n_groups, p.top_groups, p.renorm) == (2.5, 4, 4, 0)
+
+
+def test_route_parameters_past_32_bits_are_refused(vp):
+    from paper_2609_34340_amd.layer import _route_params
+    for bad in (dict(n_groups=(1 << 32) + 1), dict(top_groups=1 << 31), dict(group_top=-(1 << 31)), dict(k=(1 << 32) + 4)):
+        how = {**dict(score="softmax", k=4, n_groups=1, top_groups=1, group_top=1, renorm=True, scale=1.0), **bad}
+        with pytest.raises(ValueError):
+            _route_params(**how)
