@@ -94,12 +94,22 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteArgs a) {
   };
   uint32_t key[V];
   const bool by_logit = !a.bias && a.n_groups == 1;
+  // A NaN is in every score of its row (an infinity too), and so in the weights.  The choice is made by the scores of
+  // the numbers: NaN left out, infinity their limit.
+  float key_inv = inv;
+  const bool odd = !a.sigmoid && !by_logit && !(inv == inv);
+  if (odd) {   // the same in all lanes of the token
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum += x[v] == -INFINITY || !(x[v] == x[v]) ? 0.0f : x[v] == top ? 1.0f : expf(x[v] - top);
+    key_inv = 1.0f / across<LPT>(sum, [](float p, float q) { return p + q; });
+  }
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int e = expert_of<LPT>(v, sub);
     float s = x[v];
     if (!by_logit) {
-      s = score(s);
+      s = odd && s == s && s != -INFINITY ? (s == top ? 1.0f : expf(s - top)) * key_inv : score(s);
       if (a.bias && e < E) s += a.bias[e];
     }
     key[v] = e >= E ? kTaken : (x[v] == -INFINITY || !(s == s)) ? kMasked : ordered(s);

@@ -35,6 +35,33 @@ def test_a_scale_that_changed_in_place(vp):
          torch.zeros(4, 16))
 
 
+@pytest.mark.parametrize("T,E", [(3, 40), (4099, 40), (3, 256), (4099, 256), (3, 1024), (2, 1280)])
+@pytest.mark.parametrize("groups", [1, 8])
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_logits_that_are_no_numbers_do_not_decide(vp, T, E, groups, dtype):
+    """A softmax's NaN is in every score of its row; the choice is that of the row's numbers all the same."""
+    k = 6
+    x = normal((T, E), 201, std=2.0).to(dtype)
+    x[:, 0], x[:, 1], x[:, 3] = math.nan, -math.inf, math.nan
+    x[0, 5] = math.inf
+    x[1] = math.nan
+    x[1, 7] = 0.5
+    bias = 0.01 * normal((E,), 202)
+    for b in (bias, None):
+        if b is None and groups == 1:
+            continue   # the logits decide themselves
+        how = dict(bias=None if b is None else b.cuda(), n_groups=groups, top_groups=max(groups // 2, 1), group_top=2)
+        got = vp.route(x.cuda(), k, **how)
+        ids = got["ids"].cpu().long()
+        assert torch.isnan(got["weights"][:, 0]).all()
+        clean = torch.where(torch.isnan(x), torch.full_like(x, -math.inf), x)
+        if T > 2:   # a row of numbers, masked and not: the same choice as with the others masked
+            assert torch.equal(ids[2:], vp.route(clean.cuda(), k, **how)["ids"].cpu().long()[2:])
+        assert ids[0, 0] == 5 and not (set(ids[0, 1:].tolist()) & {0, 1, 3})   # infinity is the largest
+        assert ids[1, 0] == 7 and ids[1, 1:].tolist() == [0, 1, 2, 3, 4]      # then nothing is left
+        assert all(len(set(r.tolist())) == k for r in ids)
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture
