@@ -610,7 +610,9 @@ vp_status vp_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, int64_
                    void* stream);
 
 /* Its gradient: d_rows[t * k + j] = weights[t, j] * d_out[t] and d_weights[t,
- * j] = <d_out[t], rows[t * k + j]> (float32); both 0 for a slot of weight 0. */
+ * j] = <d_out[t], rows[t * k + j]> (float32).  Of a slot of weight 0 the former
+ * is 0, and so is the latter where it would be infinite or NaN (a dropped
+ * slot's row may hold anything). */
 vp_status vp_merge_grad(const void* d_out, int32_t dtype, int64_t T, int32_t k, int64_t H, int64_t d_out_stride,
                         const void* rows, int64_t row_stride, const float* weights, void* d_rows,
                         int64_t d_rows_stride, float* d_weights, void* stream);

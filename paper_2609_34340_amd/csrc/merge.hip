@@ -3,8 +3,9 @@
 //   out_t    = residual_t + sum_j w_tj row_(t k + j)
 //   d_row    = w d_out,   d_w = <d_out, row>
 //
-// A slot of weight zero adds nothing and gets no gradient, whatever its row
-// holds (an assignment that was dropped leaves its row unwritten).  Sums are
+// A slot of weight zero adds nothing whatever its row holds (an assignment that
+// was dropped leaves its row unwritten); its weight's gradient is the product
+// too, unless that is no number: then 0.  Sums are
 // in 32 bits and rounded once.  Every row is read once and the output written
 // once: HBM bounds it.  One workgroup per token; a thread holds one 16-byte
 // vector of the token and has up to eight rows' loads in flight.  4096 tokens
@@ -137,7 +138,7 @@ __global__ void __launch_bounds__(kMaxThreads) merge_grad_kernel(MergeArgs a) {
   for (int j = threadIdx.x; j < a.k; j += blockDim.x) {
     float s = 0.0f;
     for (int v = 0; v < waves; ++v) s += part[v * a.k + j];
-    a.d_weights[t * a.k + j] = w[j] == 0.0f ? 0.0f : s;
+    a.d_weights[t * a.k + j] = w[j] == 0.0f && !isfinite(s) ? 0.0f : s;
   }
 }
 

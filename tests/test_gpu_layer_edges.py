@@ -62,6 +62,39 @@ def test_logits_that_are_no_numbers_do_not_decide(vp, T, E, groups, dtype):
         assert all(len(set(r.tolist())) == k for r in ids)
 
 
+# ------------------------------------------------------------------ merge
+
+@pytest.mark.parametrize("T,k,H", [(1, 1, 8), (3, 2, 264), (7, 9, 72), (5, 17, 4104), (33, 8, 7168)])
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_the_gradient_of_a_weight_that_is_zero(vp, T, k, H, dtype):
+    """<d_out, row> there too; 0 where the row of a dropped slot is no numbers."""
+    rows, w, d = normal((T * k, H), 210, dtype), normal((T, k), 211), normal((T, H), 212, dtype)
+    w[:, k - 1] = 0.0
+    w[0, 0] = -0.0
+    rows[k - 1, H - 1] = math.nan
+    if T > 1:
+        rows[2 * k - 1, 3] = math.inf
+    _, gw = vp.merge_grad(d.cuda(), rows.cuda(), w.cuda())
+    prod = d.double()[:, None, :] * rows.double().view(T, k, H)
+    want, size = prod.sum(2), prod.abs().sum(2)
+    dropped = (w == 0) & ~torch.isfinite(want)
+    assert dropped[0, k - 1] and int(dropped.sum()) == min(T, 2)
+    assert (gw.cpu()[dropped] == 0).all()
+    near(gw.cpu()[~dropped], want[~dropped], (H + 2) * 2.0 ** -24 * size[~dropped], "d_weights")
+
+
+def test_the_gradient_of_zero_weights_against_differences(vp):
+    T, k, H = 2, 3, 16
+    rows, d, w = normal((T * k, H), 213), normal((T, H), 214), torch.zeros(T, k)
+    _, gw = vp.merge_grad(d.cuda(), rows.cuda(), w.cuda())
+    f = lambda v: float((d.double() * vp.merge(rows.cuda(), v.cuda()).double().cpu()).sum())  # noqa: E731
+    for i in range(T):
+        for j in range(k):
+            h = torch.zeros(T, k)
+            h[i, j] = 0.5   # the merge is linear in its weights
+            assert abs((f(h) - f(-h)) - float(gw[i, j])) < 1e-5
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture
