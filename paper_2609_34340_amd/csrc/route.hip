@@ -223,7 +223,10 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteGradArgs a) {
   for (int e = lane; e < E; e += 64) mine[e] = 0.0f;
   __syncthreads();
   float dot = 0.0f;
-  for (int j = lane; j < k && live; j += 64) dot += a.weights[t * k + j] * a.d_weights[t * k + j];
+  for (int j = lane; j < k && live; j += 64) {
+    const float w = a.weights[t * k + j];
+    dot += w == 0.0f ? 0.0f : w * a.d_weights[t * k + j];   // a weight of 0 passes nothing on, infinities and NaN neither
+  }
   dot = across<64>(dot, [](float p, float q) { return p + q; });
   for (int j = lane; j < k && live; j += 64) {
     const int id = a.ids[t * k + j];

@@ -62,6 +62,21 @@ def test_logits_that_are_no_numbers_do_not_decide(vp, T, E, groups, dtype):
         assert all(len(set(r.tolist())) == k for r in ids)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_a_weight_of_zero_passes_no_gradient_on(vp, score, renorm):
+    """Whatever the gradient at a slot of weight 0 is, it does not reach the other slots'."""
+    x = normal((2, 12), 203)
+    x[:, 3:] = -math.inf   # three experts are left for five slots
+    out = vp.route(x.cuda(), 5, score=score, renorm=renorm)
+    assert (out["weights"][:, 3:] == 0).all()
+    d = normal((2, 5), 204)
+    want = vp.route_grad(x.cuda(), out["ids"], out["weights"], d.cuda(), score=score, renorm=renorm)
+    d[0, 3:], d[1, 3], d[1, 4] = math.nan, math.inf, -math.inf
+    got = vp.route_grad(x.cuda(), out["ids"], out["weights"], d.cuda(), score=score, renorm=renorm)
+    assert torch.isfinite(want).all() and torch.equal(got, want)
+
+
 # ------------------------------------------------------------------ merge
 
 @pytest.mark.parametrize("T,k,H", [(1, 1, 8), (3, 2, 264), (7, 9, 72), (5, 17, 4104), (33, 8, 7168)])
