@@ -144,6 +144,15 @@ def _stream(stream=None):
     return stream.cuda_stream
 
 
+def _from(stream, make, *args, **kw):
+    """What a call makes for itself (tensors, a schedule), of the memory of the stream its kernels run on: memory that
+    another stream has freed may still be in use there, and that stream may take it again while it is in use here."""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
 def topology(topo) -> _Topology:
     """vp_topology from any object with the vpgen.Topology fields."""
     return _Topology(topo.n_nodes, topo.sockets_per_node, topo.switches_per_socket,
@@ -279,15 +288,16 @@ def demand(routing: torch.Tensor, n_ranks: int, n_experts: int, unit: int, first
     R, T, k = routing.shape
     dev = routing.device
     if out is None:
-        out = dict(counts=torch.empty((R, n_experts), dtype=torch.int32, device=dev),
-                   demand=torch.empty((R, n_ranks), dtype=torch.int64, device=dev),
-                   sorted_tok=torch.empty(max(T * k, 1), dtype=torch.int32, device=dev),
-                   sorted_slot=torch.empty(max(T * k, 1), dtype=torch.uint8, device=dev),
-                   dest_off=torch.empty(n_ranks + 1, dtype=torch.int64, device=dev))
+        out = dict(counts=_from(stream, torch.empty, (R, n_experts), dtype=torch.int32, device=dev),
+                   demand=_from(stream, torch.empty, (R, n_ranks), dtype=torch.int64, device=dev),
+                   sorted_tok=_from(stream, torch.empty, max(T * k, 1), dtype=torch.int32, device=dev),
+                   sorted_slot=_from(stream, torch.empty, max(T * k, 1), dtype=torch.uint8, device=dev),
+                   dest_off=_from(stream, torch.empty, n_ranks + 1, dtype=torch.int64, device=dev))
     if status is None:
-        status = new_status(dev)
+        status = _from(stream, new_status, dev)
     if ws is None:
-        ws = torch.zeros(max(demand_workspace_bytes(R, T, k, n_experts), 1), dtype=torch.uint8, device=dev)
+        ws = _from(stream, torch.zeros, max(demand_workspace_bytes(R, T, k, n_experts), 1), dtype=torch.uint8,
+                   device=dev)
     _check(lib().vp_demand(_ptr(routing), R, T, k, n_experts, n_ranks, first_rank, sort_row, unit,
                            _ptr(out["counts"]), _ptr(out["demand"]), _ptr(out["sorted_tok"]),
                            _ptr(out.get("sorted_slot")), _ptr(out["dest_off"]), _ptr(status), _ptr(ws),
@@ -302,9 +312,9 @@ def demand_heads(T: int, head_lo: torch.Tensor, head_bytes: int, first_rank: int
     _dev(head_lo, torch.int64, "head_lo")
     N = head_lo.numel() - 1
     if out is None:
-        out = torch.empty((R, N), dtype=torch.int64, device=head_lo.device)
+        out = _from(stream, torch.empty, (R, N), dtype=torch.int64, device=head_lo.device)
     if status is None:
-        status = new_status(head_lo.device)
+        status = _from(stream, new_status, head_lo.device)
     _check(lib().vp_demand_heads(T, _ptr(head_lo), head_bytes, N, first_rank, R, _ptr(out), _ptr(status),
                                  _stream(stream)), "vp_demand_heads")
     return out
@@ -318,9 +328,9 @@ def control_words(counts: torch.Tensor, n_ranks: int, first_rank: int = 0,
     _dev(counts, torch.int32, "counts")
     R, E = counts.shape
     if out is None:
-        out = torch.empty((R, n_ranks), dtype=torch.int32, device=counts.device)
+        out = _from(stream, torch.empty, (R, n_ranks), dtype=torch.int32, device=counts.device)
     if status is None:
-        status = new_status(counts.device)
+        status = _from(stream, new_status, counts.device)
     _check(lib().vp_control_words(_ptr(counts), R, E, n_ranks, first_rank, _ptr(out), _ptr(status),
                                   _stream(stream)), "vp_control_words")
     return out
@@ -339,7 +349,7 @@ def receive_counts(words: torch.Tensor, word_stride: int, signal: torch.Tensor, 
     if offset < 0 or word_stride < 1 or offset + (N - 1) * word_stride >= words.numel():
         raise ValueError("words too short for N sources at this offset and stride")
     if out is None:
-        out = torch.empty((N, n_local), dtype=torch.int32, device=signal.device)
+        out = _from(stream, torch.empty, (N, n_local), dtype=torch.int32, device=signal.device)
     _check(lib().vp_receive_counts(words.data_ptr() + 4 * offset, word_stride, _ptr(signal), N,
                                    n_local, _ptr(out), _stream(stream)), "vp_receive_counts")
     return out
@@ -376,11 +386,11 @@ def plan(cat: Catalog, D: torch.Tensor, p: PlanParams, status: Optional[torch.Te
     if tuple(D.shape) != (N, N):
         raise ValueError("demand must be [%d, %d]" % (N, N))
     if out is None:
-        out = alloc_schedule(N, p.k_max, D.device)
+        out = _from(stream, alloc_schedule, N, p.k_max, D.device)
     if status is None:
-        status = new_status(D.device)
+        status = _from(stream, new_status, D.device)
     if ws is None:
-        ws = torch.empty(plan_workspace_bytes(cat, p), dtype=torch.uint8, device=D.device)
+        ws = _from(stream, torch.empty, plan_workspace_bytes(cat, p), dtype=torch.uint8, device=D.device)
     _check(lib().vp_plan(cat.handle, _ptr(D), C.byref(p), _ptr(out["K"]), _ptr(out["family"]),
                          _ptr(out["dst"]), _ptr(out["inst"]), _ptr(out["bytes"]), _ptr(out.get("send_off")),
                          _ptr(out.get("stream_off")), _ptr(out.get("recv_src")), _ptr(out["tau"]), _ptr(status),
@@ -399,9 +409,9 @@ def plan_noalloc(cat: Catalog, D: torch.Tensor, p: PlanParams, status: Optional[
     if tuple(D.shape) != (N, N):
         raise ValueError("demand must be [%d, %d]" % (N, N))
     if out is None:
-        out = alloc_schedule(N, p.k_max, D.device)
+        out = _from(stream, alloc_schedule, N, p.k_max, D.device)
     if status is None:
-        status = new_status(D.device)
+        status = _from(stream, new_status, D.device)
     _check(lib().vp_plan_noalloc(cat.handle, _ptr(D), C.byref(p), _ptr(out["K"]), _ptr(out["family"]),
                                  _ptr(out["dst"]), _ptr(out["inst"]), _ptr(out["bytes"]), _ptr(out.get("send_off")),
                                  _ptr(out.get("stream_off")), _ptr(out.get("recv_src")), _ptr(out["tau"]),
@@ -438,15 +448,15 @@ def plan_batch(cat: Catalog, D: torch.Tensor, p: PlanParams, status: Optional[to
         raise ValueError("demand must be [B, %d, %d]" % (N, N))
     B = D.shape[0]
     if out is None:
-        out = alloc_schedule_batch(B, N, p.k_max, D.device)
+        out = _from(stream, alloc_schedule_batch, B, N, p.k_max, D.device)
     if out["K"].numel() != B or tuple(out["dst"].shape) != (B, p.k_max, N):
         raise ValueError("schedule buffers do not hold B = %d schedules of k_max = %d" % (B, p.k_max))
     if status is None:
-        status = torch.zeros(B, dtype=torch.int32, device=D.device)
+        status = _from(stream, torch.zeros, B, dtype=torch.int32, device=D.device)
     if status.numel() != B:
         raise ValueError("status must hold B entries")
     if ws is None:
-        ws = torch.empty(plan_batch_workspace_bytes(cat, p, B), dtype=torch.uint8, device=D.device)
+        ws = _from(stream, torch.empty, plan_batch_workspace_bytes(cat, p, B), dtype=torch.uint8, device=D.device)
     _check(lib().vp_plan_batch(cat.handle, B, _ptr(D), C.byref(p), _ptr(out["K"]), _ptr(out["family"]),
                                _ptr(out["dst"]), _ptr(out["inst"]), _ptr(out["bytes"]), _ptr(out.get("send_off")),
                                _ptr(out.get("stream_off")), _ptr(out.get("recv_src")), _ptr(out["tau"]),
@@ -485,8 +495,8 @@ def pack_rows(tokens: torch.Tensor, row_bytes: int, sorted_tok: torch.Tensor, so
     N = sched["dst"].shape[1]
     cap = send.numel() * send.element_size()
     if ws is None:
-        ws = torch.zeros(pack_workspace_bytes(k_max, cap, row_bytes, T, k), dtype=torch.uint8,
-                         device=send.device)
+        ws = _from(stream, torch.zeros, pack_workspace_bytes(k_max, cap, row_bytes, T, k), dtype=torch.uint8,
+                   device=send.device)
     _check(lib().vp_pack_rows(_ptr(tokens), T, k, row_bytes, _ptr(sorted_tok), _ptr(sorted_slot), _ptr(dest_off),
                               self_rank, N,
                               _ptr(sched["K"]), _ptr(sched["dst"]), _ptr(sched["bytes"]),
@@ -506,7 +516,8 @@ def pack_heads(act: torch.Tensor, token_stride: int, head_lo: torch.Tensor, head
     N = sched["dst"].shape[1]
     cap = send.numel() * send.element_size()
     if ws is None:
-        ws = torch.zeros(pack_workspace_bytes(k_max, cap, head_bytes), dtype=torch.uint8, device=send.device)
+        ws = _from(stream, torch.zeros, pack_workspace_bytes(k_max, cap, head_bytes), dtype=torch.uint8,
+                   device=send.device)
     _check(lib().vp_pack_heads(_ptr(act), T, token_stride, _ptr(head_lo), head_bytes, self_rank, N,
                                _ptr(sched["K"]), _ptr(sched["dst"]), _ptr(sched["bytes"]),
                                _ptr(sched.get("send_off")), _ptr(sched.get("stream_off")), k_max,
@@ -530,7 +541,7 @@ def demand_transpose(D: torch.Tensor, out: Optional[torch.Tensor] = None, stream
     _dev(D, torch.int64, "demand")
     N = D.shape[0]
     if out is None:
-        out = torch.empty_like(D)
+        out = _from(stream, torch.empty_like, D)
     _check(lib().vp_demand_transpose(_ptr(D), N, _ptr(out), _stream(stream)), "vp_demand_transpose")
     return out
 
@@ -547,7 +558,8 @@ def unpack_rows(recv: torch.Tensor, row_bytes: int, counts: torch.Tensor, self_r
     k_max = sched["dst"].shape[0]
     cap = _nbytes(recv)
     if ws is None:
-        ws = torch.empty(unpack_workspace_bytes(cap // slot_bytes(row_bytes)), dtype=torch.uint8, device=recv.device)
+        ws = _from(stream, torch.empty, unpack_workspace_bytes(cap // slot_bytes(row_bytes)), dtype=torch.uint8,
+                   device=recv.device)
     _check(lib().vp_unpack_rows(_ptr(recv), cap, row_bytes, _ptr(counts), E, self_rank, N, _ptr(sched["K"]),
                                 _ptr(sched["dst"]), _ptr(sched["bytes"]), _ptr(sched["recv_src"]), k_max,
                                 _ptr(out), _nbytes(out), _ptr(status), _ptr(ws), ws.numel(), _stream(stream)),
@@ -563,7 +575,7 @@ def pack_combine(out: torch.Tensor, row_bytes: int, counts: torch.Tensor, self_r
     k_max = sched["dst"].shape[0]
     cap = _nbytes(send)
     if ws is None:
-        ws = torch.empty(unpack_workspace_bytes(cap // row_bytes), dtype=torch.uint8, device=send.device)
+        ws = _from(stream, torch.empty, unpack_workspace_bytes(cap // row_bytes), dtype=torch.uint8, device=send.device)
     _check(lib().vp_pack_combine(_ptr(out), _nbytes(out), row_bytes, _ptr(counts), E, self_rank, N,
                                  _ptr(sched["K"]), _ptr(sched["dst"]), _ptr(sched["bytes"]), k_max, _ptr(send), cap,
                                  _ptr(step_off), _ptr(status), _ptr(ws), ws.numel(), _stream(stream)),
@@ -580,7 +592,8 @@ def unpack_combine(recv: torch.Tensor, row_bytes: int, T: int, k: int, sorted_to
         raise ValueError("combined must hold T * k slots")
     cap = _nbytes(recv)
     if ws is None:
-        ws = torch.empty(unpack_workspace_bytes(cap // slot_bytes(row_bytes)), dtype=torch.uint8, device=recv.device)
+        ws = _from(stream, torch.empty, unpack_workspace_bytes(cap // slot_bytes(row_bytes)), dtype=torch.uint8,
+                   device=recv.device)
     _check(lib().vp_unpack_combine(_ptr(recv), cap, row_bytes, T, k, _ptr(sorted_tok), _ptr(sorted_slot),
                                    _ptr(dest_off), self_rank, N, _ptr(sched["K"]), _ptr(sched["dst"]),
                                    _ptr(sched["bytes"]), _ptr(sched["recv_src"]), k_max, _ptr(combined),

@@ -17,7 +17,7 @@ from typing import Optional
 
 import torch
 
-from . import _check, _ptr, _stream, lib
+from . import _check, _from, _ptr, _stream, lib
 
 SCORES = {"softmax": 0, "sigmoid": 1}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -123,8 +123,8 @@ def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optiona
     if bias is not None:
         _whole(bias, torch.float32, (E,), "bias")
     if out is None:
-        out = dict(ids=torch.empty((T, k), dtype=torch.int32, device=logits.device),
-                   weights=torch.empty((T, k), dtype=torch.float32, device=logits.device))
+        out = dict(ids=_from(stream, torch.empty, (T, k), dtype=torch.int32, device=logits.device),
+                   weights=_from(stream, torch.empty, (T, k), dtype=torch.float32, device=logits.device))
     ids = _whole(out["ids"], torch.int32, (T, k), "ids")
     weights = _whole(out["weights"], torch.float32, (T, k), "weights")
     _same_device(logits, bias, ids, weights)
@@ -148,7 +148,7 @@ def route_grad(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, d
     _whole(weights, torch.float32, (T, k), "weights")
     _whole(d_weights, torch.float32, (T, k), "d_weights")
     if out is None:
-        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        out = _from(stream, torch.empty, (T, E), dtype=logits.dtype, device=logits.device)
     _whole(out, logits.dtype, (T, E), "d_logits")
     _same_device(logits, ids, weights, d_weights, out, status)
     p = _route_params(score, k, 1, 1, 1, renorm, scale)
@@ -168,7 +168,7 @@ def expert_offsets(counts: torch.Tensor, self_rank: int, out: Optional[torch.Ten
     _whole(counts, torch.int32, (N, E), "counts")
     n_local = E // max(N, 1)
     if out is None:
-        out = torch.empty(n_local + 1, dtype=torch.int64, device=counts.device)
+        out = _from(stream, torch.empty, n_local + 1, dtype=torch.int64, device=counts.device)
     _whole(out, torch.int64, (n_local + 1,), "offsets")
     _same_device(counts, out, status)
     _check(lib().vp_expert_offsets(_ptr(counts), N, E, self_rank, _ptr(out), _ptr(status), _stream(stream)),
@@ -199,7 +199,7 @@ def expert_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, ga
     _groups(offsets, L)
     width = N // 2 if gated else N
     if out is None:
-        out = torch.empty((R, width), dtype=x.dtype, device=x.device)
+        out = _from(stream, torch.empty, (R, width), dtype=x.dtype, device=x.device)
     ldy = _matrix(out, "out", cols=width, dtype=x.dtype, rows=R)
     ldp = 0 if pre is None else _matrix(pre, "pre", cols=N, dtype=x.dtype, rows=R)
     _same_device(x, w, offsets, out, pre, status)
@@ -218,7 +218,7 @@ def expert_matmul_grad_x(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tenso
     R = dy.shape[0]
     _groups(offsets, L)
     if out is None:
-        out = torch.empty((R, K), dtype=dy.dtype, device=dy.device)
+        out = _from(stream, torch.empty, (R, K), dtype=dy.dtype, device=dy.device)
     ldx = _matrix(out, "out", cols=K, dtype=dy.dtype, rows=R)
     _same_device(dy, w, offsets, out, status)
     _check(lib().vp_expert_matmul_grad_x(_ptr(dy), 2 * ldy, dt, _ptr(w), _ptr(offsets), R, L, N, K, _ptr(out),
@@ -239,7 +239,7 @@ def expert_matmul_grad_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tenso
     K, L = x.shape[1], offsets.numel() - 1
     _groups(offsets, L)
     if out is None:
-        out = torch.empty((L, N, K), dtype=torch.float32, device=dy.device)
+        out = _from(stream, torch.empty, (L, N, K), dtype=torch.float32, device=dy.device)
     _whole(out, torch.float32, (L, N, K), "out")
     _same_device(dy, x, offsets, out, status)
     _check(lib().vp_expert_matmul_grad_w(_ptr(dy), 2 * ldy, _ptr(x), 2 * ldx, dt, _ptr(offsets), R, L, N, K,
@@ -258,7 +258,7 @@ def expert_gate_grad(dh: torch.Tensor, pre: torch.Tensor, offsets: torch.Tensor,
     L = offsets.numel() - 1
     _groups(offsets, L)
     if out is None:
-        out = torch.empty((R, 2 * half), dtype=dh.dtype, device=dh.device)
+        out = _from(stream, torch.empty, (R, 2 * half), dtype=dh.dtype, device=dh.device)
     ldo = _matrix(out, "out", cols=2 * half, dtype=dh.dtype, rows=R)
     _same_device(dh, pre, offsets, out, status)
     _check(lib().vp_expert_gate_grad(_ptr(dh), 2 * ldh, _ptr(pre), 2 * ldp, dt, _ptr(offsets), R, L, half, _ptr(out),
@@ -280,7 +280,7 @@ def merge(rows: torch.Tensor, weights: torch.Tensor, *, residual: Optional[torch
     H, size = rows.shape[1], rows.element_size()
     lds = 0 if residual is None else _matrix(residual, "residual", cols=H, dtype=rows.dtype, rows=T)
     if out is None:
-        out = torch.empty((T, H), dtype=rows.dtype, device=rows.device)
+        out = _from(stream, torch.empty, (T, H), dtype=rows.dtype, device=rows.device)
     ldo = _matrix(out, "out", cols=H, dtype=rows.dtype, rows=T)
     _same_device(rows, weights, residual, out)
     _check(lib().vp_merge(_ptr(rows), dt, T, k, H, ldr * size, _ptr(weights), _ptr(residual), lds * size, _ptr(out),
@@ -300,9 +300,9 @@ def merge_grad(d_out: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, *
     H, size = rows.shape[1], rows.element_size()
     ldd = _matrix(d_out, "d_out", cols=H, dtype=rows.dtype, rows=T)
     if d_rows is None:
-        d_rows = torch.empty((T * k, H), dtype=rows.dtype, device=rows.device)
+        d_rows = _from(stream, torch.empty, (T * k, H), dtype=rows.dtype, device=rows.device)
     if d_weights is None:
-        d_weights = torch.empty((T, k), dtype=torch.float32, device=rows.device)
+        d_weights = _from(stream, torch.empty, (T, k), dtype=torch.float32, device=rows.device)
     ldo = _matrix(d_rows, "d_rows", cols=H, dtype=rows.dtype, rows=T * k)
     _whole(d_weights, torch.float32, (T, k), "d_weights")
     _same_device(rows, d_out, weights, d_rows, d_weights)
@@ -329,7 +329,7 @@ def mx_quantize(x: torch.Tensor, *, out: Optional[torch.Tensor] = None, stream=N
     ldx = _matrix(flat, "x")
     rb = mx_row_bytes(K)
     if out is None:
-        out = torch.empty((*x.shape[:-1], rb), dtype=torch.uint8, device=x.device)
+        out = _from(stream, torch.empty, (*x.shape[:-1], rb), dtype=torch.uint8, device=x.device)
     if out.shape != (*x.shape[:-1], rb) or (out.dim() != 2 and not out.is_contiguous()):
         raise ValueError("out must be uint8 %s" % ((*x.shape[:-1], rb),))
     ldq = _matrix(out if out.dim() == 2 else out.view(-1, rb), "out", dtype=torch.uint8)
@@ -345,7 +345,7 @@ def mx_dequantize(q: torch.Tensor, K: int, *, dtype=torch.bfloat16, out: Optiona
     ldq = _matrix(q, "q", cols=mx_row_bytes(K), dtype=torch.uint8)
     R = q.shape[0]
     if out is None:
-        out = torch.empty((R, K), dtype=dtype, device=q.device)
+        out = _from(stream, torch.empty, (R, K), dtype=dtype, device=q.device)
     dt = _float_dtype(out, "out")
     ldo = _matrix(out, "out", cols=K, rows=R)
     _same_device(q, out)
@@ -367,7 +367,7 @@ def expert_matmul_mx(xq: torch.Tensor, wq: torch.Tensor, offsets: torch.Tensor, 
     _groups(offsets, L)
     width = N // 2 if gated else N
     if out is None:
-        out = torch.empty((R, width), dtype=dtype, device=xq.device)
+        out = _from(stream, torch.empty, (R, width), dtype=dtype, device=xq.device)
     dt = _float_dtype(out, "out", halves=True)
     ldy = _matrix(out, "out", cols=width, rows=R)
     _same_device(xq, wq, offsets, out, status)

@@ -110,6 +110,46 @@ def test_the_gradient_of_zero_weights_against_differences(vp):
             assert abs((f(h) - f(-h)) - float(gw[i, j])) < 1e-5
 
 
+# ---------------------------------------------------------------- streams
+
+def test_outputs_come_from_the_stream_they_are_written_on(vp):
+    """Memory that the current stream freed, and may still be using, is not handed to a call on another stream."""
+    T, k, H = 4096, 2, 4096
+    rows, w = torch.ones((T * k, H), dtype=torch.bfloat16, device="cuda"), torch.ones((T, k), device="cuda")
+    off = torch.tensor([0, 2 * T]).cuda()
+    wt = torch.ones((1, 512, H), dtype=torch.bfloat16, device="cuda")
+    logits = torch.zeros((1 << 20, 16), device="cuda")
+    pre = torch.ones((T * k, H), dtype=torch.bfloat16, device="cuda")
+    routing = torch.zeros((8, 1 << 20, 1), dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    r, q, qw = vp.route(logits, 2), vp.mx_quantize(rows), vp.mx_quantize(wt)
+    calls = dict(
+        merge=lambda s: vp.merge(rows, w, stream=s), merge_grad=lambda s: vp.merge_grad(rows[:T], rows, w, stream=s)[0],
+        quantize=lambda s: vp.mx_quantize(rows, stream=s),
+        dequantize=lambda s: vp.mx_dequantize(q, H, stream=s),
+        matmul=lambda s: vp.expert_matmul(rows, wt, off, stream=s),
+        grad_x=lambda s: vp.expert_matmul_grad_x(rows[:, :512], wt, off, stream=s),
+        grad_w=lambda s: vp.expert_matmul_grad_w(rows, rows, off, stream=s),
+        gate_grad=lambda s: vp.expert_gate_grad(pre[:, :H // 2], pre, off, stream=s),
+        mx=lambda s: vp.expert_matmul_mx(q, qw, off, H, stream=s),
+        route=lambda s: vp.route(logits, 2, stream=s)["weights"],
+        route_grad=lambda s: vp.route_grad(logits, r["ids"], r["weights"], r["weights"], stream=s),
+        demand=lambda s: vp.demand(routing, 8, 8, 64, stream=s)["sorted_tok"])
+    for name, call in calls.items():
+        torch.cuda.synchronize()
+        like = call(None)
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        freed = [torch.empty_like(like) for _ in range(8)]
+        places = {t.data_ptr() for t in freed}
+        del freed
+        side.wait_stream(torch.cuda.current_stream())
+        got = call(side)
+        side.synchronize()
+        assert got.data_ptr() not in places, name
+        assert torch.equal(got, like), name
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture
