@@ -591,7 +591,7 @@ vp_status vp_expert_matmul_grad_w(const void* dy, int64_t dy_stride, const void*
 
 /* Gradient of the gated product by x G^T and x U^T: dh device [R, I], pre as
  * vp_expert_matmul left it (I = N/2), dpre device [R, 2 I]; the products'
- * gradients then follow from dpre. */
+ * gradients then follow from dpre.  Offsets as in vp_expert_matmul. */
 vp_status vp_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride, int32_t dtype,
                               const int64_t* offsets, int64_t R, int32_t L, int32_t I, void* dpre,
                               int64_t dpre_stride, int32_t* dev_status, void* stream);

@@ -150,7 +150,7 @@ __device__ inline int nth_largest(const ProductArgs& a, int n, int lane) {
 
 // Offsets that decrease or pass the buffer are the caller's error; products
 // stay inside the buffers all the same.
-__device__ inline void check_offsets(const ProductArgs& a) {
+template <typename Args> __device__ inline void check_offsets(const Args& a) {
   for (int e = threadIdx.x; e < a.L; e += blockDim.x) {
     const int64_t lo = a.offsets[e], hi = a.offsets[e + 1];
     if (lo < 0 || hi < lo || hi > a.R) report(a.status, VP_ERR_INVALID_ARGUMENT);
@@ -854,13 +854,9 @@ struct GateArgs {
 
 template <typename T>
 __global__ void __launch_bounds__(256) gate_grad_kernel(GateArgs a) {
-  const int64_t first = a.offsets[0], last = a.offsets[a.L];
-  if (first < 0 || last > a.R) {
-    if (threadIdx.x == 0) report(a.status, VP_ERR_INVALID_ARGUMENT);
-    return;
-  }
-  const int64_t m = block_index();
-  if (m < first || m >= last) return;
+  const int64_t m = block_index(), first = a.offsets[0], last = a.offsets[a.L];
+  if (m == 0) check_offsets(a);
+  if (first < 0 || last > a.R || m < first || m >= last) return;
   for (int c = threadIdx.x; c < a.half / 8; c += 256) {
     float dh[8], g[8], u[8];
     unpack16<T>(*(const u32x4*)(a.dh + m * a.dh_stride + c * 16), dh);

@@ -150,6 +150,20 @@ def test_outputs_come_from_the_stream_they_are_written_on(vp):
         assert torch.equal(got, like), name
 
 
+# ---------------------------------------------------------------- offsets
+
+BAD_OFFSETS = [[0, 10, 21], [0, 15, 10], [-3, 5, 20], [0, 2 ** 40, 2 ** 41], [5, 3, 20], [20, 0, 20], [0, -2 ** 63, 20],
+               [-2 ** 63, 2 ** 63 - 1, 20]]
+
+
+def test_the_gates_gradient_reports_offsets_out_of_order(vp):
+    dh, pre = normal((20, 32), 220, torch.bfloat16).cuda(), normal((20, 64), 221, torch.bfloat16).cuda()
+    for bad in BAD_OFFSETS + [[0, 5, 3, 20], [7, 0]]:
+        st = vp.new_status()
+        vp.expert_gate_grad(dh, pre, torch.tensor(bad).cuda(), status=st)
+        assert vp.read_status(st) == vp.INVALID_ARGUMENT, bad
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture
