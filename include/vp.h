@@ -573,7 +573,7 @@ vp_status vp_expert_offsets(const int32_t* counts, int32_t n_ranks, int32_t E, i
  * bytes and at most 4 MiB, addresses 16-byte aligned, R < 2^31, L <= 4096, half
  * of a gated expert's weights below 1 GiB.
  * Offsets that decrease or leave [0, R] set VP_ERR_INVALID_ARGUMENT in
- * dev_status. */
+ * dev_status, and no product writes anything. */
 vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const void* w, const int64_t* offsets,
                            int64_t R, int32_t L, int32_t N, int32_t K, int32_t gated, void* y, int64_t y_stride,
                            void* pre, int64_t pre_stride, int32_t* dev_status, void* stream);

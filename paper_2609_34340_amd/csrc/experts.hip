@@ -71,16 +71,14 @@ __device__ inline int64_t offset_at(const ProductArgs& a, int e) {
   return ((const __attribute__((address_space(4))) int64_t*)a.offsets)[e];
 }
 
-struct Group { int e; int64_t lo, hi; };   // an expert and its rows, inside the buffer
+struct Group { int e; int64_t lo, hi; };   // an expert and its rows
 
-__device__ inline void clamp(const ProductArgs& a, Group& g) {
-  g.lo = g.lo < 0 ? 0 : g.lo > a.R ? a.R : g.lo;
-  g.hi = g.hi < g.lo ? g.lo : g.hi > a.R ? a.R : g.hi;
-}
-__device__ inline Group group_of(const ProductArgs& a, int e) {
-  Group g{e, offset_at(a, e), offset_at(a, e + 1)};
-  clamp(a, g);
-  return g;
+__device__ inline Group group_of(const ProductArgs& a, int e) { return {e, offset_at(a, e), offset_at(a, e + 1)}; }
+
+// Offsets that decrease or leave the buffer are the caller's error.
+template <typename Args> __device__ inline bool in_order(const Args& a, int e) {
+  const int64_t lo = a.offsets[e], hi = a.offsets[e + 1];
+  return lo >= 0 && lo <= hi && hi <= a.R;
 }
 
 // Row tiles of BM rows, expert after expert.  Lane l of every wavefront holds
@@ -89,16 +87,20 @@ template <int BM> struct RowTiles {
   int run;         // experts of a lane
   int64_t first;   // this lane's first tile
   int64_t total;
-  bool in_order;   // false: more tiles than offsets in order can have
 
   __device__ static int64_t of(const Group& g) { return (g.hi - g.lo + BM - 1) / BM; }
-  __device__ void init(const ProductArgs& a, int lane) {
+  // False, and no tiles, for offsets out of order: every wavefront finds the same.
+  __device__ bool init(const ProductArgs& a, int lane) {
     run = (a.L + 63) / 64;
     int64_t sum = 0;
+    bool good = true;
     for (int e = lane * run; e < min((lane + 1) * run, a.L); ++e) {
-      Group g{e, a.offsets[e], a.offsets[e + 1]};
-      clamp(a, g);
-      sum += of(g);
+      if (in_order(a, e)) sum += of(Group{e, a.offsets[e], a.offsets[e + 1]});
+      else good = false;
+    }
+    if (!__all(good)) {
+      first = total = 0;
+      return false;
     }
     int64_t incl = sum;
 #pragma unroll
@@ -110,9 +112,7 @@ template <int BM> struct RowTiles {
     total = __shfl(incl, 63);
     total = (int64_t)((uint64_t)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32 |
                       (uint32_t)__builtin_amdgcn_readfirstlane((int)total));
-    // others (an error, reported) get no work, instead of any amount
-    in_order = total <= a.R / BM + a.L;
-    if (!in_order) total = 0;
+    return true;
   }
   // The expert of tile `t` (below the total) and the first row of the tile.
   __device__ Group find(const ProductArgs& a, int64_t t, int64_t* m0) const {
@@ -137,7 +137,6 @@ __device__ inline int nth_largest(const ProductArgs& a, int n, int lane) {
   if (lane < a.L) {
     g.lo = a.offsets[lane];
     g.hi = a.offsets[lane + 1];
-    clamp(a, g);
   }
   const int rows = (int)(g.hi - g.lo);
   int before = 0;
@@ -146,15 +145,6 @@ __device__ inline int nth_largest(const ProductArgs& a, int n, int lane) {
     before += other > rows || (other == rows && e < lane);
   }
   return __builtin_ctzll(__ballot(lane < a.L && before == n));
-}
-
-// Offsets that decrease or pass the buffer are the caller's error; products
-// stay inside the buffers all the same.
-template <typename Args> __device__ inline void check_offsets(const Args& a) {
-  for (int e = threadIdx.x; e < a.L; e += blockDim.x) {
-    const int64_t lo = a.offsets[e], hi = a.offsets[e + 1];
-    if (lo < 0 || hi < lo || hi > a.R) report(a.status, VP_ERR_INVALID_ARGUMENT);
-  }
 }
 
 __device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -308,7 +298,6 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   const int wm = wave / WN, wn = wave % WN;
   const int half = a.half;
   const int row_bytes = kMx ? a.C / 2 : a.C * 2;
-  if (blockIdx.x == 0) check_offsets(a);
 
   // Tiles: XCD x (block % 8) takes a contiguous eighth of them (of every
   // expert's, for grad w), in bands of four row tiles by all columns: what 32
@@ -318,12 +307,11 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
   constexpr int kBand = 4;
   const int nt = (a.N + kTileN - 1) / kTileN, mt = MODE == kGradW ? (a.M + BM - 1) / BM : 0;
   RowTiles<BM> row_tiles;
-  row_tiles.init(a, lane);
-  int64_t slots = row_tiles.total;   // row tiles
-  if (MODE == kGradW) {
-    if (!row_tiles.in_order) return;
-    slots = mt;
+  if (!row_tiles.init(a, lane)) {   // an error: nothing is written
+    if (blockIdx.x == 0 && threadIdx.x == 0) report(a.status, VP_ERR_INVALID_ARGUMENT);
+    return;
   }
+  const int64_t slots = MODE == kGradW ? mt : row_tiles.total;   // row tiles
   const uint32_t all = (uint32_t)(slots * nt), per = (all + 7) / 8;   // tiles, below 2^31; this XCD's
   const uint32_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW ? per * a.L : per;
   const auto tile_at = [&](uint32_t idx, TileAt& t) -> bool {
@@ -825,9 +813,11 @@ __device__ inline void few_rows(const ProductArgs& a, const Group& g, int64_t m0
 
 template <typename T, bool GATED> __global__ void __launch_bounds__(256) product_few(ProductArgs a) {
   __shared__ float sums[4 * 2 * (kFewRows / 16) * 64 * 4];
-  if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets(a);
   RowTiles<kFewRows> tiles;
-  tiles.init(a, threadIdx.x % 64);
+  if (!tiles.init(a, threadIdx.x % 64)) {   // an error: nothing is written
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) report(a.status, VP_ERR_INVALID_ARGUMENT);
+    return;
+  }
   if (blockIdx.y >= tiles.total) return;
   int64_t m0;
   const Group g = tiles.find(a, blockIdx.y, &m0);
@@ -855,7 +845,10 @@ struct GateArgs {
 template <typename T>
 __global__ void __launch_bounds__(256) gate_grad_kernel(GateArgs a) {
   const int64_t m = block_index(), first = a.offsets[0], last = a.offsets[a.L];
-  if (m == 0) check_offsets(a);
+  if (m == 0) {
+    for (int e = threadIdx.x; e < a.L; e += blockDim.x)
+      if (!in_order(a, e)) report(a.status, VP_ERR_INVALID_ARGUMENT);
+  }
   if (first < 0 || last > a.R || m < first || m >= last) return;
   for (int c = threadIdx.x; c < a.half / 8; c += 256) {
     float dh[8], g[8], u[8];

@@ -164,6 +164,31 @@ def test_the_gates_gradient_reports_offsets_out_of_order(vp):
         assert vp.read_status(st) == vp.INVALID_ARGUMENT, bad
 
 
+def test_products_of_offsets_out_of_order_write_nothing(vp):
+    for R, N, K, L in ((20, 32, 64, 2), (2304, 2064, 264, 2), (8205, 2064, 64, 2)):
+        x, w = normal((R, K), 222, torch.bfloat16).cuda(), normal((L, N, K), 223, torch.bfloat16).cuda()
+        dy = normal((R, N), 224, torch.bfloat16).cuda()
+        xq = wq = None
+        if K % 32 == 0:
+            xq, wq = vp.mx_quantize(x), vp.mx_quantize(w)
+        for bad in BAD_OFFSETS + [[0, R, 0], [R, 0, R], [0, R + 1, R + 1], [1, 0, R]]:
+            off = torch.tensor(bad).cuda()
+            if all(0 <= a <= b <= R for a, b in zip(bad, bad[1:])):
+                continue
+            calls = [
+                ((R, N), torch.bfloat16, lambda o, st: vp.expert_matmul(x, w, off, out=o, status=st)),
+                ((R, N // 2), torch.bfloat16, lambda o, st: vp.expert_matmul(x, w, off, gated=True, out=o, status=st)),
+                ((R, K), torch.bfloat16, lambda o, st: vp.expert_matmul_grad_x(dy, w, off, out=o, status=st)),
+                ((L, N, K), torch.float32, lambda o, st: vp.expert_matmul_grad_w(dy, x, off, out=o, status=st))]
+            if xq is not None:
+                calls.append(((R, N), torch.bfloat16, lambda o, st: vp.expert_matmul_mx(xq, wq, off, K, out=o, status=st)))
+            for shape, dtype, call in calls:
+                st, out = vp.new_status(), torch.full(shape, 7.0, dtype=dtype, device="cuda")
+                call(out, st)
+                assert vp.read_status(st) == vp.INVALID_ARGUMENT, bad
+                assert (out == 7.0).all(), bad
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture
