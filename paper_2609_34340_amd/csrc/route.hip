@@ -95,21 +95,24 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteArgs a) {
   uint32_t key[V];
   const bool by_logit = !a.bias && a.n_groups == 1;
   // A NaN is in every score of its row (an infinity too), and so in the weights.  The choice is made by the scores of
-  // the numbers: NaN left out, infinity their limit.
+  // the numbers: NaN left out, infinity their limit.  (From the row again: in registers, another pass over them would
+  // cost the 4,096-expert kernel a wavefront per SIMD.)
   float key_inv = inv;
-  const bool odd = !a.sigmoid && !by_logit && !(inv == inv);
-  if (odd) {   // the same in all lanes of the token
+  if (!a.sigmoid && !by_logit && !(inv == inv)) {   // the same in all lanes of the token
     float sum = 0.0f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum += x[v] == -INFINITY || !(x[v] == x[v]) ? 0.0f : x[v] == top ? 1.0f : expf(x[v] - top);
+    for (int e = sub; e < E; e += LPT) {
+      const float z = to_f32(row[e]);
+      sum += z == -INFINITY || !(z == z) ? 0.0f : z == top ? 1.0f : expf(z - top);
+    }
     key_inv = 1.0f / across<LPT>(sum, [](float p, float q) { return p + q; });
   }
+  const auto key_score = [&](float z) { return a.sigmoid ? sigmoid(z) : (z == top ? 1.0f : expf(z - top)) * key_inv; };
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int e = expert_of<LPT>(v, sub);
     float s = x[v];
     if (!by_logit) {
-      s = odd && s == s && s != -INFINITY ? (s == top ? 1.0f : expf(s - top)) * key_inv : score(s);
+      s = key_score(s);
       if (a.bias && e < E) s += a.bias[e];
     }
     key[v] = e >= E ? kTaken : (x[v] == -INFINITY || !(s == s)) ? kMasked : ordered(s);
