@@ -508,8 +508,13 @@ vp_status vp_unpack_combine(const void* recv, int64_t recv_capacity, int64_t row
 /* ------------------------------------------------- layer: routing, experts
  *
  * What stands before, between and after the two exchanges of a
- * mixture-of-experts layer.  In these calls dev_status may be NULL: device
- * errors then stay unreported.  Element types: */
+ * mixture-of-experts layer.  In these calls dev_status may be NULL: the first
+ * device error of such calls is kept by the library, a word on each device,
+ * until vp_take_status moves it into dev_status (as any error: the first wins;
+ * of the calls before it on the stream and those that have ended on others). */
+vp_status vp_take_status(int32_t* dev_status, void* stream);
+
+/* Element types: */
 typedef enum { VP_F32 = 0, VP_BF16 = 1, VP_F16 = 2 } vp_dtype;
 
 enum { VP_SCORE_SOFTMAX = 0, VP_SCORE_SIGMOID = 1 };

@@ -751,4 +751,4 @@ class Pipeline:
 from . import layer  # noqa: E402
 from .layer import (expert_gate_grad, expert_kernel, expert_matmul, expert_matmul_grad_w,  # noqa: E402,F401
                     expert_matmul_grad_x, expert_matmul_mx, expert_offsets, merge, merge_grad, mx_dequantize,
-                    mx_quantize, mx_row_bytes, route, route_grad, route_lanes)
+                    mx_quantize, mx_row_bytes, route, route_grad, route_lanes, unclaimed_status)

@@ -249,6 +249,12 @@ vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq,
   return vp::launch_expert_product(a, stream);
 }
 
+vp_status vp_take_status(int32_t* dev_status, void* stream) {
+  if (!dev_status) return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
+  const vp_status st = vp::take_unclaimed_route(dev_status, stream);
+  return st != VP_OK ? st : vp::take_unclaimed_experts(dev_status, stream);
+}
+
 int32_t vp_expert_kernel(int32_t direction, int32_t mx, int32_t gated, int64_t R, int32_t L, int32_t N, int32_t K) {
   static const int64_t some_offsets = 0;   // only for the check
   if (direction < 0 || direction > 2 || (mx != 0 && mx != 1) || (gated != 0 && gated != 1)) return -1;

@@ -35,6 +35,7 @@
 
 #include "internal.h"
 #include "numeric.h"
+#include "report.h"
 
 namespace vp {
 namespace {
@@ -44,11 +45,6 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// A caller without a status does not learn of device errors.
-__device__ inline void report(int32_t* status, int code) {
-  if (status) atomicCAS(status, 0, code);
-}
 
 enum { kForward = 0, kGradX = 1, kGradW = 2 };
 
@@ -1006,6 +1002,12 @@ vp_status launch_expert_gate_grad(const void* dh, int64_t dh_stride, const void*
     else hipLaunchKernelGGL(gate_grad_kernel<F16>, grid_of(R), dim3(256), 0, (hipStream_t)stream, a);
   }
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "gate gradient launch failed");
+  return VP_OK;
+}
+
+vp_status take_unclaimed_experts(int32_t* out, void* stream) {
+  hipLaunchKernelGGL(take_unclaimed_kernel, dim3(1), dim3(1), 0, (hipStream_t)stream, out);
+  if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "status launch failed");
   return VP_OK;
 }
 

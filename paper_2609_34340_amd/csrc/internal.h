@@ -203,6 +203,9 @@ int32_t route_lanes(int64_t T, int32_t E);
 vp_status launch_route_grad(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t stride,
                             const vp_route_params& p, const int32_t* ids, const float* weights,
                             const float* d_weights, void* d_logits, int32_t* status, void* stream);
+// Moves the first error of this source's calls without a status into `out`.
+vp_status take_unclaimed_route(int32_t* out, void* stream);
+vp_status take_unclaimed_experts(int32_t* out, void* stream);
 vp_status launch_expert_offsets(const int32_t* counts, int32_t N, int32_t E, int32_t self, int64_t* offsets,
                                 int32_t* status, void* stream);
 enum { kExpertForward = 0, kExpertGradX = 1, kExpertGradW = 2 };

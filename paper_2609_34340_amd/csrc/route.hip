@@ -29,17 +29,13 @@
 
 #include "internal.h"
 #include "numeric.h"
+#include "report.h"
 
 namespace vp {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr uint32_t kTaken = 0, kMasked = 1;   // below the key of every number
-
-// A caller without a status does not learn of device errors.
-__device__ inline void report(int32_t* status, int code) {
-  if (status) atomicCAS(status, 0, code);
-}
 
 __device__ inline uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);   // -0 counts as +0
@@ -362,6 +358,12 @@ vp_status launch_expert_offsets(const int32_t* counts, int32_t N, int32_t E, int
   hipLaunchKernelGGL(offsets_kernel, dim3(1), dim3(kOffsetThreads), (size_t)(E / N) * 8, (hipStream_t)stream, counts,
                      N, E, self, offsets, status);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "offsets launch failed");
+  return VP_OK;
+}
+
+vp_status take_unclaimed_route(int32_t* out, void* stream) {
+  hipLaunchKernelGGL(take_unclaimed_kernel, dim3(1), dim3(1), 0, (hipStream_t)stream, out);
+  if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "status launch failed");
   return VP_OK;
 }
 

@@ -6,7 +6,8 @@ these names too.
 Matrices may have strided rows (the receive slots' 128-byte stride), their
 elements must be neighbours.  Every call enqueues on `stream` (the current one
 by default) and returns; outputs may be given to reuse buffers.  Errors that
-only the device can see go to `status` (new_status()) where one is given.
+only the device can see go to `status` (new_status()) where one is given, else
+the first of them is kept until unclaimed_status() asks.
 """
 from __future__ import annotations
 
@@ -17,7 +18,7 @@ from typing import Optional
 
 import torch
 
-from . import _check, _from, _ptr, _stream, lib
+from . import _check, _from, _ptr, _stream, lib, new_status, read_status
 
 SCORES = {"softmax": 0, "sigmoid": 1}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -47,6 +48,7 @@ def declare(L) -> None:
     L.vp_mx_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp]
     L.vp_mx_dequantize.argtypes = [vp, i64, i64, i64, vp, i32, i64, vp]
     L.vp_expert_matmul_mx.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, vp, i32, i64, vp, vp]
+    L.vp_take_status.argtypes = [vp, vp]
     L.vp_expert_kernel.argtypes = [i32, i32, i32, i64, i32, i32, i32]
     L.vp_route_lanes.argtypes = [i64, i32]
 
@@ -93,6 +95,14 @@ def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
     for t in others:
         if t is not None and t.get_device() != device:
             raise ValueError("all tensors must be on one device")
+
+
+def unclaimed_status(stream=None) -> int:
+    """vp_take_status: the first device error of this module's calls that were given no status since this was last asked,
+    0 if there was none.  Waits for the stream."""
+    status = _from(stream, new_status)
+    _check(lib().vp_take_status(_ptr(status), _stream(stream)), "vp_take_status")
+    return _from(stream, read_status, status)
 
 
 # --------------------------------------------------------------- routing

@@ -189,6 +189,30 @@ def test_products_of_offsets_out_of_order_write_nothing(vp):
                 assert (out == 7.0).all(), bad
 
 
+def test_errors_without_a_status_are_kept(vp):
+    x, w = normal((20, 64), 225, torch.bfloat16).cuda(), normal((2, 32, 64), 226, torch.bfloat16).cuda()
+    dy, pre = normal((20, 32), 227, torch.bfloat16).cuda(), normal((20, 64), 228, torch.bfloat16).cuda()
+    off = torch.tensor([0, 15, 10]).cuda()
+    ids = torch.tensor([[0, 1, 8]], dtype=torch.int32).cuda()
+    one, counts = torch.ones(1, 3).cuda(), torch.full((2, 4), -1, dtype=torch.int32).cuda()
+    xq, wq = vp.mx_quantize(x), vp.mx_quantize(w)
+    vp.unclaimed_status()
+    assert vp.unclaimed_status() == 0
+    for call in (lambda: vp.expert_matmul(x, w, off), lambda: vp.expert_matmul_grad_x(dy, w, off),
+                 lambda: vp.expert_matmul_grad_w(dy, x, off), lambda: vp.expert_gate_grad(dy, pre, off),
+                 lambda: vp.expert_matmul_mx(xq, wq, off, 64), lambda: vp.expert_offsets(counts, 0),
+                 lambda: vp.route_grad(torch.zeros(1, 8).cuda(), ids, one, one)):
+        call()
+        assert vp.unclaimed_status() == vp.INVALID_ARGUMENT
+        assert vp.unclaimed_status() == 0   # taken
+    st = vp.new_status()
+    vp.expert_matmul(x, w, off, status=st)
+    assert vp.unclaimed_status() == 0 and vp.read_status(st) == vp.INVALID_ARGUMENT
+    with torch.cuda.stream(torch.cuda.Stream()):
+        vp.expert_matmul(x, w, off)
+        assert vp.unclaimed_status() == vp.INVALID_ARGUMENT
+
+
 # ------------------------------------- more than 2^32 threads, wide strides
 
 @pytest.fixture

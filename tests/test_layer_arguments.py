@@ -49,3 +49,7 @@ def test_route_parameters_past_32_bits_are_refused(vp):
         how = {**dict(score="softmax", k=4, n_groups=1, top_groups=1, group_top=1, renorm=True, scale=1.0), **bad}
         with pytest.raises(ValueError):
             _route_params(**how)
+
+
+def test_taking_a_status_needs_a_place(vp):
+    assert vp.lib().vp_take_status(None, None) == vp.INVALID_ARGUMENT
