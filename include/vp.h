@@ -574,9 +574,9 @@ vp_status vp_expert_offsets(const int32_t* counts, int32_t n_ranks, int32_t E, i
  *           with G the first and U the second N/2 rows of W_e
  *   pre     gated: device [R, N], x G^T and x U^T (rounded), or NULL
  * Sums are in 32 bits and rounded once.  Rows outside the experts' are neither
- * read nor written.  K and N are multiples of 8 (gated: N of 16), strides of 16
- * bytes and at most 4 MiB, addresses 16-byte aligned, R < 2^31, L <= 4096, half
- * of a gated expert's weights below 1 GiB.
+ * read nor written.  K and N are multiples of 8 (gated: N of 16) up to 2^20,
+ * strides of 16 bytes and at most 4 MiB, addresses 16-byte aligned, R < 2^31, L
+ * <= 4096, half of a gated expert's weights below 1 GiB.
  * Offsets that decrease or leave [0, R] set VP_ERR_INVALID_ARGUMENT in
  * dev_status, and no product writes anything. */
 vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const void* w, const int64_t* offsets,
@@ -596,7 +596,8 @@ vp_status vp_expert_matmul_grad_w(const void* dy, int64_t dy_stride, const void*
 
 /* Gradient of the gated product by x G^T and x U^T: dh device [R, I], pre as
  * vp_expert_matmul left it (I = N/2), dpre device [R, 2 I]; the products'
- * gradients then follow from dpre.  Offsets as in vp_expert_matmul. */
+ * gradients then follow from dpre.  Sizes and offsets as in vp_expert_matmul,
+ * strides without an upper limit; offsets out of order are reported. */
 vp_status vp_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre, int64_t pre_stride, int32_t dtype,
                               const int64_t* offsets, int64_t R, int32_t L, int32_t I, void* dpre,
                               int64_t dpre_stride, int32_t* dev_status, void* stream);
@@ -608,8 +609,8 @@ vp_status vp_expert_gate_grad(const void* dh, int64_t dh_stride, const void* pre
  *   residual, out  device [T, H] of the same type; residual may be NULL, or
  *           out itself
  * A slot of weight 0 adds nothing whatever its row holds.  Sums are in 32
- * bits, in slot order.  H elements fill whole 16-byte vectors; strides are
- * multiples of 16 bytes, addresses 16-byte aligned; k <= 255, T < 2^31. */
+ * bits, in slot order.  H <= 2^20 elements fill whole 16-byte vectors; strides
+ * are multiples of 16 bytes, addresses 16-byte aligned; k <= 255, T < 2^31. */
 vp_status vp_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, int64_t H, int64_t row_stride,
                    const float* weights, const void* residual, int64_t residual_stride, void* out, int64_t out_stride,
                    void* stream);
@@ -633,8 +634,8 @@ int64_t vp_mx_row_bytes(int64_t K);
  * q_stride bytes apart.  A block's power of two is that of its largest
  * magnitude over 4 (never below 2^-127); values are rounded to nearest, ties
  * to the even code, and end at 6 times that power.  A block with an infinity
- * or NaN gets exponent 255 and reads back as NaN.  Strides are multiples of
- * 16 bytes, addresses 16-byte aligned. */
+ * or NaN gets exponent 255 and reads back as NaN.  K <= 2^20, rows < 2^31;
+ * strides are multiples of 16 bytes, addresses 16-byte aligned. */
 vp_status vp_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t K, int64_t x_stride, void* q,
                          int64_t q_stride, void* stream);
 vp_status vp_mx_dequantize(const void* q, int64_t rows, int64_t K, int64_t q_stride, void* out, int32_t dtype,

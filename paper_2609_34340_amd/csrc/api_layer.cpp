@@ -57,11 +57,18 @@ vp_status check_gated(int32_t gated, int32_t N, int64_t row_bytes) {
   return VP_OK;
 }
 
-// One operand of a product: `width` bytes of each row.
+// `width` bytes of each row, moved in 16-byte vectors.
 vp_status check_rows(const void* p, int64_t width, int64_t stride, int64_t R, const char* name) {
   if (R > 0 && !p) return set_error(VP_ERR_INVALID_ARGUMENT, std::string("null ") + name);
   if (!vector_rows(p, width, stride))
     return set_error(VP_ERR_INVALID_ARGUMENT, std::string(name) + ": rows must be 16-byte vectors, aligned, within the stride");
+  return VP_OK;
+}
+
+// Of a product, whose tiles address their rows by 32-bit offsets.
+vp_status check_operand(const void* p, int64_t width, int64_t stride, int64_t R, const char* name) {
+  const vp_status st = check_rows(p, width, stride, R, name);
+  if (st != VP_OK) return st;
   if (stride > kMaxStride) return set_error(VP_ERR_UNSUPPORTED, std::string(name) + ": stride above 4 MiB");
   return VP_OK;
 }
@@ -107,10 +114,10 @@ vp_status vp_expert_matmul(const void* x, int64_t x_stride, int32_t dtype, const
   if (st != VP_OK) return st;
   if ((st = check_gated(gated, N, (int64_t)K * 2)) != VP_OK) return st;
   if (!gated && pre) return set_error(VP_ERR_INVALID_ARGUMENT, "pre belongs to a gated product");
-  if ((st = check_rows(x, (int64_t)K * 2, x_stride, R, "x")) != VP_OK) return st;
-  if ((st = check_rows(w, (int64_t)K * 2, (int64_t)K * 2, 1, "w")) != VP_OK) return st;
-  if ((st = check_rows(y, (int64_t)(gated ? N / 2 : N) * 2, y_stride, R, "y")) != VP_OK) return st;
-  if (pre && (st = check_rows(pre, (int64_t)N * 2, pre_stride, R, "pre")) != VP_OK) return st;
+  if ((st = check_operand(x, (int64_t)K * 2, x_stride, R, "x")) != VP_OK) return st;
+  if ((st = check_operand(w, (int64_t)K * 2, (int64_t)K * 2, 1, "w")) != VP_OK) return st;
+  if ((st = check_operand(y, (int64_t)(gated ? N / 2 : N) * 2, y_stride, R, "y")) != VP_OK) return st;
+  if (pre && (st = check_operand(pre, (int64_t)N * 2, pre_stride, R, "pre")) != VP_OK) return st;
   if (R == 0) return VP_OK;
   const vp::ExpertLaunch a{vp::kExpertForward, gated != 0, false, dtype, x, w, x_stride, (int64_t)K * 2, offsets, R, L,
                            N, K, y, pre, y_stride, pre_stride, dev_status};
@@ -122,9 +129,9 @@ vp_status vp_expert_matmul_grad_x(const void* dy, int64_t dy_stride, int32_t dty
                                   int64_t dx_stride, int32_t* dev_status, void* stream) {
   vp_status st = check_experts(dtype, offsets, R, L, N, K);
   if (st != VP_OK) return st;
-  if ((st = check_rows(dy, (int64_t)N * 2, dy_stride, R, "dy")) != VP_OK) return st;
-  if ((st = check_rows(w, (int64_t)K * 2, (int64_t)K * 2, 1, "w")) != VP_OK) return st;
-  if ((st = check_rows(dx, (int64_t)K * 2, dx_stride, R, "dx")) != VP_OK) return st;
+  if ((st = check_operand(dy, (int64_t)N * 2, dy_stride, R, "dy")) != VP_OK) return st;
+  if ((st = check_operand(w, (int64_t)K * 2, (int64_t)K * 2, 1, "w")) != VP_OK) return st;
+  if ((st = check_operand(dx, (int64_t)K * 2, dx_stride, R, "dx")) != VP_OK) return st;
   if (R == 0) return VP_OK;
   const vp::ExpertLaunch a{vp::kExpertGradX, false, false, dtype, dy, w, dy_stride, (int64_t)K * 2, offsets, R, L, N, K,
                            dx, nullptr, dx_stride, 0, dev_status};
@@ -136,9 +143,9 @@ vp_status vp_expert_matmul_grad_w(const void* dy, int64_t dy_stride, const void*
                                   int32_t* dev_status, void* stream) {
   vp_status st = check_experts(dtype, offsets, R, L, N, K);
   if (st != VP_OK) return st;
-  if ((st = check_rows(dy, (int64_t)N * 2, dy_stride, R, "dy")) != VP_OK) return st;
-  if ((st = check_rows(x, (int64_t)K * 2, x_stride, R, "x")) != VP_OK) return st;
-  if ((st = check_rows(dw, (int64_t)K * 4, (int64_t)K * 4, 1, "dw")) != VP_OK) return st;
+  if ((st = check_operand(dy, (int64_t)N * 2, dy_stride, R, "dy")) != VP_OK) return st;
+  if ((st = check_operand(x, (int64_t)K * 2, x_stride, R, "x")) != VP_OK) return st;
+  if ((st = check_operand(dw, (int64_t)K * 4, (int64_t)K * 4, 1, "dw")) != VP_OK) return st;
   const vp::ExpertLaunch a{vp::kExpertGradW, false, false, dtype, dy, x, dy_stride, x_stride, offsets, R, L, N, K, dw,
                            nullptr, (int64_t)K * 4, 0, dev_status};
   return vp::launch_expert_product(a, stream);
@@ -240,9 +247,9 @@ vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq,
   if (K % 32 != 0) return set_error(VP_ERR_UNSUPPORTED, "K must be a multiple of 32");
   const int64_t rb = vp::mx_row_bytes(K);
   if ((st = check_gated(gated, N, rb)) != VP_OK) return st;
-  if ((st = check_rows(xq, rb, xq_stride, R, "xq")) != VP_OK) return st;
-  if ((st = check_rows(wq, rb, rb, 1, "wq")) != VP_OK) return st;
-  if ((st = check_rows(y, (int64_t)(gated ? N / 2 : N) * 2, y_stride, R, "y")) != VP_OK) return st;
+  if ((st = check_operand(xq, rb, xq_stride, R, "xq")) != VP_OK) return st;
+  if ((st = check_operand(wq, rb, rb, 1, "wq")) != VP_OK) return st;
+  if ((st = check_operand(y, (int64_t)(gated ? N / 2 : N) * 2, y_stride, R, "y")) != VP_OK) return st;
   if (R == 0) return VP_OK;
   const vp::ExpertLaunch a{vp::kExpertForward, gated != 0, true, dtype, xq, wq, xq_stride, rb, offsets, R, L, N, K, y,
                            nullptr, y_stride, 0, dev_status};

@@ -281,3 +281,30 @@ def test_route_gradient_of_two_to_the_26_tokens(vp, room):
     at = ends(T)
     small = vp.route_grad(x[at], out["ids"][at], out["weights"][at], d[at], score="sigmoid", renorm=False)
     assert torch.equal(got[at], small) and ((got != 0).sum(1) == 1).all()
+
+
+def far_rows(n, m, dtype, seed):
+    """A matrix whose rows lie more than 4 MiB apart."""
+    wide = torch.full((n, (5 << 20) // dtype.itemsize), 255 if dtype == torch.uint8 else math.nan, dtype=dtype, device="cuda")
+    wide[:, :m] = normal((n, m), seed, dtype).cuda()
+    return wide[:, :m]
+
+
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_rows_more_than_4_mib_apart(vp, dtype):
+    rows, res, w = far_rows(6, 72, dtype, 240), far_rows(3, 72, dtype, 241), normal((3, 2), 242).cuda()
+    out = far_rows(3, 72, dtype, 243)
+    near_rows, near_res = rows.contiguous(), res.contiguous()
+    assert torch.equal(vp.merge(rows, w, residual=res, out=out), vp.merge(near_rows, w, residual=near_res))
+    g, gw = vp.merge_grad(res, rows, w, d_rows=far_rows(6, 72, dtype, 244))
+    g2, gw2 = vp.merge_grad(near_res, near_rows, w)
+    assert torch.equal(g, g2) and torch.equal(gw, gw2)
+    x = far_rows(4, 96, dtype, 245)
+    q = far_rows(4, vp.mx_row_bytes(96), torch.uint8, 246)
+    assert torch.equal(vp.mx_quantize(x, out=q), vp.mx_quantize(x.contiguous()))
+    back = vp.mx_dequantize(q, 96, out=far_rows(4, 96, dtype, 247))
+    assert torch.equal(back, vp.mx_dequantize(q.contiguous(), 96, dtype=dtype))
+    if dtype != torch.float32:
+        dh, pre, off = far_rows(4, 32, dtype, 248), far_rows(4, 64, dtype, 249), torch.tensor([0, 4]).cuda()
+        got = vp.expert_gate_grad(dh, pre, off, out=far_rows(4, 64, dtype, 250))
+        assert torch.equal(got, vp.expert_gate_grad(dh.contiguous(), pre.contiguous(), off))
