@@ -90,11 +90,16 @@ def _float_dtype(t: torch.Tensor, name: str, halves: bool = False) -> int:
     return code
 
 
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
+def _queue(stream, first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The handle of the stream a call runs on, once all of its tensors are known to be on that stream's device."""
     device = first.get_device()
     for t in others:
         if t is not None and t.get_device() != device:
             raise ValueError("all tensors must be on one device")
+    # kernels run on the current device, which need not reach another one's memory
+    if device != torch.cuda.current_device() or (stream is not None and stream.device_index != device):
+        raise ValueError("the tensors must be on the current device, and the stream too")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def unclaimed_status(stream=None) -> int:
@@ -137,10 +142,10 @@ def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optiona
                    weights=_from(stream, torch.empty, (T, k), dtype=torch.float32, device=logits.device))
     ids = _whole(out["ids"], torch.int32, (T, k), "ids")
     weights = _whole(out["weights"], torch.float32, (T, k), "weights")
-    _same_device(logits, bias, ids, weights)
+    queue = _queue(stream, logits, bias, ids, weights)
     p = _route_params(score, k, n_groups, top_groups, group_top, renorm, scale)
-    _check(lib().vp_route(_ptr(logits), dt, T, E, ld, p, _ptr(bias), _ptr(ids), _ptr(weights),
-                          _stream(stream)), "vp_route")
+    _check(lib().vp_route(_ptr(logits), dt, T, E, ld, p, _ptr(bias), _ptr(ids), _ptr(weights), queue),
+           "vp_route")
     return out
 
 
@@ -160,10 +165,10 @@ def route_grad(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, d
     if out is None:
         out = _from(stream, torch.empty, (T, E), dtype=logits.dtype, device=logits.device)
     _whole(out, logits.dtype, (T, E), "d_logits")
-    _same_device(logits, ids, weights, d_weights, out, status)
+    queue = _queue(stream, logits, ids, weights, d_weights, out, status)
     p = _route_params(score, k, 1, 1, 1, renorm, scale)
     _check(lib().vp_route_grad(_ptr(logits), dt, T, E, ld, p, _ptr(ids), _ptr(weights), _ptr(d_weights),
-                               _ptr(out), _ptr(status), _stream(stream)), "vp_route_grad")
+                               _ptr(out), _ptr(status), queue), "vp_route_grad")
     return out
 
 
@@ -180,8 +185,8 @@ def expert_offsets(counts: torch.Tensor, self_rank: int, out: Optional[torch.Ten
     if out is None:
         out = _from(stream, torch.empty, n_local + 1, dtype=torch.int64, device=counts.device)
     _whole(out, torch.int64, (n_local + 1,), "offsets")
-    _same_device(counts, out, status)
-    _check(lib().vp_expert_offsets(_ptr(counts), N, E, self_rank, _ptr(out), _ptr(status), _stream(stream)),
+    queue = _queue(stream, counts, out, status)
+    _check(lib().vp_expert_offsets(_ptr(counts), N, E, self_rank, _ptr(out), _ptr(status), queue),
            "vp_expert_offsets")
     return out
 
@@ -212,9 +217,9 @@ def expert_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, ga
         out = _from(stream, torch.empty, (R, width), dtype=x.dtype, device=x.device)
     ldy = _matrix(out, "out", cols=width, dtype=x.dtype, rows=R)
     ldp = 0 if pre is None else _matrix(pre, "pre", cols=N, dtype=x.dtype, rows=R)
-    _same_device(x, w, offsets, out, pre, status)
+    queue = _queue(stream, x, w, offsets, out, pre, status)
     _check(lib().vp_expert_matmul(_ptr(x), 2 * ldx, dt, _ptr(w), _ptr(offsets), R, L, N, K, int(gated), _ptr(out),
-                                  2 * ldy, _ptr(pre), 2 * ldp, _ptr(status), _stream(stream)), "vp_expert_matmul")
+                                  2 * ldy, _ptr(pre), 2 * ldp, _ptr(status), queue), "vp_expert_matmul")
     return out
 
 
@@ -230,9 +235,9 @@ def expert_matmul_grad_x(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tenso
     if out is None:
         out = _from(stream, torch.empty, (R, K), dtype=dy.dtype, device=dy.device)
     ldx = _matrix(out, "out", cols=K, dtype=dy.dtype, rows=R)
-    _same_device(dy, w, offsets, out, status)
+    queue = _queue(stream, dy, w, offsets, out, status)
     _check(lib().vp_expert_matmul_grad_x(_ptr(dy), 2 * ldy, dt, _ptr(w), _ptr(offsets), R, L, N, K, _ptr(out),
-                                         2 * ldx, _ptr(status), _stream(stream)), "vp_expert_matmul_grad_x")
+                                         2 * ldx, _ptr(status), queue), "vp_expert_matmul_grad_x")
     return out
 
 
@@ -251,9 +256,9 @@ def expert_matmul_grad_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tenso
     if out is None:
         out = _from(stream, torch.empty, (L, N, K), dtype=torch.float32, device=dy.device)
     _whole(out, torch.float32, (L, N, K), "out")
-    _same_device(dy, x, offsets, out, status)
+    queue = _queue(stream, dy, x, offsets, out, status)
     _check(lib().vp_expert_matmul_grad_w(_ptr(dy), 2 * ldy, _ptr(x), 2 * ldx, dt, _ptr(offsets), R, L, N, K,
-                                         _ptr(out), _ptr(status), _stream(stream)), "vp_expert_matmul_grad_w")
+                                         _ptr(out), _ptr(status), queue), "vp_expert_matmul_grad_w")
     return out
 
 
@@ -270,9 +275,9 @@ def expert_gate_grad(dh: torch.Tensor, pre: torch.Tensor, offsets: torch.Tensor,
     if out is None:
         out = _from(stream, torch.empty, (R, 2 * half), dtype=dh.dtype, device=dh.device)
     ldo = _matrix(out, "out", cols=2 * half, dtype=dh.dtype, rows=R)
-    _same_device(dh, pre, offsets, out, status)
+    queue = _queue(stream, dh, pre, offsets, out, status)
     _check(lib().vp_expert_gate_grad(_ptr(dh), 2 * ldh, _ptr(pre), 2 * ldp, dt, _ptr(offsets), R, L, half, _ptr(out),
-                                     2 * ldo, _ptr(status), _stream(stream)), "vp_expert_gate_grad")
+                                     2 * ldo, _ptr(status), queue), "vp_expert_gate_grad")
     return out
 
 
@@ -292,9 +297,9 @@ def merge(rows: torch.Tensor, weights: torch.Tensor, *, residual: Optional[torch
     if out is None:
         out = _from(stream, torch.empty, (T, H), dtype=rows.dtype, device=rows.device)
     ldo = _matrix(out, "out", cols=H, dtype=rows.dtype, rows=T)
-    _same_device(rows, weights, residual, out)
+    queue = _queue(stream, rows, weights, residual, out)
     _check(lib().vp_merge(_ptr(rows), dt, T, k, H, ldr * size, _ptr(weights), _ptr(residual), lds * size, _ptr(out),
-                          ldo * size, _stream(stream)), "vp_merge")
+                          ldo * size, queue), "vp_merge")
     return out
 
 
@@ -315,9 +320,9 @@ def merge_grad(d_out: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, *
         d_weights = _from(stream, torch.empty, (T, k), dtype=torch.float32, device=rows.device)
     ldo = _matrix(d_rows, "d_rows", cols=H, dtype=rows.dtype, rows=T * k)
     _whole(d_weights, torch.float32, (T, k), "d_weights")
-    _same_device(rows, d_out, weights, d_rows, d_weights)
+    queue = _queue(stream, rows, d_out, weights, d_rows, d_weights)
     _check(lib().vp_merge_grad(_ptr(d_out), dt, T, k, H, ldd * size, _ptr(rows), ldr * size, _ptr(weights),
-                               _ptr(d_rows), ldo * size, _ptr(d_weights), _stream(stream)), "vp_merge_grad")
+                               _ptr(d_rows), ldo * size, _ptr(d_weights), queue), "vp_merge_grad")
     return d_rows, d_weights
 
 
@@ -343,9 +348,9 @@ def mx_quantize(x: torch.Tensor, *, out: Optional[torch.Tensor] = None, stream=N
     if out.shape != (*x.shape[:-1], rb) or (out.dim() != 2 and not out.is_contiguous()):
         raise ValueError("out must be uint8 %s" % ((*x.shape[:-1], rb),))
     ldq = _matrix(out if out.dim() == 2 else out.view(-1, rb), "out", dtype=torch.uint8)
-    _same_device(x, out)
-    _check(lib().vp_mx_quantize(_ptr(x), dt, flat.shape[0], K, ldx * x.element_size(), _ptr(out), ldq,
-                                _stream(stream)), "vp_mx_quantize")
+    queue = _queue(stream, x, out)
+    _check(lib().vp_mx_quantize(_ptr(x), dt, flat.shape[0], K, ldx * x.element_size(), _ptr(out), ldq, queue),
+           "vp_mx_quantize")
     return out
 
 
@@ -358,8 +363,8 @@ def mx_dequantize(q: torch.Tensor, K: int, *, dtype=torch.bfloat16, out: Optiona
         out = _from(stream, torch.empty, (R, K), dtype=dtype, device=q.device)
     dt = _float_dtype(out, "out")
     ldo = _matrix(out, "out", cols=K, rows=R)
-    _same_device(q, out)
-    _check(lib().vp_mx_dequantize(_ptr(q), R, K, ldq, _ptr(out), dt, ldo * out.element_size(), _stream(stream)),
+    queue = _queue(stream, q, out)
+    _check(lib().vp_mx_dequantize(_ptr(q), R, K, ldq, _ptr(out), dt, ldo * out.element_size(), queue),
            "vp_mx_dequantize")
     return out
 
@@ -380,9 +385,9 @@ def expert_matmul_mx(xq: torch.Tensor, wq: torch.Tensor, offsets: torch.Tensor, 
         out = _from(stream, torch.empty, (R, width), dtype=dtype, device=xq.device)
     dt = _float_dtype(out, "out", halves=True)
     ldy = _matrix(out, "out", cols=width, rows=R)
-    _same_device(xq, wq, offsets, out, status)
+    queue = _queue(stream, xq, wq, offsets, out, status)
     _check(lib().vp_expert_matmul_mx(_ptr(xq), ldx, _ptr(wq), _ptr(offsets), R, L, N, K, int(gated), _ptr(out), dt,
-                                     2 * ldy, _ptr(status), _stream(stream)), "vp_expert_matmul_mx")
+                                     2 * ldy, _ptr(status), queue), "vp_expert_matmul_mx")
     return out
 
 

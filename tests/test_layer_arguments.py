@@ -53,3 +53,15 @@ def test_route_parameters_past_32_bits_are_refused(vp):
 
 def test_taking_a_status_needs_a_place(vp):
     assert vp.lib().vp_take_status(None, None) == vp.INVALID_ARGUMENT
+
+
+def test_tensors_of_another_device_are_refused(vp, monkeypatch):
+    from types import SimpleNamespace as Plain
+    from paper_2609_34340_amd.layer import _queue
+    on = lambda i: Plain(get_device=lambda: i)  # noqa: E731
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    here, there = Plain(device_index=0, cuda_stream=7), Plain(device_index=1, cuda_stream=8)
+    assert _queue(here, on(0), None, on(0)) == 7
+    for args in ((None, on(0), on(1)), (None, on(1), on(1)), (here, on(1)), (there, on(0)), (there, on(1)), (None, on(0), on(-1))):
+        with pytest.raises(ValueError):
+            _queue(*args)
