@@ -249,6 +249,10 @@ template <int ROWS, bool COLS, int WAVES> struct Operand {
   }
 };
 
+// Steps of a contraction over an expert's rows, of which a buffer may hold 2^31 - 1.
+constexpr __host__ __device__ int row_steps(int rows) { return rows / 64 + (rows % 64 != 0); }
+static_assert(row_steps(0) == 0 && row_steps(64) == 1 && row_steps(65) == 2 && row_steps(0x7fffffff) == 1 << 25, "whole steps");
+
 template <typename T> struct Mx { using out = T; };   // both operands in 4-bit blocks, results of type T
 template <typename T> struct Elem { using out = T; static constexpr bool mx = false; };
 template <typename T> struct Elem<Mx<T>> { using out = T; static constexpr bool mx = true; };
@@ -335,7 +339,7 @@ __global__ void __launch_bounds__(WM * WN * 64) product_tiled(ProductArgs a) {
       t.a_left = t.b_left = rows;
       t.a_width = (int)(a.M - m0) * 2;
       t.b_width = (a.N - n0) * 2;
-      t.steps = (rows + 63) / 64;   // an expert without rows: zeros
+      t.steps = row_steps(rows);   // an expert without rows: zeros
     } else {
       t.a = a.a + m0 * a.a_stride;
       t.a_left = (t.rows - 1) * (int)a.a_stride + row_bytes;
