@@ -134,6 +134,29 @@ def test_four_bit_blocks(vp, counts, N, K, kernel, gated, dtype):
         assert (out[cuts[-1]:] == 7.0).all() and (out[:, width:] == 7.0).all()
 
 
+@pytest.mark.parametrize("counts,N,K,kernel", [([1025, 0, 700, 3, 576], 2064, 264, "tiles_128"),
+                                               ([2560, 1, 0, 2303, 341], 2064, 328, "tiles_256")], ids=shape)
+def test_tiles_of_rows_4_mib_apart(vp, counts, N, K, kernel):
+    """The longest stride the products take: rows up to 9 and 20 GiB into the buffer."""
+    cuts, off, x, w = operands(counts, N, K, torch.bfloat16, 0, 145)
+    R, L = x.shape[0], len(counts)
+    assert vp.expert_kernel(R, L, N, K, gated=True) == vp.expert_kernel(R, L, N, K) == kernel
+    far = torch.empty((R, 1 << 21), dtype=torch.bfloat16, device="cuda")
+    far[:, :K], far[:, K:K + 8] = x.cuda(), math.nan
+    far[:, 4096:4096 + 2 * N] = 7.0
+    xs, ys, zs, w, st = far[:, :K], far[:, 4096:4096 + N], far[:, 4096 + N:4096 + 2 * N], w.cuda(), vp.new_status()
+    x = x.cuda()
+    assert torch.equal(vp.expert_matmul(xs, w, off, out=ys, status=st), vp.expert_matmul(x, w, off))
+    pre = torch.empty((R, N), dtype=torch.bfloat16, device="cuda")
+    y = vp.expert_matmul(xs, w, off, gated=True, out=ys[:, :N // 2], pre=zs, status=st)
+    assert torch.equal(y, vp.expert_matmul(x, w, off, gated=True, pre=pre)) and torch.equal(zs, pre)
+    assert torch.equal(vp.expert_matmul_grad_x(zs, w, off, out=far[:, 32768:32768 + K], status=st), vp.expert_matmul_grad_x(pre, w, off))
+    assert torch.equal(vp.expert_matmul_grad_w(zs, xs, off, status=st), vp.expert_matmul_grad_w(pre, x, off))
+    assert vp.read_status(st) == 0 and (far[:, 4096 + N // 2:4096 + N] == vp.expert_matmul(x, w, off)[:, N // 2:]).all()
+    del far, xs, ys, zs, y
+    torch.cuda.empty_cache()
+
+
 def test_a_graph_of_tiled_products_replays(vp):
     """Several tiles to a workgroup, replayed with other work between: the results of the eager call, bit for bit."""
     counts, N, K = [4097, 0, 255, 1, 3847], 2064, 56
