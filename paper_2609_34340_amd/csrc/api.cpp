@@ -366,6 +366,13 @@ size_t vp_pack_workspace(int32_t k_max, int64_t send_capacity, int64_t unit_byte
 
 namespace {
 
+// The copies of a pack's rows take a workgroup each, of tokens in whole eights.
+vp_status check_copies(int64_t T, int32_t k, int64_t row_bytes) {
+  if (T >= ((int64_t)1 << 32) || !vp::fits_launch((T + 7) / 8 * 8 * k, vp::row_threads(row_bytes / 16)))
+    return set_error(VP_ERR_UNSUPPORTED, "too many token copies");
+  return VP_OK;
+}
+
 vp_status pack_rows_stages(int stages, const void* tokens, int64_t T, int32_t k, int64_t row_bytes,
                            const int32_t* sorted_tok, const uint8_t* sorted_slot, const int64_t* dest_off,
                            int32_t self_rank,
@@ -384,6 +391,8 @@ vp_status pack_rows_stages(int stages, const void* tokens, int64_t T, int32_t k,
     return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
   if (ws_bytes < vp::pack_workspace(k_max, send_capacity, row_bytes, T, k) || !ws)
     return set_error(VP_ERR_INVALID_ARGUMENT, "workspace too small");
+  const vp_status st = stages & 2 ? check_copies(T, k, row_bytes) : VP_OK;
+  if (st != VP_OK) return st;
   vp::PackLaunch a{0, stages, tokens, T, k, row_bytes, row_bytes, sorted_tok, sorted_slot, dest_off, nullptr,
                    self_rank, n_ranks,
                    K, dst, bytes, send_off, stream_off, k_max, send, send_capacity, step_off, dev_status, ws,
@@ -471,6 +480,8 @@ vp_status vp_pack_gather(const void* src, int64_t unit_bytes, int64_t T, int32_t
     return set_error(VP_ERR_INVALID_ARGUMENT, "null pointer");
   if (ws_bytes < vp::pack_workspace(k_max, send_capacity, unit_bytes, T, k) || !ws)
     return set_error(VP_ERR_INVALID_ARGUMENT, "workspace too small");
+  const vp_status st = k > 0 ? check_copies(T, k, unit_bytes) : VP_OK;
+  if (st != VP_OK) return st;
   vp::PackLaunch a{k > 0 ? 0 : 1, 2, src, T, k, unit_bytes, unit_bytes, nullptr, nullptr, nullptr, nullptr, 0, 1,
                    K, nullptr, nullptr, nullptr, nullptr, k_max, send, send_capacity,
                    const_cast<int64_t*>(step_off), dev_status, ws, ws_bytes};

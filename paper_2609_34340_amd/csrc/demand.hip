@@ -662,7 +662,7 @@ vp_status launch_demand(const DemandLaunch& a, void* stream) {
     return VP_OK;
   }
   const int64_t blocks1 = (int64_t)a.R * w.P + (sorting ? w.nch : 0);
-  if (blocks1 >= ((int64_t)1 << 31)) return set_error(VP_ERR_UNSUPPORTED, "too many histogram parts");
+  if (!fits_launch(blocks1, kThreads)) return set_error(VP_ERR_UNSUPPORTED, "too many histogram parts");
   hipLaunchKernelGGL(demand_count, dim3((unsigned)blocks1), dim3(kThreads), (size_t)kWaves * a.E * sizeof(int32_t),
                      s, d);
   if (d.scanned)

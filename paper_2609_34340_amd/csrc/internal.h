@@ -190,6 +190,11 @@ struct UnpackLaunch {
 };
 int64_t slot_bytes(int64_t row_bytes);
 size_t unpack_workspace(int64_t rows);
+// Threads that copy a row of `vecs` 16-byte vectors in the packs and unpacks, about 2 KiB to a wavefront: rows up to 2, 4
+// and 8 KiB take 1, 2 and 4 wavefronts of two vectors per thread, longer rows 8 of one.
+inline int row_threads(int64_t vecs) { return vecs <= 128 ? 64 : vecs <= 256 ? 128 : vecs <= 512 ? 256 : 512; }
+// A dimension of a grid holds fewer than 2^32 threads; a launch of more runs some of them and returns no error.
+inline bool fits_launch(int64_t blocks, int threads) { return blocks < ((int64_t)1 << 32) / threads; }
 size_t unpack_lds_bytes(int mode, int32_t N, int32_t eloc);
 vp_status launch_unpack(const UnpackLaunch& a, void* stream);
 vp_status launch_transpose(const int64_t* D, int32_t N, int64_t* DT, void* stream);

@@ -341,6 +341,8 @@ size_t unpack_lds_bytes(int mode, int32_t N, int32_t eloc) {
 
 vp_status launch_unpack(const UnpackLaunch& a, void* stream) {
   hipStream_t s = (hipStream_t)stream;
+  const int threads = row_threads(a.row_bytes / 16);
+  if (!fits_launch((a.rows_cap + 7) / 8 * 8, threads)) return set_error(VP_ERR_UNSUPPORTED, "too many buffer rows");
   const int eloc = a.E / a.N;
   const size_t lds = unpack_lds_bytes(a.mode, a.N, eloc);
   if (lds > 64 * 1024) return set_error(VP_ERR_UNSUPPORTED, "too many ranks or local experts for the row map");
@@ -352,21 +354,18 @@ vp_status launch_unpack(const UnpackLaunch& a, void* stream) {
             map, total, a.status};
   hipLaunchKernelGGL(map_kernel, dim3(a.k_max), dim3(kMapThreads), lds, s, m);
   if (a.rows_cap > 0) {
-    if (a.rows_cap >= ((int64_t)1 << 31) - 8) return set_error(VP_ERR_UNSUPPORTED, "too many buffer rows");
     const int64_t vpr = a.row_bytes / 16;
     const dim3 grid((unsigned)((a.rows_cap + 7) / 8 * 8));   // rows past the buffer's count exit at once
     const unsigned char* sp = (const unsigned char*)a.src;
     unsigned char* dp = (unsigned char*)a.dst_buf;
     const int ms = a.mode == kModeCombinePack ? 1 : 0;
-    // about 2 KiB per wavefront: rows up to 2, 4 and 8 KiB take 1, 2 and 4
-    // wavefronts of two vectors per thread, longer rows 8 wavefronts of one
-    if (vpr <= 128)
+    if (threads == 64)
       hipLaunchKernelGGL((copy_rows_kernel<64, 2>), grid, dim3(64), 0, s, sp, a.src_stride, dp, a.dst_stride, vpr,
                          map, ms, total, a.rows_cap, a.status);
-    else if (vpr <= 256)
+    else if (threads == 128)
       hipLaunchKernelGGL((copy_rows_kernel<128, 2>), grid, dim3(128), 0, s, sp, a.src_stride, dp, a.dst_stride, vpr,
                          map, ms, total, a.rows_cap, a.status);
-    else if (vpr <= 512)
+    else if (threads == 256)
       hipLaunchKernelGGL((copy_rows_kernel<256, 2>), grid, dim3(256), 0, s, sp, a.src_stride, dp, a.dst_stride, vpr,
                          map, ms, total, a.rows_cap, a.status);
     else
