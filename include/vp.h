@@ -469,13 +469,12 @@ vp_status vp_demand_transpose(const int64_t* demand, int32_t n_ranks, int64_t* d
  *                                      1, ..., each in token order; the slots
  *                                      of this rank's own rows (never sent)
  *                                      are left untouched
- * row_bytes must be a multiple of 16, and the buffer's rows, in whole eights,
- * below 2^26 for rows up to 2 KiB, 2^25 up to 4, 2^24 up to 8 and 2^23 for
- * longer ones (VP_ERR_UNSUPPORTED; also in the combine's calls); the schedule
- * must deliver every source's stream to this rank whole (the rows of its
- * assignments to this rank's experts), else VP_ERR_INVALID_ARGUMENT.  A
- * receive buffer or output too small sets VP_ERR_CAPACITY.  On a device error
- * nothing is copied.  Calls that share a workspace must not overlap. */
+ * row_bytes must be a multiple of 16, and the buffer's rows below 2^31 (also in
+ * the combine's calls); the schedule must deliver every source's stream to this
+ * rank whole (the rows of its assignments to this rank's experts), else
+ * VP_ERR_INVALID_ARGUMENT.  A receive buffer or output too small sets
+ * VP_ERR_CAPACITY.  On a device error nothing is copied.  Calls that share a
+ * workspace must not overlap. */
 vp_status vp_unpack_rows(const void* recv, int64_t recv_capacity, int64_t row_bytes, const int32_t* counts,
                          int32_t E, int32_t self_rank, int32_t n_ranks, const int32_t* K, const int32_t* dst,
                          const int64_t* bytes, const int32_t* recv_src, int32_t k_max, void* out,

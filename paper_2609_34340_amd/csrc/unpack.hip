@@ -288,24 +288,25 @@ __global__ void __launch_bounds__(TH) copy_rows_kernel(const unsigned char* __re
   U = U < rows_cap ? U : rows_cap;
   // XCD x (block % 8) copies the x-th eighth of the buffer's rows, in order
   // (measured 4-6 % faster than rows dealt to the XCDs in turn); the grid
-  // covers rows_cap rounded up to eight, and blocks past the rows exit
+  // covers rows_cap rounded up to eight, and blocks past the rows exit (of more
+  // rows than blocks, a block takes several)
   const int64_t per = (U + 7) / 8;
-  const int64_t j = blockIdx.x >> 3;
-  if (j >= per) return;
-  const int64_t g = (int64_t)(blockIdx.x & 7) * per + j;
-  if (g >= U) return;
-  const int64_t m = map[g];
-  const int64_t sr = map_src ? m : g, dr = map_src ? g : m;
-  const u32x4* s = (const u32x4*)(src + sr * src_stride);
-  u32x4* d = (u32x4*)(dst + dr * dst_stride);
-  for (int64_t e0 = threadIdx.x; e0 < vpr; e0 += (int64_t)V * TH) {
-    u32x4 r[V];
+  for (int64_t j = blockIdx.x >> 3; j < per; j += gridDim.x >> 3) {
+    const int64_t g = (int64_t)(blockIdx.x & 7) * per + j;
+    if (g >= U) return;
+    const int64_t m = map[g];
+    const int64_t sr = map_src ? m : g, dr = map_src ? g : m;
+    const u32x4* s = (const u32x4*)(src + sr * src_stride);
+    u32x4* d = (u32x4*)(dst + dr * dst_stride);
+    for (int64_t e0 = threadIdx.x; e0 < vpr; e0 += (int64_t)V * TH) {
+      u32x4 r[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (e0 + i * TH < vpr) r[i] = s[e0 + i * TH];
+      for (int i = 0; i < V; ++i)
+        if (e0 + i * TH < vpr) r[i] = s[e0 + i * TH];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (e0 + i * TH < vpr) __builtin_nontemporal_store(r[i], d + e0 + i * TH);
+      for (int i = 0; i < V; ++i)
+        if (e0 + i * TH < vpr) __builtin_nontemporal_store(r[i], d + e0 + i * TH);
+    }
   }
 }
 
@@ -341,8 +342,6 @@ size_t unpack_lds_bytes(int mode, int32_t N, int32_t eloc) {
 
 vp_status launch_unpack(const UnpackLaunch& a, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  const int threads = row_threads(a.row_bytes / 16);
-  if (!fits_launch((a.rows_cap + 7) / 8 * 8, threads)) return set_error(VP_ERR_UNSUPPORTED, "too many buffer rows");
   const int eloc = a.E / a.N;
   const size_t lds = unpack_lds_bytes(a.mode, a.N, eloc);
   if (lds > 64 * 1024) return set_error(VP_ERR_UNSUPPORTED, "too many ranks or local experts for the row map");
@@ -355,7 +354,9 @@ vp_status launch_unpack(const UnpackLaunch& a, void* stream) {
   hipLaunchKernelGGL(map_kernel, dim3(a.k_max), dim3(kMapThreads), lds, s, m);
   if (a.rows_cap > 0) {
     const int64_t vpr = a.row_bytes / 16;
-    const dim3 grid((unsigned)((a.rows_cap + 7) / 8 * 8));   // rows past the buffer's count exit at once
+    // rows past the buffer's count exit at once; at most 2^22 blocks of up to 512 threads, below a grid's 2^32
+    const dim3 grid((unsigned)std::min<int64_t>((a.rows_cap + 7) / 8 * 8, 1 << 22));
+    const int threads = row_threads(vpr);
     const unsigned char* sp = (const unsigned char*)a.src;
     unsigned char* dp = (unsigned char*)a.dst_buf;
     const int ms = a.mode == kModeCombinePack ? 1 : 0;

@@ -1,6 +1,7 @@
-"""Packs and unpacks of more than 2^32 threads are refused before anything is enqueued (no GPU): such a launch runs in part
-and returns no error."""
+"""Calls whose rows would take more than 2^32 threads, a launch that runs in part and returns no error: packs are refused
+before anything is enqueued, unpacks give a workgroup several rows."""
 import pytest
+import torch
 
 
 @pytest.fixture(scope="module")
@@ -18,12 +19,29 @@ LIMITS = [(16, 26), (2048, 26), (2064, 25), (4096, 25), (4112, 24), (8192, 24), 
 
 
 @pytest.mark.parametrize("row,bits", LIMITS)
-def test_pack_and_unpack_refuse_launches_of_2_to_the_32_threads(vp, row, bits):
-    L, n, slot = vp.lib(), 1 << bits, vp.slot_bytes(row)
+def test_packs_refuse_launches_of_2_to_the_32_threads(vp, row, bits):
+    L, n = vp.lib(), 1 << bits
     pack = lambda T, k: L.vp_pack_rows(P, T, k, row, P, P, P, 0, 8, P, P, P, P, P, 8, P, 1 << 20, P, P, P, BIG, None)  # noqa: E731
     gather = lambda T, k: L.vp_pack_gather(P, row, T, k, P, P, 8, P, 1 << 20, P, P, BIG, None)  # noqa: E731
     for call in (pack, gather):
         assert call(n, 1) == call(n // 8, 8) == call(n - 7, 1) == vp.UNSUPPORTED
-    assert L.vp_unpack_rows(P, (n - 7) * slot, row, P, 8, 0, 8, P, P, P, P, 8, P, 1 << 20, P, P, BIG, None) == vp.UNSUPPORTED
-    assert L.vp_pack_combine(P, 1 << 20, row, P, 8, 0, 8, P, P, P, 8, P, (n - 7) * row, P, P, P, BIG, None) == vp.UNSUPPORTED
-    assert L.vp_unpack_combine(P, (n - 7) * slot, row, 8, 1, P, P, P, 0, 8, P, P, P, P, 8, P, P, P, BIG, None) == vp.UNSUPPORTED
+
+
+@pytest.mark.gpu
+def test_unpack_of_two_to_the_26_rows(vp):
+    """One source's rows of 16 bytes to one expert, 64 threads a row."""
+    torch.cuda.empty_cache()
+    R, row = (1 << 26) + 5, 16
+    dev = dict(device="cuda")
+    counts = torch.tensor([[0, 0], [R, 0]], dtype=torch.int32, **dev)
+    sched = dict(K=torch.tensor([1], dtype=torch.int32, **dev), dst=torch.tensor([[1, 0]], dtype=torch.int32, **dev),
+                 bytes=torch.tensor([[0, R * row]], dtype=torch.int64, **dev),
+                 recv_src=torch.tensor([[1, 0]], dtype=torch.int32, **dev))
+    recv = torch.zeros((R, vp.slot_bytes(row) // 8), dtype=torch.int64, **dev)
+    recv[:, 0] = torch.arange(R, **dev)
+    recv[:, 1] = ~recv[:, 0]
+    out, st = torch.zeros_like(recv), vp.new_status()
+    vp.unpack_rows(recv, row, counts, 0, sched, out, st)
+    assert vp.read_status(st) == 0 and torch.equal(out, recv)
+    del recv, out
+    torch.cuda.empty_cache()
