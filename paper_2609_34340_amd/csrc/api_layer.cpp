@@ -12,7 +12,6 @@ constexpr int32_t kMaxExperts = 4096, kMaxTopK = 64, kMaxGroups = 64, kMaxWidth 
 
 bool is_float(int32_t d) { return d == VP_F32 || d == VP_BF16 || d == VP_F16; }
 bool is_half(int32_t d) { return d == VP_BF16 || d == VP_F16; }
-int64_t size_of(int32_t d) { return d == VP_F32 ? 4 : 2; }
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // Rows of `width` bytes, `stride` apart, moved in 16-byte vectors.
 bool vector_rows(const void* p, int64_t width, int64_t stride) {
@@ -181,7 +180,7 @@ vp_status vp_merge(const void* rows, int32_t dtype, int64_t T, int32_t k, int64_
                    void* stream) {
   vp_status st = check_merge(dtype, T, k, H, weights);
   if (st != VP_OK) return st;
-  const int64_t width = H * size_of(dtype);
+  const int64_t width = H * vp::dtype_size(dtype);
   if ((st = check_rows(rows, width, row_stride, T, "rows")) != VP_OK) return st;
   if ((st = check_rows(out, width, out_stride, T, "out")) != VP_OK) return st;
   if (residual && (st = check_rows(residual, width, residual_stride, T, "residual")) != VP_OK) return st;
@@ -195,7 +194,7 @@ vp_status vp_merge_grad(const void* d_out, int32_t dtype, int64_t T, int32_t k, 
                         int64_t d_rows_stride, float* d_weights, void* stream) {
   vp_status st = check_merge(dtype, T, k, H, weights);
   if (st != VP_OK) return st;
-  const int64_t width = H * size_of(dtype);
+  const int64_t width = H * vp::dtype_size(dtype);
   if ((st = check_rows(d_out, width, d_out_stride, T, "d_out")) != VP_OK) return st;
   if ((st = check_rows(rows, width, row_stride, T, "rows")) != VP_OK) return st;
   if ((st = check_rows(d_rows, width, d_rows_stride, T, "d_rows")) != VP_OK) return st;
@@ -223,7 +222,7 @@ vp_status vp_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t K, 
                          int64_t q_stride, void* stream) {
   vp_status st = check_mx(dtype, rows, K);
   if (st != VP_OK) return st;
-  if ((st = check_rows(x, K * size_of(dtype), x_stride, rows, "x")) != VP_OK) return st;
+  if ((st = check_rows(x, K * vp::dtype_size(dtype), x_stride, rows, "x")) != VP_OK) return st;
   if ((st = check_rows(q, vp::mx_row_bytes(K), q_stride, rows, "q")) != VP_OK) return st;
   if (rows == 0) return VP_OK;
   return vp::launch_mx_quantize(x, dtype, rows, K, x_stride, q, q_stride, stream);
@@ -234,7 +233,7 @@ vp_status vp_mx_dequantize(const void* q, int64_t rows, int64_t K, int64_t q_str
   vp_status st = check_mx(dtype, rows, K);
   if (st != VP_OK) return st;
   if ((st = check_rows(q, vp::mx_row_bytes(K), q_stride, rows, "q")) != VP_OK) return st;
-  if ((st = check_rows(out, K * size_of(dtype), out_stride, rows, "out")) != VP_OK) return st;
+  if ((st = check_rows(out, K * vp::dtype_size(dtype), out_stride, rows, "out")) != VP_OK) return st;
   if (rows == 0) return VP_OK;
   return vp::launch_mx_dequantize(q, rows, K, q_stride, out, dtype, out_stride, stream);
 }

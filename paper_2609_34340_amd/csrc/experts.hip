@@ -153,14 +153,14 @@ template <> struct Frag<F16> { using type = f16x8; };
 // with log2 e is rounded), far inside the 16 bits that the result is rounded
 // to; the library's exponential and divide cost a gated tile 64 times 30
 // instructions a lane.
-__device__ inline float sigmoid(float g) {
+__device__ inline float fast_sigmoid(float g) {
 #ifdef __HIP_DEVICE_COMPILE__
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504089f));
 #else
   return g;
 #endif
 }
-__device__ inline float silu(float g) { return g * sigmoid(g); }
+__device__ inline float silu(float g) { return g * fast_sigmoid(g); }
 
 // ---------------------------------------------------------------- tiled products
 
@@ -857,7 +857,7 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(GateArgs a) {
     unpack16<T>(*(const u32x4*)(a.pre + m * a.pre_stride + (int64_t)a.half * 2 + c * 16), u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float s = sigmoid(g[i]), du = dh[i] * g[i] * s;
+      const float s = fast_sigmoid(g[i]), du = dh[i] * g[i] * s;
       g[i] = dh[i] * u[i] * s * (1.0f + g[i] * (1.0f - s));
       u[i] = du;
     }

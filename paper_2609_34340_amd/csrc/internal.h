@@ -202,6 +202,7 @@ vp_status launch_transpose(const int64_t* D, int32_t N, int64_t* DT, void* strea
 // The layer around the exchanges: routing, the experts' products, the merge
 // of the returned rows, rows in 4-bit blocks.  Strides are bytes between rows
 // (the logits' in elements).
+inline int64_t dtype_size(int32_t d) { return d == VP_F32 ? 4 : 2; }
 vp_status launch_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t stride,
                        const vp_route_params& p, const float* bias, int32_t* ids, float* weights, void* stream);
 int32_t route_lanes(int64_t T, int32_t E);

@@ -5,8 +5,6 @@
 
 #include <cstdint>
 
-#include "../../include/vp.h"
-
 namespace vp {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -84,8 +82,5 @@ inline dim3 grid_of(int64_t blocks) {
   return blocks <= kGridLine ? dim3((unsigned)blocks) : dim3((unsigned)kGridLine, (unsigned)((blocks + kGridLine - 1) / kGridLine));
 }
 __device__ inline int64_t block_index() { return (int64_t)blockIdx.y * kGridLine + blockIdx.x; }
-
-inline int64_t dtype_size(int32_t d) { return d == VP_F32 ? 4 : 2; }
-inline bool is_dtype(int32_t d) { return d == VP_F32 || d == VP_BF16 || d == VP_F16; }
 
 }  // namespace vp
