@@ -223,8 +223,8 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteGradArgs a) {
   __syncthreads();
   float dot = 0.0f;
   for (int j = lane; j < k && live; j += 64) {
-    const float w = a.weights[t * k + j];
-    dot += w == 0.0f ? 0.0f : w * a.d_weights[t * k + j];   // a weight of 0 passes nothing on, infinities and NaN neither
+    const float w = a.weights[t * k + j], d = a.d_weights[t * k + j];
+    dot += w == 0.0f ? 0.0f : w * d;   // a weight of 0 passes nothing on, infinities and NaN neither
   }
   dot = across<64>(dot, [](float p, float q) { return p + q; });
   for (int j = lane; j < k && live; j += 64) {
