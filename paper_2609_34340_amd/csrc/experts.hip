@@ -271,10 +271,11 @@ struct TileAt : TileOut {
 
 // Measured: 32768 rows by 4096 x 4096, bf16 0.83-0.88 ms (1.25-1.33 PFLOP/s; the
 // library's product of that size 0.71 ms, 1.55), gated 0.82 and with the values
-// before the gate 0.89, its row gradient 0.82-0.88, its weight gradient 0.82-0.89, 4-bit blocks 0.28-0.30 (3.7-3.9 PFLOP/s).  The matrix
-// units are busy 62 % of the time at 1.8 to 1.9 GHz, to which the card's power
-// holds the clock (registers alone, random operands: 1.75-1.85 PFLOP/s).  Without
-// the loads 0.73 ms, without the LDS reads 0.85; waiting for neither changes
+// before the gate 0.89, its row gradient 0.82-0.88, its weight gradient
+// 0.82-0.89, 4-bit blocks 0.28-0.30 (3.7-3.9 PFLOP/s).  The matrix units are
+// busy 62 % of the time at 1.8 to 1.9 GHz, to which the card's power holds the
+// clock (registers alone, random operands: 1.75-1.85 PFLOP/s).  Without the
+// loads 0.73 ms, without the LDS reads 0.85; waiting for neither changes
 // nothing, nor does bringing the lines to the L2 ahead.  A tile costs 4 to 6 us
 // beside its steps (results of all CUs go out together).
 //
@@ -888,13 +889,14 @@ vp_status launch_tiled(const ProductArgs& a, hipStream_t s) {
 
 // Which kernel, from the sizes the host knows (R rows at most, spread over L
 // experts; a buffer much larger than its rows in use selects tiles: 61 rows at
-// four experts of 4096 x 4096, gated, 27 us in a buffer of 61, 61 in one of 512).  Few rows: the weights are read again for every 64 rows, at about
-// 3.6 TB/s (2.5 in 4-bit blocks); tiles take 0.85 us a step of the contraction
+// four experts of 4096 x 4096, gated, 27 us in a buffer of 61, 61 in one of
+// 512).  Few rows: the weights are read again for every 64 rows, at about 3.6
+// TB/s (2.5 in 4-bit blocks); tiles take 0.85 us a step of the contraction
 // (1.35) and 6 us around it for each round of workgroups, and read all weights
 // at 4.5 TB/s or less.  Measured, few rows against tiles, us: 64 rows at 4
 // experts of 4096 x 4096 35 / 60, 256 at 4 50 / 60, 256 at 1 48 / 60, 512 at 1
-// 91 / 62, 512 at 8 of 2048 x 2048 29 / 33, 768 at 8 52 / 35; in 4-bit blocks 256
-// at 1 of 4096 x 4096 19 / 27, 512 at 1 34 / 27.
+// 91 / 62, 512 at 8 of 2048 x 2048 29 / 33, 768 at 8 52 / 35; in 4-bit blocks
+// 256 at 1 of 4096 x 4096 19 / 27, 512 at 1 34 / 27.
 template <typename T> bool few_rows_win(const ProductArgs& a, int64_t weight_rows) {
   constexpr bool kMx = Elem<T>::mx;
   const int64_t tiles = a.R / kFewRows + a.L;

@@ -62,6 +62,22 @@ def test_logits_that_are_no_numbers_do_not_decide(vp, T, E, groups, dtype):
         assert all(len(set(r.tolist())) == k for r in ids)
 
 
+@pytest.mark.parametrize("T,E", [(33, 40), (4101, 40), (4101, 256), (9, 1280)])
+def test_a_row_with_a_nan_beside_rows_of_numbers(vp, T, E):
+    """Tokens that share a wavefront: each is routed as if it were alone."""
+    x = normal((T, E), 205, std=2.0)
+    odd = torch.arange(T) % 3 == 1
+    x[odd, 2], x[odd, 9] = math.nan, math.inf
+    x[::7, 4] = -math.inf
+    how = dict(bias=0.01 * normal((E,), 206).cuda(), n_groups=8, top_groups=5, group_top=2)
+    got = vp.route(x.cuda(), 5, **how)
+    for rows in (odd, ~odd):
+        alone = vp.route(x[rows].cuda(), 5, **how)
+        assert torch.equal(got["ids"][rows.cuda()], alone["ids"])
+        assert torch.equal(got["weights"][rows.cuda()].isnan(), alone["weights"].isnan())
+    assert torch.isfinite(got["weights"][(~odd).cuda()]).all() and (got["ids"].cpu()[odd][:, 0] == 9).all()
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [True, False])
 def test_a_weight_of_zero_passes_no_gradient_on(vp, score, renorm):
