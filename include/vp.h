@@ -546,8 +546,10 @@ typedef struct {
  * weights 0.  NaN logits are chosen last too, and the formulas carry them
  * into the weights; a softmax that holds a NaN or an infinity makes all its
  * row's weights NaN, while the choice follows the scores of the numbers alone
- * (an infinity counting as the limit).  Sums are in 32 bits.  E <= 4096, top_k
- * <= min(64, E) and <= the experts of the kept groups, T * top_k < 2^31. */
+ * (an infinity counting as the limit).  Scores and sums are in 32 bits: a
+ * sigmoid of a logit below -88 is 0, and a row of nothing else has weights 0.
+ * E <= 4096, top_k <= min(64, E) and <= the experts of the kept groups, T *
+ * top_k < 2^31. */
 vp_status vp_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t logits_stride,
                    const vp_route_params* p, const float* bias, int32_t* ids, float* weights, void* stream);
 
