@@ -8,7 +8,8 @@
  * (Sec. 4.1, Alg. 1), and unpacks received buffers into the output layout,
  * for the dispatch and for the combine that returns the rows.  Around these
  * stand the calls of the layer itself: routing to experts, the experts'
- * products, the merge of the returned rows, and rows in 4-bit blocks.
+ * products, the merge of the returned rows, rows in 4-bit blocks, and the
+ * dense operators of the block around it: norm, dense products, dropout.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -663,6 +664,107 @@ vp_status vp_expert_matmul_mx(const void* xq, int64_t xq_stride, const void* wq,
 typedef enum { VP_EXPERT_FEW_ROWS = 0, VP_EXPERT_TILES_128 = 1, VP_EXPERT_TILES_256 = 2 } vp_expert_kind;
 int32_t vp_expert_kernel(int32_t direction, int32_t mx, int32_t gated, int64_t R, int32_t L, int32_t N, int32_t K);
 int32_t vp_route_lanes(int64_t T, int32_t E);
+
+/* --------------------------------------- layer: norm, dropout, dense products
+ *
+ * The dense operators of the block around the exchanges.  Sums, statistics and
+ * the gradients of weights and biases are in 32 bits, results are rounded
+ * once, and every sum has one fixed order, so that a call repeats bit for bit.
+ * These calls have no device errors. */
+
+/* y[t] = (x[t] - m) r w + b with the row's mean m and r = 1 / sqrt(mean((x[t] -
+ * m)^2) + eps); without `center` m is 0 (root mean square).
+ *   x, y    device [T, H] of any vp_dtype, rows *_stride bytes apart; y may be
+ *           x itself
+ *   weight, bias  device [H] of param_dtype, which is VP_F32 or x's type;
+ *           either may be NULL (ones, zeros)
+ *   stats   device float32 [T, 2], (m, r) for the gradient, or NULL
+ * A row with an infinity or NaN becomes NaN and touches no other.  H <= 2^20, T
+ * < 2^31; strides and addresses are multiples of the element (of 16 bytes for
+ * full speed), eps >= 0 and finite. */
+vp_status vp_layer_norm(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, const void* weight,
+                        const void* bias, int32_t param_dtype, float eps, int32_t center, void* y, int64_t y_stride,
+                        float* stats, void* stream);
+
+/* Its gradient.  With u = (x[t] - m) r and g = d_out[t] w:
+ *   d_x[t]   = r (g - mean(g) - u mean(g u)) + residual[t]   (mean(g) only with `center`)
+ *   d_weight = sum_t d_out[t] u,  d_bias = sum_t d_out[t]    device float32 [H]
+ * weight (w = 1), residual, d_weight and d_bias may be NULL; d_x may be d_out
+ * or the residual itself.  stats as vp_layer_norm left them.  The workspace
+ * (needed where d_weight or d_bias is asked for) needs no clearing; calls
+ * that share one must not overlap. */
+size_t vp_layer_norm_grad_workspace(int64_t T, int64_t H);
+vp_status vp_layer_norm_grad(const void* d_out, int64_t d_out_stride, const void* x, int64_t x_stride, int32_t dtype,
+                             int64_t T, int64_t H, const float* stats, const void* weight, int32_t param_dtype,
+                             int32_t center, const void* residual, int64_t residual_stride, void* d_x,
+                             int64_t d_x_stride, float* d_weight, float* d_bias, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/* out = keep ? x * scale : 0, + residual where one is given.  The mask is a
+ * function of seed, step and a value's place alone and is never stored: the
+ * gradient is this call on d_out with the same seed and step (and the
+ * residual's is d_out itself).
+ *   step    device int64 [1], mixed into the seed (a replayed graph gets
+ *           another mask when it counts up), or NULL for 0
+ * With mix(z) SplitMix64's output function, g its increment, k = mix((mix(seed +
+ * g) xor step) + g) and W = (H + 3) / 4, bits 16 (c % 4) up to 16 (c % 4) + 15 of
+ * mix(k + (t W + c / 4 + 1) g) belong to value (t, c); it is kept where they
+ * reach least = round(65536 p), and scale = 65536 / (65536 - least), so that the
+ * expectation is x's own for every p (0 to 1, in steps of 2^-16; at 1 nothing
+ * is kept).  A dropped value adds nothing whatever it holds.  out may be x or
+ * the residual itself.  H <= 2^20, T < 2^31; strides and addresses as for the
+ * norm. */
+vp_status vp_dropout(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, double p, uint64_t seed,
+                     const int64_t* step, const void* residual, int64_t residual_stride, void* out,
+                     int64_t out_stride, void* stream);
+
+/* Activations: x; max(x, 0); x s(x) with the logistic s; x Phi(x) with the
+ * normal distribution; x s(2 sqrt(2 / pi) (x + 0.044715 x^3)). */
+enum { VP_ACT_NONE = 0, VP_ACT_RELU = 1, VP_ACT_SILU = 2, VP_ACT_GELU = 3, VP_ACT_GELU_TANH = 4 };
+
+/* Dense products: y = act(x W^T + bias) + residual.
+ *   x       device [R, K] bf16 or fp16, rows x_stride bytes apart
+ *   w       device [N, K] of the same type, rows w_stride bytes apart
+ *   bias    device [N] of bias_dtype, which is VP_F32 or x's type, or NULL
+ *   y, residual   device [R, N] of out_dtype, which is VP_F32 or x's type;
+ *           residual may be NULL, or y itself
+ *   pre     device [R, N] of x's type: x W^T + bias, rounded, for the
+ *           gradient, or NULL
+ * K and N are multiples of 8 up to 2^20, strides multiples of 16 bytes up to 4
+ * MiB, addresses 16-byte aligned, R < 2^31.  Where rows and columns are too few
+ * to fill the device, the contraction is split and the parts' sums joined from
+ * the workspace, which needs no clearing; calls that share one must not
+ * overlap.  vp_linear_workspace(direction, R, N, K): its bytes (often 0);
+ * direction 0 vp_linear, 1 vp_linear_grad_x, 2 vp_linear_grad_w. */
+size_t vp_linear_workspace(int32_t direction, int64_t R, int32_t N, int32_t K);
+vp_status vp_linear(const void* x, int64_t x_stride, int32_t dtype, const void* w, int64_t w_stride, int64_t R,
+                    int32_t N, int32_t K, const void* bias, int32_t bias_dtype, int32_t act, const void* residual,
+                    int64_t residual_stride, void* y, int32_t out_dtype, int64_t y_stride, void* pre,
+                    int64_t pre_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* Through the activation: d_pre = d_y * act'(pre) [R, N] of one type (any
+ * vp_dtype), and the bias's gradient d_bias = sum over rows (device float32
+ * [N]; of the values before d_pre's rounding).  d_pre or d_bias may be NULL, not
+ * both; pre is NULL exactly for VP_ACT_NONE; d_pre may be d_y itself.  relu's
+ * slope at 0 is 0.  N <= 2^20, R < 2^31; strides and addresses as for the norm.
+ * The workspace is needed for d_bias. */
+size_t vp_linear_act_grad_workspace(int64_t R, int64_t N);
+vp_status vp_linear_act_grad(const void* d_y, int64_t d_y_stride, const void* pre, int64_t pre_stride, int32_t dtype,
+                             int64_t R, int64_t N, int32_t act, void* d_pre, int64_t d_pre_stride, float* d_bias,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient by x: d_x = (d_y W) * act'(pre) + residual [R, K]: pre [R, K] the
+ * values before the activation that made x (NULL exactly for VP_ACT_NONE),
+ * residual [R, K] another gradient of x (NULL, or d_x itself), all of one type,
+ * bf16 or fp16.  Sizes, strides and workspace as for vp_linear. */
+vp_status vp_linear_grad_x(const void* d_y, int64_t d_y_stride, int32_t dtype, const void* w, int64_t w_stride,
+                           int64_t R, int32_t N, int32_t K, int32_t act, const void* pre, int64_t pre_stride,
+                           const void* residual, int64_t residual_stride, void* d_x, int64_t d_x_stride, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* Gradient by W: d_w = d_y^T x, device float32 [N, K], contiguous. */
+vp_status vp_linear_grad_w(const void* d_y, int64_t d_y_stride, const void* x, int64_t x_stride, int32_t dtype,
+                           int64_t R, int32_t N, int32_t K, float* d_w, void* ws, size_t ws_bytes, void* stream);
 
 /* --------------------------------------------------------------- helpers */
 

@@ -113,6 +113,7 @@ def lib():
     L.vp_last_error.argtypes = []
     L.vp_last_error.restype = C.c_char_p
     layer.declare(L)
+    dense.declare(L)
     _lib = L
     return L
 
@@ -752,3 +753,7 @@ from . import layer  # noqa: E402
 from .layer import (expert_gate_grad, expert_kernel, expert_matmul, expert_matmul_grad_w,  # noqa: E402,F401
                     expert_matmul_grad_x, expert_matmul_mx, expert_offsets, merge, merge_grad, mx_dequantize,
                     mx_quantize, mx_row_bytes, route, route_grad, route_lanes, unclaimed_status)
+from . import dense  # noqa: E402
+from .dense import (dropout, layer_norm, layer_norm_grad, layer_norm_grad_workspace_bytes, linear,  # noqa: E402,F401
+                    linear_act_grad, linear_act_grad_workspace_bytes, linear_grad_w, linear_grad_x,
+                    linear_workspace_bytes)

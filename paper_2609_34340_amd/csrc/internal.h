@@ -245,4 +245,46 @@ vp_status launch_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t
 vp_status launch_mx_dequantize(const void* q, int64_t rows, int64_t K, int64_t q_stride, void* out, int32_t dtype,
                                int64_t out_stride, void* stream);
 
+// Norm, dropout and dense products.  Strides are bytes between rows.
+struct NormLaunch {
+  int32_t dtype, param_dtype;
+  bool center;
+  int64_t T, H;
+  const void *x, *d_out, *residual, *weight, *bias;
+  int64_t x_stride, d_out_stride, residual_stride, out_stride;
+  void* out;            // y, or d_x
+  float* stats;         // forward: written unless null
+  const float* given;   // gradient: read
+  float eps;
+  float *d_weight, *d_bias;
+  void* ws;
+};
+vp_status launch_layer_norm(const NormLaunch& p, void* stream);
+size_t layer_norm_grad_workspace(int64_t T, int64_t H);
+vp_status launch_layer_norm_grad(const NormLaunch& p, void* stream);
+// Sums `parts` rows of H floats, in their order, into out.
+vp_status launch_column_sums(const float* part, int parts, int64_t H, float* out, void* stream);
+vp_status launch_dropout(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, uint32_t least,
+                         uint64_t seed, const int64_t* step, const void* residual, int64_t residual_stride, void* out,
+                         int64_t out_stride, void* stream);
+struct LinearLaunch {
+  int mode;             // of kExpertForward, ...
+  int32_t dtype, bias_dtype, out_dtype, act;
+  const void *a, *b;    // rows and weights; grad w: d_y and x
+  int64_t a_stride, b_stride;
+  int64_t R;
+  int32_t N, K;
+  const void *bias, *residual, *slope;   // slope: pre of the activation whose derivative is applied
+  int64_t residual_stride, slope_stride;
+  void *out, *pre;
+  int64_t out_stride, pre_stride;
+  void* ws;
+};
+size_t linear_workspace(int mode, int64_t R, int32_t N, int32_t K);
+vp_status launch_linear(const LinearLaunch& p, void* stream);
+size_t act_grad_workspace(int64_t R, int64_t N);
+vp_status launch_act_grad(const void* d_y, int64_t d_y_stride, const void* pre, int64_t pre_stride, int32_t dtype,
+                          int64_t R, int64_t N, int32_t act, void* d_pre, int64_t d_pre_stride, float* d_bias,
+                          void* ws, void* stream);
+
 }  // namespace vp

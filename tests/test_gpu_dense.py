@@ -1,0 +1,609 @@
+"""Norm, dropout and dense products on the GPU against their definitions in 64 bits, with the bounds of
+dense_reference.py, which follow from 32-bit sums and one rounding to the output's type."""
+import math
+
+import pytest
+import torch
+
+import dense_reference as ref
+from layer_reference import rounded
+
+pytestmark = pytest.mark.gpu
+
+HALVES = [torch.bfloat16, torch.float16]
+FLOATS = HALVES + [torch.float32]
+
+
+@pytest.fixture(scope="module")
+def vp():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2609_34340_amd as vp
+    return vp
+
+
+def normal(shape, seed, dtype=torch.float32, std=1.0, mean=0.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std + mean).to(dtype)
+
+
+def strided(t, pad, before=0):
+    """The same matrix on the GPU in rows `pad` elements longer, NaN between, `before` elements into its memory."""
+    wide = torch.full((t.shape[0] * (t.shape[1] + pad) + before,), math.nan, dtype=t.dtype).cuda()
+    out = wide[before:].view(t.shape[0], t.shape[1] + pad)[:, :t.shape[1]]
+    out.copy_(t)
+    return out
+
+
+def guarded(shape, dtype, pad=0):
+    """An output of NaN with guard values around its rows, and a check that these stayed."""
+    T, H = shape
+    wide = torch.full((T + 2, H + pad), 7.0, dtype=dtype, device="cuda")
+    out = wide[1:T + 1, :H]
+    out.fill_(math.nan)
+
+    def untouched():
+        assert (wide[0] == 7).all() and (wide[-1] == 7).all() and (wide[:, H:] == 7).all()
+    return out, untouched
+
+
+def near(got, want, bound, what=""):
+    got = got.double().cpu()
+    bad = ~((got - want).abs() <= bound)
+    assert not bad.any(), "%s: %d of %d, worst %.3g of a bound %.3g" % (
+        what, int(bad.sum()), bad.numel(), float((got - want).abs()[bad].max()), float(bound[bad].min()))
+
+
+def near_rounded(got, want, err, what=""):
+    near(got, want, rounded(err, want, got.dtype), what)
+
+
+# ------------------------------------------------------------------- norm
+
+NORMS = [
+    # T, H, elements between rows
+    (1, 1, 0), (3, 2, 1), (5, 8, 0), (2, 63, 0), (7, 64, 8), (4, 65, 3), (33, 200, 0), (130, 512, 0), (9, 520, 8),
+    (6, 1000, 24), (5, 2047, 0), (257, 2048, 0), (12, 4096, 8), (11, 4104, 0), (3, 7168, 0), (2, 8191, 1), (3, 8200, 0),
+    (2, 16384, 8), (2, 16392, 0), (2, 32776, 0), (1, 70001, 0), (1, 131080, 0)]
+
+
+def norm_inputs(T, H, dtype, param, seed=0):
+    x = normal((T, H), seed + 1, std=1.5, mean=0.7)
+    x *= torch.exp(normal((T, 1), seed + 2))
+    return x.to(dtype), normal((H,), seed + 3, mean=1.0, std=0.3).to(param), normal((H,), seed + 4, std=0.2).to(param)
+
+
+@pytest.mark.parametrize("T,H,pad", NORMS)
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_layer_norm(vp, T, H, pad, dtype):
+    for center, param, has_w, has_b in ((True, torch.float32, True, True), (False, dtype, True, False),
+                                        (True, dtype, False, True), (False, torch.float32, False, False)):
+        x, w, b = norm_inputs(T, H, dtype, param)
+        w, b = w if has_w else None, b if has_b else None
+        y, err, stats, stats_err = ref.norm(x, w, b, 1e-5, center)
+        out, untouched = guarded((T, H), dtype, pad)
+        got_stats = torch.full((T, 2), math.nan, device="cuda")
+        vp.layer_norm(strided(x, pad), None if w is None else w.cuda(), None if b is None else b.cuda(), center=center,
+                      out=out, stats=got_stats)
+        near_rounded(out, y, err, "y center=%s" % center)
+        near(got_stats, stats, stats_err + 1e-30, "stats")
+        untouched()
+
+
+@pytest.mark.parametrize("T,H,pad", NORMS)
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_layer_norm_grad(vp, T, H, pad, dtype):
+    for center, param, has_w, has_r in ((True, torch.float32, True, True), (False, dtype, True, False),
+                                        (True, dtype, False, True)):
+        x, w, _ = norm_inputs(T, H, dtype, param)
+        w = w if has_w else None
+        stats = ref.norm(x, None, None, 1e-5, center)[2].float()
+        dy, res = normal((T, H), 8, dtype), normal((T, H), 9, dtype) if has_r else None
+        dx, e_x, dw, e_w, db, e_b = ref.norm_grad(dy, x, stats, w, center, res)
+        out, untouched = guarded((T, H), dtype, pad)
+        got = vp.layer_norm_grad(strided(dy, pad), strided(x, pad), stats.cuda(), None if w is None else w.cuda(),
+                                 center=center, residual=None if res is None else strided(res, pad), d_x=out)
+        near_rounded(out, dx, e_x, "dx")
+        near(got[1], dw, e_w + 1e-30, "dw")
+        near(got[2], db, e_b + 1e-30, "db")
+        untouched()
+        only, none, nothing = vp.layer_norm_grad(dy.cuda(), x.cuda(), stats.cuda(), None if w is None else w.cuda(),
+                                                 center=center, residual=None if res is None else res.cuda(), params=False)
+        near_rounded(only, dx, e_x, "dx alone")
+        assert none is None and nothing is None
+
+
+@pytest.mark.parametrize("T", [1, 255, 256, 257, 1000, 4097])
+@pytest.mark.parametrize("H", [8, 264, 1021])
+def test_layer_norm_grad_of_many_rows(vp, T, H):
+    x, w, _ = norm_inputs(T, H, torch.bfloat16, torch.float32)
+    stats = ref.norm(x, None, None, 1e-5, True)[2].float()
+    dy = normal((T, H), 8, torch.bfloat16)
+    dx, e_x, dw, e_w, db, e_b = ref.norm_grad(dy, x, stats, w, True)
+    got = vp.layer_norm_grad(dy.cuda(), x.cuda(), stats.cuda(), w.cuda())
+    again = vp.layer_norm_grad(dy.cuda(), x.cuda(), stats.cuda(), w.cuda())
+    near_rounded(got[0], dx, e_x, "dx")
+    near(got[1], dw, e_w, "dw")
+    near(got[2], db, e_b, "db")
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_layer_norm_unaligned_memory(vp):
+    """Rows and parameters that start inside a 16-byte vector."""
+    for dtype, before in ((torch.bfloat16, 1), (torch.float32, 2)):
+        x, w, b = norm_inputs(6, 264, dtype, dtype)
+        y, err, stats, _ = ref.norm(x, w, b, 1e-5, True)
+        place = lambda v: strided(v[None], 0, before)[0]  # noqa: E731
+        near_rounded(vp.layer_norm(strided(x, 0, before), place(w), place(b)), y, err)
+        near_rounded(vp.layer_norm(x.cuda(), place(w), place(b)), y, err)
+        out = strided(torch.zeros(6, 264, dtype=dtype), 0, before)
+        near_rounded(vp.layer_norm(x.cuda(), w.cuda(), b.cuda(), out=out), y, err)
+        dy, stats = normal((6, 264), 8, dtype), stats.float()
+        dx, e_x, dw, e_w, _, _ = ref.norm_grad(dy, x, stats, w, True)
+        got = vp.layer_norm_grad(strided(dy, 0, before), x.cuda(), stats.cuda(), place(w))
+        near_rounded(got[0], dx, e_x)
+        near(got[1], dw, e_w)
+
+
+@pytest.mark.parametrize("H", [100, 4096, 20000])
+def test_layer_norm_far_from_zero(vp, H):
+    """Rows whose mean is thousands of times their deviation, equal rows, rows of zeros."""
+    x = normal((4, H), 1)
+    x[0] += 5000.0
+    x[1] = 1000.1
+    x[2] = 0.0
+    for center in (True, False):
+        y, err, stats, stats_err = ref.norm(x, None, None, 1e-5, center)
+        got_stats = torch.zeros(4, 2, device="cuda")
+        near_rounded(vp.layer_norm(x.cuda(), center=center, stats=got_stats), y, err)
+        near(got_stats, stats, stats_err + 1e-30)
+
+
+def test_layer_norm_of_infinities_and_nan(vp):
+    for H in (40, 3000):
+        x = normal((5, H), 1)
+        x[1, 3], x[2, H - 1], x[3, 0] = math.inf, math.nan, -math.inf
+        y, err, stats, _ = ref.norm(x, None, None, 1e-5, True)
+        got = vp.layer_norm(x.cuda())
+        assert got[1:4].isnan().all()
+        near_rounded(got[::4], y[::4], err[::4])
+        stats = ref.norm(torch.where(x.isfinite(), x, 0.0), None, None, 1e-5, True)[2].float()
+        dx, e_x, dw, _, _, _ = ref.norm_grad(torch.ones_like(x), x, stats, None, True)
+        got = vp.layer_norm_grad(torch.ones_like(x).cuda(), x.cuda(), stats.cuda())
+        near_rounded(got[0][::4], dx[::4], e_x[::4])
+        assert torch.equal(got[1].cpu().isnan(), dw.isnan()) and got[2].isfinite().all()
+
+
+def test_layer_norm_in_place_and_empty(vp):
+    for H in (264, 40000):
+        x, w, b = norm_inputs(9, H, torch.float16, torch.float32)
+        y, err, stats, _ = ref.norm(x, w, b, 1e-5, True)
+        here = x.cuda()
+        assert vp.layer_norm(here, w.cuda(), b.cuda(), out=here) is here
+        near_rounded(here, y, err)
+        dy, stats = normal((9, H), 8, torch.float16), stats.float()
+        dx, e_x, dw, e_w, _, _ = ref.norm_grad(dy, x, stats, w, True, dy)
+        here = dy.cuda()
+        got = vp.layer_norm_grad(here, x.cuda(), stats.cuda(), w.cuda(), residual=here, d_x=here)
+        near_rounded(here, dx, e_x)
+        near(got[1], dw, e_w)
+    none = torch.empty(0, 16, device="cuda")
+    assert vp.layer_norm(none).shape == (0, 16)
+    got = vp.layer_norm_grad(none, none, torch.empty(0, 2, device="cuda"), d_weight=torch.ones(16, device="cuda"))
+    assert (got[1] == 0).all() and (got[2] == 0).all()   # sums over no rows
+
+
+@pytest.mark.parametrize("center", [True, False])
+def test_layer_norm_grad_against_differences(vp, center):
+    """The loss sum(y c) by central differences of the forward call: its own error is the third derivative's, h^2 times
+    about the loss (1e-4 at h = 1e-2), and the rounding of y, 2^-24 |y c| sqrt(H T) / h (6e-5)."""
+    T, H, h = 3, 37, 1e-2
+    x, w, b = (v.cuda() for v in norm_inputs(T, H, torch.float32, torch.float32))
+    c = normal((T, H), 7).cuda()
+    stats = torch.empty(T, 2, device="cuda")
+    vp.layer_norm(x, w, b, center=center, stats=stats)
+    dx, dw, db = vp.layer_norm_grad(c, x, stats, w, center=center)
+    loss = lambda *a: float((vp.layer_norm(*a, center=center).double() * c.double()).sum())  # noqa: E731
+    for v, grad, args in ((x, dx, lambda u: (u, w, b)), (w, dw, lambda u: (x, u, b)), (b, db, lambda u: (x, w, u))):
+        d = normal(v.shape, 11).cuda()
+        d /= d.norm()
+        numeric = (loss(*args(v + h * d)) - loss(*args(v - h * d))) / (2 * h)
+        assert abs(numeric - float((grad.double() * d.double()).sum())) < 2e-3
+
+
+# ---------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("T,H,pad", [(1, 1, 0), (3, 2, 1), (2, 3, 0), (5, 4, 4), (7, 5, 0), (4, 8, 0), (130, 264, 8),
+                                     (9, 1023, 0), (33, 2048, 0), (3, 7168, 8), (2, 8193, 7), (1, 70004, 0)])
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_dropout(vp, T, H, pad, dtype):
+    x, res = normal((T, H), 1, dtype), normal((T, H), 2, dtype)
+    for p, seed, step in ((0.1, 7, None), (0.5, (1 << 64) - 3, 12345), (0.0, 1, 0), (1.0, 2, -5), (0.999, 3, 1 << 62)):
+        mask, scale = ref.kept(T, H, p, seed, step or 0)
+        at = None if step is None else torch.tensor([step], dtype=torch.int64).cuda()
+        for r in (None, res):
+            out, untouched = guarded((T, H), dtype, pad)
+            vp.dropout(strided(x, pad), p, seed, step=at, residual=None if r is None else strided(r, pad), out=out)
+            y, err = ref.dropout(x, mask, scale, r)
+            near_rounded(out, y, err)
+            if r is None:
+                assert torch.equal(out.cpu() != 0, mask & (x != 0))
+            untouched()
+
+
+def test_dropout_share_and_streams(vp):
+    """Shares of kept values within six standard deviations, of steps and seeds that agree no more than chance has it."""
+    T, H, p = 512, 4096, 0.3
+    x = torch.ones(T, H, device="cuda")
+    masks = [vp.dropout(x, p, seed, step=torch.tensor([step]).cuda()) != 0
+             for seed, step in ((5, 0), (5, 1), (6, 0), (5 + (1 << 32), 0))]
+    least = math.floor(p * 65536 + 0.5) / 65536
+    for m in masks:
+        assert abs(float(m.double().mean()) - (1 - least)) < 6 * math.sqrt(least * (1 - least) / (T * H))
+    agree = least ** 2 + (1 - least) ** 2
+    for i, m in enumerate(masks):
+        for n in masks[:i]:
+            assert abs(float((m == n).double().mean()) - agree) < 6 * math.sqrt(agree * (1 - agree) / (T * H))
+        # neighbours along a row, and across rows
+        for a, b in ((m[:, 1:], m[:, :-1]), (m[:, 4:], m[:, :-4]), (m[1:], m[:-1])):
+            assert abs(float((a == b).double().mean()) - agree) < 6 * math.sqrt(agree * (1 - agree) / a.numel())
+
+
+def test_dropout_drops_whatever_a_value_holds(vp):
+    for dtype in FLOATS:
+        mask, scale = ref.kept(4, 96, 0.5, 9)
+        x = torch.where(mask, normal((4, 96), 1), torch.tensor([math.nan, math.inf, -math.inf]).repeat(32)).to(dtype)
+        y, err = ref.dropout(torch.where(mask, x, 0), mask, scale)
+        near_rounded(vp.dropout(x.cuda(), 0.5, 9), y, err)
+        assert (vp.dropout(torch.full_like(x, math.nan).cuda(), 1.0, 9) == 0).all()
+
+
+def test_dropout_is_its_own_gradient_in_place_and_empty(vp):
+    x, d = normal((17, 100), 1, torch.bfloat16).cuda(), normal((17, 100), 2, torch.bfloat16).cuda()
+    step = torch.tensor([3]).cuda()
+    y = vp.dropout(x, 0.4, 11, step=step)
+    dx = vp.dropout(d, 0.4, 11, step=step)
+    assert torch.equal(y != 0, (dx != 0) & (x != 0) | (y != 0) & (d == 0))
+    here = x.clone()
+    assert torch.equal(vp.dropout(here, 0.4, 11, step=step, out=here), y)
+    res = d.clone()
+    assert torch.equal(vp.dropout(x, 0.4, 11, step=step, residual=res, out=res),
+                       vp.dropout(x, 0.4, 11, step=step, residual=d))
+    assert vp.dropout(x[:0], 0.4, 11).shape == (0, 100)
+    with_strides = strided(x.cpu(), 0, 1)
+    assert torch.equal(vp.dropout(with_strides, 0.4, 11, step=step), y)   # memory that no vector is aligned in
+
+
+# ---------------------------------------------------------- dense products
+
+LINEARS = [
+    # R, N, K
+    (1, 8, 8), (1, 256, 7168), (2, 16, 40), (15, 24, 64), (16, 32, 72), (17, 40, 128), (61, 4096, 512), (64, 264, 256),
+    (65, 256, 4096), (96, 128, 2048), (100, 1000, 1032), (127, 136, 136), (129, 128, 64), (200, 520, 264), (257, 256, 1024),
+    (300, 2048, 512), (513, 1032, 200), (1030, 264, 128), (2049, 512, 64)]
+
+
+def linear_inputs(R, N, K, dtype, seed=0):
+    return normal((R, K), seed + 1, dtype), normal((N, K), seed + 2, dtype, std=K ** -0.5), normal((N,), seed + 3)
+
+
+@pytest.mark.parametrize("R,N,K", LINEARS)
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_linear(vp, R, N, K, dtype):
+    x, w, b = linear_inputs(R, N, K, dtype)
+    for i, (act, bias, res, wide, pre) in enumerate((
+            ("none", None, False, False, False), ("gelu", b, True, False, True), ("silu", b.to(dtype), False, True, False),
+            ("none", b, True, True, True), ("relu", None, True, False, False), ("gelu_tanh", b, False, False, True))):
+        kind = torch.float32 if wide else dtype
+        r = normal((R, N), 5, kind) if res else None
+        y, err, z, e = ref.linear(x, w, bias, act, r)
+        pad = 8 * (i % 3)
+        out, untouched = guarded((R, N), kind, pad)
+        got_pre, pre_untouched = guarded((R, N), dtype, pad) if pre else (None, None)
+        vp.linear(strided(x, pad), strided(w, pad), None if bias is None else bias.cuda(), act=act,
+                  residual=None if r is None else strided(r, pad), out=out, pre=got_pre)
+        near_rounded(out, y, err, "y %s" % act)
+        untouched()
+        if pre:
+            near_rounded(got_pre, z, e, "pre")
+            pre_untouched()
+
+
+@pytest.mark.parametrize("R,N,K", LINEARS)
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_linear_grad_x(vp, R, N, K, dtype):
+    dy, w, pre, res = normal((R, N), 1, dtype), normal((N, K), 2, dtype, std=N ** -0.5), normal((R, K), 3, dtype, std=2.0), normal((R, K), 4, dtype)
+    for i, (act, has_res) in enumerate((("none", False), ("gelu", True), ("silu", False), ("relu", True), ("gelu_tanh", False))):
+        pad = 8 * (i % 3)
+        dx, e = ref.linear_grad_x(dy, w, act, pre, res if has_res else None)
+        out, untouched = guarded((R, K), dtype, pad)
+        vp.linear_grad_x(strided(dy, pad), strided(w, pad), act=act, pre=None if act == "none" else strided(pre, pad),
+                         residual=strided(res, pad) if has_res else None, out=out)
+        near_rounded(out, dx, e, "dx %s" % act)
+        untouched()
+
+
+@pytest.mark.parametrize("R,N,K", LINEARS + [(0, 8, 16), (8, 264, 512), (5000, 256, 128)])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_linear_grad_w(vp, R, N, K, dtype):
+    dy, x = normal((R, N), 1, dtype), normal((R, K), 2, dtype)
+    dw, e = ref.linear_grad_w(dy, x)
+    for pad in (0, 8):
+        out, untouched = guarded((N, K), torch.float32)
+        near(vp.linear_grad_w(strided(dy, pad), strided(x, pad), out=out), dw, e + 1e-30)
+        untouched()
+
+
+@pytest.mark.parametrize("R,N,pad", [(1, 1, 0), (3, 5, 2), (300, 8, 0), (17, 264, 8), (257, 1000, 0), (1000, 131, 1), (2, 9000, 0)])
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("dtype", FLOATS, ids=str)
+def test_linear_act_grad(vp, R, N, pad, act, dtype):
+    dy, pre = normal((R, N), 1, dtype), normal((R, N), 2, dtype, std=3.0)
+    d, e, db, e_b = ref.act_grad(dy, pre, act)
+    out, untouched = guarded((R, N), dtype, pad)
+    got, got_b = vp.linear_act_grad(strided(dy, pad), None if act == "none" else strided(pre, pad), act=act, out=out)
+    near_rounded(out, d, e, "d_pre")
+    near(got_b, db, e_b + 1e-30, "d_bias")
+    untouched()
+    assert got is out
+    got, none = vp.linear_act_grad(dy.cuda(), None if act == "none" else pre.cuda(), act=act, bias=False)
+    assert none is None
+    near_rounded(got, d, e, "d_pre alone")
+    here = dy.cuda()
+    vp.linear_act_grad(here, None if act == "none" else pre.cuda(), act=act, out=here)
+    near_rounded(here, d, e, "in place")
+
+
+@pytest.mark.parametrize("act", ref.ACTS[1:])
+def test_activations_over_their_range(vp, act):
+    """Every kind of argument: the tails, both zeros, the smallest values, and what lies past the exponential's range."""
+    v = torch.cat([torch.linspace(-14, 14, 8192 - 16), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 40.0, -40.0, 87.0, -87.0, 89.0,
+                                                                     -89.0, 1e4, -1e4, 1e18, -1e18, 1e-3, -1e-3])]).view(32, 256)
+    one = torch.eye(256, dtype=torch.float16)
+    # 16-bit arguments reach the epilogue exactly through the identity; fp32 results show its own error
+    h = v.clamp(-6e4, 6e4).half()
+    y, err, _, _ = ref.linear(h, one, None, act)
+    near_rounded(vp.linear(h.cuda(), one.cuda(), act=act, dtype=torch.float32), y, err)
+    dy = torch.ones_like(v)
+    d, e, _, _ = ref.act_grad(dy, v, act)
+    got, _ = vp.linear_act_grad(dy.cuda(), v.cuda(), act=act)
+    near_rounded(got, d, torch.where(v.abs() > 1e3, 1e-28, e), "slope")   # the limits 0 and 1
+    z = torch.full((16, 256), math.nan, dtype=torch.float16).cuda()
+    assert vp.linear(z, one.cuda(), act=act).isnan().all()
+
+
+def test_linear_carries_infinities_and_nan_in_their_rows_only(vp):
+    for R, N, K in ((5, 64, 72), (300, 264, 128)):
+        x, w, b = linear_inputs(R, N, K, torch.bfloat16)
+        x[1, 3], x[3, K - 1] = math.nan, math.inf
+        y, err, _, _ = ref.linear(x, w, b)
+        got = vp.linear(x.cuda(), w.cuda(), b.cuda())
+        ok = [0, 2, 4]
+        near_rounded(got[ok], y[ok], err[ok])
+        assert got[1].isnan().all() and not got[3].isfinite().any()
+        assert got[4:].isfinite().all()
+
+
+def test_linear_in_place_and_empty(vp):
+    for R in (3, 200):
+        x, w, b = linear_inputs(R, 136, 72, torch.bfloat16)
+        for kind in (torch.bfloat16, torch.float32):
+            res = normal((R, 136), 5, kind)
+            y, err, _, _ = ref.linear(x, w, b, "silu", res)
+            here = res.cuda()
+            assert vp.linear(x.cuda(), w.cuda(), b.cuda(), act="silu", residual=here, out=here) is here
+            near_rounded(here, y, err)
+    e = torch.empty(0, 72, dtype=torch.bfloat16, device="cuda")
+    assert vp.linear(e, w.cuda()).shape == (0, 136)
+    assert vp.linear_grad_x(torch.empty(0, 136, dtype=torch.bfloat16, device="cuda"), w.cuda()).shape == (0, 72)
+    assert (vp.linear_act_grad(torch.empty(0, 9, device="cuda"), d_bias=torch.ones(9, device="cuda"))[1] == 0).all()
+
+
+def test_linear_gradients_against_differences(vp):
+    """Of sum(y c) in one direction of x, w and bias, y in 32 bits from fp16 inputs that h d moves exactly (powers of
+    two): the third derivative's share is h^2 / 6 of its size (below 1e-2 at h = 2^-4), y's rounding 1e-5 / h."""
+    R, N, K = 5, 16, 24
+    x, w, b = linear_inputs(R, N, K, torch.float16)
+    x, w = (x * 16).round() / 16, (w * 16).round() / 16
+    x, w, b, c = x.cuda(), w.cuda(), b.cuda(), normal((R, N), 7).half().cuda()
+    h = 2.0 ** -4
+    for act in ref.ACTS[2:]:
+        pre = torch.empty(R, N, dtype=torch.float16, device="cuda")
+        vp.linear(x, w, b, act=act, pre=pre)
+        dz, db = vp.linear_act_grad(c, pre, act=act)
+        grads = vp.linear_grad_x(dz, w), vp.linear_grad_w(dz, x), db
+        loss = lambda *a: float((vp.linear(*a, act=act, dtype=torch.float32).double() * c.double()).sum())  # noqa: E731
+        for v, grad, args in ((x, grads[0], lambda u: (u, w, b)), (w, grads[1], lambda u: (x, u, b)), (b, grads[2], lambda u: (x, w, u))):
+            d = torch.zeros_like(v)
+            d.view(-1)[::7] = h
+            numeric = (loss(*args(v + d)) - loss(*args(v - d))) / 2
+            analytic = float((grad.double() * d.double()).sum())
+            size = float((grad.double() * d.double()).abs().sum())
+            # roundings of pre, dz and dx to fp16, three halves of a step of 2^-10, and the differences' own error
+            assert abs(numeric - analytic) < size * (3 * 2.0 ** -11 + 1e-2) + 2e-3, (act, numeric, analytic)
+
+
+# --------------------------------------------------- together, streams, graphs
+
+def block(vp, t, ws=None):
+    """Norm, router, shared expert and dropout as a block uses them, with every gradient."""
+    stats = torch.empty(len(t["x"]), 2, device="cuda")
+    n = vp.layer_norm(t["x"], t["nw"], t["nb"], stats=stats)
+    logits = vp.linear(n, t["router"], t["router_bias"], dtype=torch.float32)
+    routed = vp.route(logits, 2)
+    pre = torch.empty(len(n), t["up"].shape[0], dtype=n.dtype, device="cuda")
+    h = vp.linear(n, t["up"], t["up_bias"], act="gelu", pre=pre)
+    y = vp.linear(h, t["down"])
+    out = vp.dropout(y, 0.25, 77, step=t["step"], residual=t["x"])
+    # backward of sum(out d) + sum(weights d_weights)
+    dy = vp.dropout(t["d"], 0.25, 77, step=t["step"])
+    d_down = vp.linear_grad_w(dy, h)
+    d_pre = vp.linear_grad_x(dy, t["down"], act="gelu", pre=pre)
+    _, d_up_bias = vp.linear_act_grad(d_pre)
+    d_up = vp.linear_grad_w(d_pre, n)
+    d_logits = vp.route_grad(logits, routed["ids"], routed["weights"], t["d_weights"]).to(n.dtype)
+    d_router = vp.linear_grad_w(d_logits, n)
+    dn = vp.linear_grad_x(d_logits, t["router"])
+    dn = vp.linear_grad_x(d_pre, t["up"], residual=dn)
+    dx, d_nw, d_nb = vp.layer_norm_grad(dn, t["x"], stats, t["nw"], residual=t["d"])
+    return dict(out=out, weights=routed["weights"], ids=routed["ids"], d_down=d_down, d_up_bias=d_up_bias, d_up=d_up,
+                d_router=d_router, dx=dx, d_nw=d_nw, d_nb=d_nb)
+
+
+def block_inputs(T=77, H=264, E=16, I=136):
+    bf = torch.bfloat16
+    t = dict(x=normal((T, H), 1, bf), nw=normal((H,), 2, mean=1.0, std=0.1), nb=normal((H,), 3, std=0.1),
+             router=normal((E, H), 4, bf, std=H ** -0.5), router_bias=normal((E,), 5, std=0.1),
+             up=normal((I, H), 6, bf, std=H ** -0.5), up_bias=normal((I,), 7, std=0.1), down=normal((H, I), 8, bf, std=I ** -0.5),
+             d=normal((T, H), 9, bf), d_weights=normal((T, 2), 10), step=torch.tensor([5]))
+    return {k: v.cuda() for k, v in t.items()}
+
+
+def test_block_against_autograd(vp):
+    """A whole block with its backward pass against torch in 64 bits.  Values round to bf16 up to seven times on a way
+    (norm, pre, h, y, out and back), each by at most 2^-8 of its size."""
+    t = block_inputs()
+    got = block(vp, t)
+    leaf = {k: v.double().cpu().requires_grad_() for k, v in t.items() if k not in ("step", "d", "d_weights")}
+    x = leaf["x"]
+    m = x.mean(1, keepdim=True)
+    n = (x - m) / ((x - m).square().mean(1, keepdim=True) + 1e-5).sqrt() * leaf["nw"] + leaf["nb"]
+    logits = n @ leaf["router"].t() + leaf["router_bias"]
+    ids = got["ids"].cpu().long()
+    chosen = torch.softmax(logits, 1).gather(1, ids)
+    weights = chosen / chosen.sum(1, keepdim=True)
+    y = ref.act(n @ leaf["up"].t() + leaf["up_bias"], "gelu") @ leaf["down"].t()
+    mask, scale = ref.kept(*t["x"].shape, 0.25, 77, 5)
+    out = torch.where(mask, y * scale, 0.0) + x
+    ((out * t["d"].double().cpu()).sum() + (weights * t["d_weights"].double().cpu()).sum()).backward()
+    want = dict(out=out, weights=weights, d_down=leaf["down"].grad, d_up=leaf["up"].grad, d_up_bias=leaf["up_bias"].grad,
+                d_router=leaf["router"].grad, dx=x.grad, d_nw=leaf["nw"].grad, d_nb=leaf["nb"].grad)
+    for k, v in want.items():
+        v = v.detach()
+        off = float((got[k].double().cpu() - v).norm() / v.norm())
+        assert off < 7 * 2.0 ** -8, (k, off)
+
+
+def test_block_on_another_stream_and_in_a_graph(vp):
+    t = block_inputs(T=300, H=512, E=32, I=1032)
+    want = block(vp, t)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = block(vp, t)
+        block(vp, t)
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], want[k]) for k in want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kept = block(vp, t)
+        t["step"] += 1
+    for i in range(4):
+        t["step"].fill_(5 + i)
+        eager = block(vp, t)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(kept[k], eager[k]) for k in eager)
+        assert int(t["step"]) == 6 + i
+        assert i == 0 or not torch.equal(eager["out"], want["out"])   # another step, another mask
+        x = torch.randn(64, 64, device="cuda")
+        (x @ x).sum().item()
+
+
+def test_calls_at_once_on_two_streams(vp):
+    """Calls that make their own workspaces may overlap."""
+    a, b = block_inputs(T=96, H=2048, E=64, I=512), block_inputs(T=65, H=1024, E=32, I=256)
+    want = block(vp, a), block(vp, b)
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        with torch.cuda.stream(one):
+            p = block(vp, a)
+        with torch.cuda.stream(two):
+            q = block(vp, b)
+        torch.cuda.synchronize()
+        for got, w in ((p, want[0]), (q, want[1])):
+            assert all(torch.equal(got[k], w[k]) for k in w)
+
+
+def test_the_stream_argument(vp):
+    t = block_inputs()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    stats = torch.empty(len(t["x"]), 2, device="cuda")
+    torch.cuda.synchronize()
+    y = vp.layer_norm(t["x"], t["nw"], t["nb"], stats=stats, stream=s)
+    z = vp.linear(y, t["up"], t["up_bias"], act="silu", stream=s)
+    d = vp.dropout(z, 0.5, 3, step=t["step"], stream=s)
+    dz, db = vp.linear_act_grad(d, z, act="silu", stream=s)
+    dx, dw = vp.linear_grad_x(dz, t["up"], stream=s), vp.linear_grad_w(dz, y, stream=s)
+    g = vp.layer_norm_grad(dx, t["x"], stats, t["nw"], stream=s)
+    s.synchronize()
+    y2 = vp.layer_norm(t["x"], t["nw"], t["nb"])
+    z2 = vp.linear(y2, t["up"], t["up_bias"], act="silu")
+    d2 = vp.dropout(z2, 0.5, 3, step=t["step"])
+    dz2, db2 = vp.linear_act_grad(d2, z2, act="silu")
+    dx2, dw2 = vp.linear_grad_x(dz2, t["up"]), vp.linear_grad_w(dz2, y2)
+    g2 = vp.layer_norm_grad(dx2, t["x"], stats, t["nw"])
+    for p, q in zip((y, z, d, dz, db, dx, dw, *g), (y2, z2, d2, dz2, db2, dx2, dw2, *g2)):
+        assert torch.equal(p, q)
+
+
+# ------------------------------------------------------------ large buffers
+
+def test_rows_past_4_gib(vp):
+    """Rows whose byte offsets pass 32 bits, in a buffer of 4.3 GiB."""
+    T, H = 70000, 32768
+    x = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    last = normal((3, H), 1, torch.bfloat16)
+    x[-3:] = last
+    y, err, stats, _ = ref.norm(last, None, None, 1e-5, True)
+    got_stats = torch.empty(T, 2, device="cuda")
+    near_rounded(vp.layer_norm(x, out=x, stats=got_stats)[-3:], y, err)
+    x[-3:] = last
+    dx, e_x, dw, e_w, _, _ = ref.norm_grad(last, last, stats.float(), None, True)
+    got = vp.layer_norm_grad(x, x, got_stats)
+    near_rounded(got[0][-3:], dx, e_x + 1e-6)   # the kernel's own statistics, a few units off
+    near(got[1], dw, e_w + 1e-4)
+    del got
+    mask, scale = ref.kept(3, H, 0.5, 4, 0, T - 3)
+    want, err = ref.dropout(last, mask, scale)
+    near_rounded(vp.dropout(x, 0.5, 4, out=x)[-3:], want, err)
+    x[-3:] = last
+    d, e, db, e_b = ref.act_grad(last, last, "silu")
+    got, got_b = vp.linear_act_grad(x, x, act="silu", out=x)
+    near_rounded(got[-3:], d, e)
+    near(got_b, db, e_b + 1e-30)
+    x[-3:] = last
+    w = normal((64, 4096), 2, torch.bfloat16, std=1 / 64)
+    part = x[:, H - 4096:]   # rows 64 KiB apart
+    z, e, _, _ = ref.linear(last[:, H - 4096:], w)
+    near_rounded(vp.linear(part, w.cuda())[-3:], z, e)
+    dw, e = ref.linear_grad_w(last[:, :64], last[:, H - 4096:])
+    near(vp.linear_grad_w(x[:, :64], part), dw, e + 1e-30)
+    gx, e = ref.linear_grad_x(last[:, :64], w)
+    near_rounded(vp.linear_grad_x(x[:, :64], w.cuda(), out=part)[-3:], gx, e)
+
+
+def test_launches_of_more_than_2_to_the_32_threads(vp):
+    """2^24 + 5 short rows: more workgroups than a dimension of a grid takes."""
+    T, H = (1 << 24) + 5, 8
+    x = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    last = normal((5, H), 1, torch.bfloat16)
+    x[-5:] = last
+    x[:5] = last
+    y, err, stats, _ = ref.norm(last, None, None, 1e-5, True)
+    got = vp.layer_norm(x)
+    near_rounded(got[-5:], y, err)
+    near_rounded(got[:5], y, err)
+    st = torch.zeros(T, 2, device="cuda")
+    st[-5:] = stats.float().cuda()
+    dx, e_x, dw, e_w, db, e_b = ref.norm_grad(last, last, stats.float(), None, True)
+    got = vp.layer_norm_grad(x * 1, x, st)
+    near_rounded(got[0][-5:], dx, e_x)
+    near(got[2], 2 * db, 4 * e_b + 1e-6)
+    for first in (0, T - 5):
+        mask, scale = ref.kept(5, H, 0.5, 4, 0, first)
+        want, err = ref.dropout(last, mask, scale)
+        near_rounded(vp.dropout(x, 0.5, 4)[first:first + 5], want, err)
+    d, e, _, _ = ref.act_grad(last, last, "silu")
+    near_rounded(vp.linear_act_grad(x, x, act="silu")[0][-5:], d, e)
