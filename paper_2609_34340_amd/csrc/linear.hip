@@ -11,69 +11,140 @@
 #include "act.h"
 #include "internal.h"
 #include "numeric.h"
+#include "product.h"
 
 namespace vp {
 namespace {
 
-constexpr int kTile = 64, kDepth = 16;
-
-struct LinearArgs {
-  const unsigned char *a, *b;
-  int64_t a_stride, b_stride;
-  int64_t M;
-  int32_t N, C;
-  const void* bias;
-  bool bias_wide;
-  int32_t act;
-  const unsigned char *residual, *slope;
-  int64_t residual_stride, slope_stride;
-  unsigned char *out, *pre;
-  bool out_wide;
-  int64_t out_stride, pre_stride;
-};
-
-// A 64 x 64 tile of the output by 256 threads, sums of 32-bit products.  COLS: the operand's rows are the contraction.
-template <typename T, bool COLS_A, bool COLS_B> __global__ void __launch_bounds__(256) linear_simple(LinearArgs a) {
-  __shared__ float la[kDepth][kTile + 1], lb[kDepth][kTile + 1];
-  const int64_t m0 = (int64_t)blockIdx.x * kTile;
-  const int n0 = blockIdx.y * kTile;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[4][4] = {};
-  const auto at = [](const unsigned char* p, int64_t stride, bool cols, int64_t i, int64_t c) {
-    return to_f32(*(const T*)(p + (cols ? c * stride + i * 2 : i * stride + c * 2)));
+// Four neighbouring results of row m from column n on: the epilogue and the store.
+template <typename T> __device__ inline void finish4(const DenseArgs& a, int64_t m, int n, f32x4 v) {
+  const auto half4 = [](const unsigned char* p) {
+    const u32x2 h = *(const u32x2*)p;
+    return f32x4{to_f32(T{(uint16_t)(h.x & 0xffffu)}), to_f32(T{(uint16_t)(h.x >> 16)}), to_f32(T{(uint16_t)(h.y & 0xffffu)}),
+                 to_f32(T{(uint16_t)(h.y >> 16)})};
   };
-  const int64_t depth = a.C;
-  for (int64_t c0 = 0; c0 < depth; c0 += kDepth) {
-    for (int i = threadIdx.x; i < kTile * kDepth; i += 256) {
-      const int r = i / kDepth, c = i % kDepth;
-      const bool in = c0 + c < depth;
-      la[c][r] = in && m0 + r < a.M ? at(a.a, a.a_stride, COLS_A, m0 + r, c0 + c) : 0.0f;
-      lb[c][r] = in && n0 + r < a.N ? at(a.b, a.b_stride, COLS_B, n0 + r, c0 + c) : 0.0f;
-    }
-    __syncthreads();
-    for (int c = 0; c < kDepth; ++c)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] += la[c][ty + 16 * i] * lb[c][tx + 16 * j];
-    __syncthreads();
+  const auto put_half = [&](unsigned char* p) {
+    u32x2 o;
+    o.x = from_f32<T>(v[0]).u | (uint32_t)from_f32<T>(v[1]).u << 16;
+    o.y = from_f32<T>(v[2]).u | (uint32_t)from_f32<T>(v[3]).u << 16;
+    *(u32x2*)p = o;
+  };
+  if (a.bias) v += bias4<T>(a, n);
+  if (a.pre) put_half(a.pre + m * a.pre_stride + (int64_t)n * 2);
+  if (a.slope) {
+    const f32x4 z = half4(a.slope + m * a.slope_stride + (int64_t)n * 2);
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = through<decltype(act)::value>(v[i], z[i]);
+    });
+  } else {
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = activation<decltype(act)::value>(v[i]);
+    });
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty + 16 * i;
-      const int n = n0 + tx + 16 * j;
-      if (m >= a.M || n >= a.N) continue;
-      float v = acc[i][j];
-      if (a.bias) v += a.bias_wide ? ((const float*)a.bias)[n] : to_f32(((const T*)a.bias)[n]);
-      if (a.pre) ((T*)(a.pre + m * a.pre_stride))[n] = from_f32<T>(v);
-      const float before = a.slope ? to_f32(((const T*)(a.slope + m * a.slope_stride))[n]) : 0.0f;
-      with_act(a.act, [&](auto act) { v = a.slope ? through<decltype(act)::value>(v, before) : activation<decltype(act)::value>(v); });
-      const unsigned char* res = a.residual + m * a.residual_stride;
-      unsigned char* out = a.out + m * a.out_stride;
-      if (a.out_wide) {
-        ((float*)out)[n] = v + (a.residual ? ((const float*)res)[n] : 0.0f);
-      } else {
-        ((T*)out)[n] = from_f32<T>(v + (a.residual ? to_f32(((const T*)res)[n]) : 0.0f));
-      }
+  if (a.wide) {
+    if (a.residual) v += *(const f32x4*)(a.residual + m * a.residual_stride + (int64_t)n * 4);
+    *(f32x4*)(a.out + m * a.out_stride + (int64_t)n * 4) = v;
+  } else {
+    if (a.residual) v += half4(a.residual + m * a.residual_stride + (int64_t)n * 2);
+    put_half(a.out + m * a.out_stride + (int64_t)n * 2);
+  }
+}
+
+// ----------------------------------------------------------- few rows
+
+// Up to 64 rows by 32 columns, forward.  The weights' bytes bound it: they go
+// straight to registers, each read once.  A workgroup has one part of the
+// contraction, of which its four wavefronts take turns on 256-byte pieces,
+// loads one piece ahead; their sums are added in LDS in the wavefronts' order.
+// The rows of x come from the L2.
+constexpr int kFewRows = 64, kFewCols = 32, kPiece = 256;
+
+template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a, int64_t m0, int n0, int part, float* sums) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 16, q = lane / 16;
+  const int rows = (int)min((int64_t)(MT * 16), a.R - m0);
+  const int c0 = part * a.chunk, bytes = min(a.chunk, a.C - c0) * 2;   // of the part
+  const int sx = (int)a.a_stride, sw = (int)a.b_stride;
+  const auto rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_stride + (int64_t)c0 * 2), 0, (rows - 1) * sx + bytes, 0x00020000);
+  const auto weights = [&](int u) {
+    const int n = n0 + u * 16, valid = max(min(16, a.N - n), 0);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + (int64_t)n * a.b_stride + (int64_t)c0 * 2), 0,
+                                             valid > 0 ? (valid - 1) * sw + bytes : 0, 0x00020000);
+  };
+  const auto rw0 = weights(0), rw1 = weights(1);
+  struct Piece { u32x4 w[2][4], x[MT][4]; };
+  const auto load = [&](Piece& p, int at) {   // `at`: the piece's first byte
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int byte = at + c * 64 + q * 16;
+      const uint32_t off = byte < bytes ? (uint32_t)byte : 0x60000000u;   // past the part: zero
+      p.w[0][c] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 0);
+      p.w[1][c] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 0);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) p.x[i][c] = __builtin_amdgcn_raw_buffer_load_b128(rx, off + (i * 16 + r) * sx, 0, 0);
     }
+  };
+  f32x4 acc[2][MT] = {};
+  const auto multiply = [&](const Piece& p) {
+    using F = typename Frag<T>::type;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) acc[u][i] = mma(__builtin_bit_cast(F, p.w[u][c]), __builtin_bit_cast(F, p.x[i][c]), acc[u][i]);
+  };
+  constexpr int kTurn = 4 * kPiece;
+  Piece p0, p1;
+  load(p0, wave * kPiece);
+  for (int at = wave * kPiece; at < bytes; at += 2 * kTurn) {
+    load(p1, at + kTurn);
+    multiply(p0);
+    load(p0, at + 2 * kTurn);
+    multiply(p1);
+  }
+  f32x4* each = (f32x4*)sums;   // [wavefront][column tile][row tile][lane]
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) each[((wave * 2 + u) * MT + i) * 64 + lane] = acc[u][i];
+  __syncthreads();
+  for (int f = wave; f < 2 * MT; f += 4) {   // a fragment to a wavefront
+    const int u = f % 2, i = f / 2, n = n0 + u * 16 + q * 4;
+    const int64_t m = m0 + i * 16 + r;
+    f32x4 z = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) z += each[((w * 2 + u) * MT + i) * 64 + lane];
+    if (m >= a.R || n >= a.N) continue;
+    if (a.raw) *(f32x4*)(a.out + part * a.part_bytes + m * a.out_stride + (int64_t)n * 4) = z;
+    else finish4<T>(a, m, n, z);
+  }
+#endif
+}
+
+template <typename T> __global__ void __launch_bounds__(256) linear_few(DenseArgs a) {
+  __shared__ float sums[4 * 2 * (kFewRows / 16) * 64 * 4];
+  const int n0 = blockIdx.x * kFewCols, part = blockIdx.y;
+  const int64_t m0 = (int64_t)blockIdx.z * kFewRows;
+  const int64_t rows = a.R - m0;
+  if (rows <= 16) few_rows<T, 1>(a, m0, n0, part, sums);
+  else if (rows <= 32) few_rows<T, 2>(a, m0, n0, part, sums);
+  else few_rows<T, 4>(a, m0, n0, part, sums);
+}
+
+// The parts' sums [parts][M][N] in their order, and the epilogue: four neighbouring results a thread.
+template <typename T> __global__ void __launch_bounds__(256) linear_join(DenseArgs a, const float* sums, int parts, int64_t M) {
+  const int64_t i = block_index() * 256 + threadIdx.x;
+  const int quads = a.N / 4;
+  if (i >= M * quads) return;
+  const int64_t m = i / quads;
+  f32x4 v = {};
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) v += *(const f32x4*)(sums + (p * M * quads + i) * 4);
+  finish4<T>(a, m, (int)(i - m * quads) * 4, v);
 }
 
 // Through the activation, and columns' sums: workgroup (columns, part).
@@ -104,29 +175,117 @@ template <typename T> __global__ void __launch_bounds__(256) act_grad_kernel(Act
 
 int act_grad_parts(int64_t R) { return (int)std::min<int64_t>(R, 256); }
 
-}  // namespace
+// How a product is computed, from its sizes alone: M rows and N columns of results, a contraction of C.
+enum LinearKind { kFew, kTiles128, kTiles256 };
+struct LinearPlan {
+  LinearKind kind;
+  int parts;
+  int64_t chunk;   // of the contraction: a part's values
+};
 
-size_t linear_workspace(int mode, int64_t R, int32_t N, int32_t K) { return 0; }
+LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
+  const int64_t M = mode == kExpertGradW ? N_ : R, N = mode == kExpertForward ? N_ : K;
+  const int64_t C = mode == kExpertForward ? K : mode == kExpertGradX ? N_ : R;
+  const auto ceil_of = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  LinearPlan p{kTiles256, 1, std::max<int64_t>(C, 1)};
+  int64_t tiles, unit;
+  if (mode == kExpertForward && M <= 128) {
+    p.kind = kFew;
+    tiles = ceil_of(M, kFewRows) * ceil_of(N, kFewCols);
+    unit = 512;
+  } else {
+    const int64_t small = ceil_of(M, 128) * ceil_of(N, 128);
+    if (small <= kCus * 5 / 2) p.kind = kTiles128;
+    tiles = p.kind == kTiles128 ? small : ceil_of(M, 256) * ceil_of(N, 256);
+    unit = 256;
+  }
+  const int64_t parts = std::min<int64_t>(p.kind == kTiles256 ? 1 : 2 * kCus / std::max<int64_t>(tiles, 1), C / unit);
+  if (parts > 1) {
+    p.chunk = ceil_of(ceil_of(C, parts), 64) * 64;
+    p.parts = (int)ceil_of(C, p.chunk);
+  }
+  return p;
+}
 
-vp_status launch_linear(const LinearLaunch& p, void* stream) {
-  const LinearArgs a{(const unsigned char*)p.a, (const unsigned char*)p.b, p.a_stride, p.b_stride,
-                     p.mode == kExpertGradW ? p.N : p.R,
-                     p.mode == kExpertForward ? p.N : p.K,
-                     p.mode == kExpertForward ? p.K : p.mode == kExpertGradX ? p.N : (int32_t)p.R,
-                     p.bias, p.bias_dtype == VP_F32, p.act, (const unsigned char*)p.residual, (const unsigned char*)p.slope,
-                     p.residual_stride, p.slope_stride, (unsigned char*)p.out, (unsigned char*)p.pre,
-                     p.out_dtype == VP_F32, p.out_stride, p.pre_stride};
-  const dim3 grid((unsigned)((a.M + kTile - 1) / kTile), (unsigned)((a.N + kTile - 1) / kTile));
-  const auto run = [&](auto t) {
-    using T = decltype(t);
-    if (p.mode == kExpertForward) hipLaunchKernelGGL((linear_simple<T, false, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
-    else if (p.mode == kExpertGradX) hipLaunchKernelGGL((linear_simple<T, false, true>), grid, dim3(256), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((linear_simple<T, true, true>), grid, dim3(256), 0, (hipStream_t)stream, a);
-  };
-  if (p.dtype == VP_BF16) run(Bf16{});
-  else run(F16{});
+template <typename T, int MODE, int WM, int WN, int MT, int NT> vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
+  constexpr int BM = WM * MT * 16, BN = WN * NT * 16;
+  const int64_t mt = ((MODE == kGradW ? a.M : a.R) + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
+  const int64_t tiles = mt * nt * a.parts;
+  if (tiles >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
+  int64_t per = MODE == kGradW ? (mt * nt + 7) / 8 * a.parts : (tiles + 7) / 8;
+  per = std::min<int64_t>(per, kCus / 8 * (BM == 128 ? 2 : 1));
+  hipLaunchKernelGGL((product_tiled<T, MODE, false, WM, WN, MT, NT, DenseArgs>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "dense product launch failed");
   return VP_OK;
+}
+
+template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPlan& p, float* ws, hipStream_t s) {
+  const DenseArgs whole = a;
+  const int64_t M = MODE == kGradW ? a.M : a.R;
+  a.parts = a.L = p.parts;
+  a.chunk = (int32_t)p.chunk;
+  if (p.parts > 1) {   // raw sums to the workspace
+    a.raw = a.wide = true;
+    a.out = (unsigned char*)ws;
+    a.out_stride = (int64_t)a.N * 4;
+    a.part_bytes = M * a.out_stride;
+    a.pre = nullptr;
+  }
+  vp_status st = VP_OK;
+  if (p.kind == kFew) {
+    if constexpr (MODE == kForward) {
+      const dim3 grid((unsigned)((a.N + kFewCols - 1) / kFewCols), (unsigned)p.parts, (unsigned)((M + kFewRows - 1) / kFewRows));
+      hipLaunchKernelGGL(linear_few<T>, grid, dim3(256), 0, s, a);
+      if (hipGetLastError() != hipSuccess) st = set_error(VP_ERR_HIP, "dense product launch failed");
+    }
+  } else {
+    st = p.kind == kTiles128 ? launch_dense_tiled<T, MODE, 2, 2, 4, 4>(a, s) : launch_dense_tiled<T, MODE, 2, 4, 8, 4>(a, s);
+  }
+  if (st != VP_OK || p.parts == 1) return st;
+  hipLaunchKernelGGL(linear_join<T>, grid_of((M * (a.N / 4) + 255) / 256), dim3(256), 0, s, whole, (const float*)ws, p.parts, M);
+  if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "dense product launch failed");
+  return VP_OK;
+}
+
+}  // namespace
+
+size_t linear_workspace(int mode, int64_t R, int32_t N, int32_t K) {
+  const LinearPlan p = plan_of(mode, R, N, K);
+  const int64_t results = mode == kExpertForward ? R * N : mode == kExpertGradX ? R * K : (int64_t)N * K;
+  return p.parts > 1 ? (size_t)(p.parts * results * 4) : 0;
+}
+
+vp_status launch_linear(const LinearLaunch& p, void* stream) {
+  DenseArgs a{};
+  a.a = (const unsigned char*)p.a;
+  a.b = (const unsigned char*)p.b;
+  a.a_stride = p.a_stride;
+  a.b_stride = p.b_stride;
+  a.R = p.R;
+  a.M = p.N;
+  a.N = p.mode == kExpertForward ? p.N : p.K;
+  a.C = p.mode == kExpertForward ? p.K : p.N;   // (grad w's is R)
+  a.bias = p.bias;
+  a.bias_wide = p.bias_dtype == VP_F32;
+  a.act = p.act;
+  a.residual = (const unsigned char*)p.residual;
+  a.residual_stride = p.residual_stride;
+  a.slope = (const unsigned char*)p.slope;
+  a.slope_stride = p.slope_stride;
+  a.out = (unsigned char*)p.out;
+  a.out_stride = p.out_stride;
+  a.wide = p.out_dtype == VP_F32;
+  a.pre = (unsigned char*)p.pre;
+  a.pre_stride = p.pre_stride;
+  const LinearPlan plan = plan_of(p.mode, p.R, p.N, p.K);
+  const hipStream_t s = (hipStream_t)stream;
+  const auto run = [&](auto t) {
+    using T = decltype(t);
+    if (p.mode == kExpertForward) return launch_as<T, kForward>(a, plan, (float*)p.ws, s);
+    if (p.mode == kExpertGradX) return launch_as<T, kGradX>(a, plan, (float*)p.ws, s);
+    return launch_as<T, kGradW>(a, plan, (float*)p.ws, s);
+  };
+  return p.dtype == VP_BF16 ? run(Bf16{}) : run(F16{});
 }
 
 size_t act_grad_workspace(int64_t R, int64_t N) { return (size_t)act_grad_parts(R) * N * 4; }
