@@ -10,6 +10,7 @@
 
 #include "internal.h"
 #include "numeric.h"
+#include "rows.h"
 
 namespace vp {
 namespace {
@@ -17,7 +18,8 @@ namespace {
 constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
 
 struct DropoutArgs {
-  int64_t T, H;
+  int64_t T;
+  int32_t H, pieces;   // 16-byte pieces of a row
   const unsigned char *x, *residual;
   int64_t x_stride, residual_stride, out_stride;
   unsigned char* out;
@@ -39,20 +41,53 @@ __device__ inline uint64_t stream_key(const DropoutArgs& a) {
   return mix((mix(a.seed + kGamma) ^ step) + kGamma);
 }
 
-template <typename T> __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
+constexpr int kThreads = 256, kAhead = 4;   // pieces of a thread whose loads are issued together
+
+// LANES threads to a row.
+template <typename T, int LANES, bool RES> __global__ void __launch_bounds__(kThreads) dropout_kernel(DropoutArgs a) {
+  constexpr int n = Vec<T>::n;
   const uint64_t key = stream_key(a);
-  const int64_t t = block_index(), words = (a.H + 3) / 4;
+  const int64_t t = block_index() * (kThreads / LANES) + threadIdx.x / LANES;
   if (t >= a.T) return;
   const T *x = (const T*)(a.x + t * a.x_stride), *res = (const T*)(a.residual + t * a.residual_stride);
   T* out = (T*)(a.out + t * a.out_stride);
-  for (int64_t w = threadIdx.x; w < words; w += 256) {
-    const uint64_t bits = mix(key + (uint64_t)(t * words + w + 1) * kGamma);
-    for (int64_t c = w * 4; c < std::min(w * 4 + 4, a.H); ++c) {
-      float v = (uint32_t)(bits >> (16 * (c % 4)) & 0xffff) >= a.least ? to_f32(x[c]) * a.scale : 0.0f;
-      if (a.residual) v += to_f32(res[c]);
-      out[c] = from_f32<T>(v);
+  const uint64_t first = key + (uint64_t)(t * ((a.H + 3) / 4) + 1) * kGamma;   // of the row's first word
+  for (int j0 = threadIdx.x % LANES; j0 < a.pieces; j0 += LANES * kAhead) {
+    u32x4 v[kAhead], r[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int c = (j0 + i * LANES) * n;
+      v[i] = load_piece(x + c, a.H - c);
+      if constexpr (RES) r[i] = load_piece(res + c, a.H - c);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int c = (j0 + i * LANES) * n;
+      if (c >= a.H) break;
+      float f[n], g[n];
+      unpack16<T>(v[i], f);
+      if constexpr (RES) unpack16<T>(r[i], g);
+#pragma unroll
+      for (int k = 0; k < n / 4; ++k) {
+        const uint64_t bits = mix(first + (uint64_t)(uint32_t)(c / 4 + k) * kGamma);
+        const uint32_t half[2] = {(uint32_t)bits, (uint32_t)(bits >> 32)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t field = e % 2 ? half[e / 2] >> 16 : half[e / 2] & 0xffffu;
+          const float y = field >= a.least ? f[4 * k + e] * a.scale : 0.0f;
+          f[4 * k + e] = RES ? y + g[4 * k + e] : y;
+        }
+      }
+      store_piece(out + c, pack16<T>(f), a.H - c);
     }
   }
+}
+
+template <typename T, int LANES> void launch_as(const DropoutArgs& a, hipStream_t s) {
+  constexpr int rows = kThreads / LANES;
+  const dim3 grid = grid_of((a.T + rows - 1) / rows);
+  if (a.residual) hipLaunchKernelGGL((dropout_kernel<T, LANES, true>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((dropout_kernel<T, LANES, false>), grid, dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -60,11 +95,15 @@ template <typename T> __global__ void __launch_bounds__(256) dropout_kernel(Drop
 vp_status launch_dropout(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, uint32_t least,
                          uint64_t seed, const int64_t* step, const void* residual, int64_t residual_stride, void* out,
                          int64_t out_stride, void* stream) {
-  const DropoutArgs a{T, H, (const unsigned char*)x, (const unsigned char*)residual, x_stride, residual_stride, out_stride,
-                      (unsigned char*)out, seed, step, least, least < 65536 ? 65536.0f / (float)(65536 - least) : 0.0f};
-  if (dtype == VP_F32) hipLaunchKernelGGL(dropout_kernel<float>, grid_of(T), dim3(256), 0, (hipStream_t)stream, a);
-  else if (dtype == VP_BF16) hipLaunchKernelGGL(dropout_kernel<Bf16>, grid_of(T), dim3(256), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(dropout_kernel<F16>, grid_of(T), dim3(256), 0, (hipStream_t)stream, a);
+  with_type(dtype, [&](auto type) {
+    using E = decltype(type);
+    const DropoutArgs a{T, (int32_t)H, (int32_t)((H + Vec<E>::n - 1) / Vec<E>::n), (const unsigned char*)x,
+                        (const unsigned char*)residual, x_stride, residual_stride, out_stride, (unsigned char*)out, seed, step,
+                        least, least < 65536 ? 65536.0f / (float)(65536 - least) : 0.0f};
+    if (a.pieces <= 16) launch_as<E, 16>(a, (hipStream_t)stream);
+    else if (a.pieces <= 256) launch_as<E, 64>(a, (hipStream_t)stream);
+    else launch_as<E, 256>(a, (hipStream_t)stream);
+  });
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "dropout launch failed");
   return VP_OK;
 }

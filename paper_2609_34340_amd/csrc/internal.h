@@ -262,8 +262,9 @@ struct NormLaunch {
 vp_status launch_layer_norm(const NormLaunch& p, void* stream);
 size_t layer_norm_grad_workspace(int64_t T, int64_t H);
 vp_status launch_layer_norm_grad(const NormLaunch& p, void* stream);
-// Sums `parts` rows of H floats, in their order, into out.
-vp_status launch_column_sums(const float* part, int parts, int64_t H, float* out, void* stream);
+// Sums `parts` rows of `width` floats, in an order of their own; columns below `split` into first, the others into second.
+vp_status launch_column_sums(const float* part, int parts, int64_t width, int64_t split, float* first, float* second,
+                             void* stream);
 vp_status launch_dropout(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, uint32_t least,
                          uint64_t seed, const int64_t* step, const void* residual, int64_t residual_stride, void* out,
                          int64_t out_stride, void* stream);

@@ -12,6 +12,7 @@
 #include "internal.h"
 #include "numeric.h"
 #include "product.h"
+#include "rows.h"
 
 namespace vp {
 namespace {
@@ -147,33 +148,70 @@ template <typename T> __global__ void __launch_bounds__(256) linear_join(DenseAr
   finish4<T>(a, m, (int)(i - m * quads) * 4, v);
 }
 
-// Through the activation, and columns' sums: workgroup (columns, part).
+// Through the activation, and the columns' sums.  A wavefront has 64 pieces of
+// 16 bytes of a row; the workgroup's four take turns on the rows of one part,
+// kAhead rows' loads at a time, and join their columns' sums in LDS.
 struct ActGradArgs {
   const unsigned char *d_y, *pre;
   int64_t d_y_stride, pre_stride, d_pre_stride;
-  int64_t R, N;
-  int32_t act;
+  int64_t R;
+  int32_t N;
   unsigned char* d_pre;
   float* part;   // [parts][N], or null
   int parts;
 };
+constexpr int kActAhead = 4;
 
-template <typename T> __global__ void __launch_bounds__(256) act_grad_kernel(ActGradArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.N) return;
-  float s = 0.0f;
-  with_act(a.act, [&](auto act) {
-    for (int64_t r = blockIdx.y; r < a.R; r += a.parts) {
-      const float d = to_f32(((const T*)(a.d_y + r * a.d_y_stride))[c]);
-      const float v = through<decltype(act)::value>(d, a.pre ? to_f32(((const T*)(a.pre + r * a.pre_stride))[c]) : 0.0f);
-      if (a.d_pre) ((T*)(a.d_pre + r * a.d_pre_stride))[c] = from_f32<T>(v);
-      s += v;
+template <typename T, int ACT> __global__ void __launch_bounds__(256) act_grad_kernel(ActGradArgs a) {
+  constexpr int n = Vec<T>::n;
+  __shared__ float lds[4][64 * n];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int c = ((int)blockIdx.x * 64 + lane) * n, left = a.N - c;
+  const int64_t stride = (int64_t)a.parts * 4;
+  float s[n] = {};
+  for (int64_t r0 = (int64_t)blockIdx.y * 4 + wave; r0 < a.R; r0 += stride * kActAhead) {
+    u32x4 d[kActAhead], z[kActAhead];
+#pragma unroll
+    for (int i = 0; i < kActAhead; ++i) {
+      const int64_t r = r0 + i * stride;
+      const int in = r < a.R ? left : 0;
+      d[i] = load_piece((const T*)(a.d_y + r * a.d_y_stride) + c, in);
+      if constexpr (ACT != VP_ACT_NONE) z[i] = load_piece((const T*)(a.pre + r * a.pre_stride) + c, in);
     }
-  });
-  if (a.part) a.part[(int64_t)blockIdx.y * a.N + c] = s;
+#pragma unroll
+    for (int i = 0; i < kActAhead; ++i) {
+      const int64_t r = r0 + i * stride;
+      if (r >= a.R) break;
+      float f[n], v[n];
+      unpack16<T>(d[i], f);
+      if constexpr (ACT != VP_ACT_NONE) {
+        unpack16<T>(z[i], v);
+#pragma unroll
+        for (int e = 0; e < n; ++e) f[e] = through<ACT>(f[e], v[e]);
+      }
+      if (a.d_pre) store_piece((T*)(a.d_pre + r * a.d_pre_stride) + c, pack16<T>(f), left);
+#pragma unroll
+      for (int e = 0; e < n; ++e) s[e] += f[e];
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int e = 0; e < n; ++e) lds[wave][e * 64 + lane] = s[e];
+  __syncthreads();
+  for (int k = threadIdx.x; k < 64 * n; k += 256) {
+    const int at = ((int)blockIdx.x * 64 + k / n) * n + k % n, l = k % n * 64 + k / n;
+    if (at < a.N) a.part[(int64_t)blockIdx.y * a.N + at] = lds[0][l] + lds[1][l] + lds[2][l] + lds[3][l];
+  }
 }
 
-int act_grad_parts(int64_t R) { return (int)std::min<int64_t>(R, 256); }
+constexpr int kActBlocks = 2048;   // workgroups, about
+
+// Parts of the rows: the columns' workgroups follow from the type, of which the workspace knows nothing, so there are
+// as many as 16-bit rows need.
+int act_grad_parts(int64_t R, int64_t N) {
+  const int64_t columns = (N + 511) / 512;
+  return (int)std::min<int64_t>((R + 3) / 4, std::max<int64_t>(kActBlocks / columns, 1));
+}
 
 // How a product is computed, from its sizes alone: M rows and N columns of results, a contraction of C.
 enum LinearKind { kFew, kTiles128, kTiles256 };
@@ -288,21 +326,24 @@ vp_status launch_linear(const LinearLaunch& p, void* stream) {
   return p.dtype == VP_BF16 ? run(Bf16{}) : run(F16{});
 }
 
-size_t act_grad_workspace(int64_t R, int64_t N) { return (size_t)act_grad_parts(R) * N * 4; }
+size_t act_grad_workspace(int64_t R, int64_t N) { return (size_t)act_grad_parts(R, N) * N * 4; }
 
 vp_status launch_act_grad(const void* d_y, int64_t d_y_stride, const void* pre, int64_t pre_stride, int32_t dtype,
                           int64_t R, int64_t N, int32_t act, void* d_pre, int64_t d_pre_stride, float* d_bias,
                           void* ws, void* stream) {
-  const ActGradArgs a{(const unsigned char*)d_y, (const unsigned char*)pre, d_y_stride, pre_stride, d_pre_stride, R, N, act,
-                      (unsigned char*)d_pre, d_bias ? (float*)ws : nullptr, act_grad_parts(R)};
+  const ActGradArgs a{(const unsigned char*)d_y, (const unsigned char*)pre, d_y_stride, pre_stride, d_pre_stride, R, (int32_t)N,
+                      (unsigned char*)d_pre, d_bias ? (float*)ws : nullptr, act_grad_parts(R, N)};
   if (R > 0) {
-    const dim3 grid((unsigned)((N + 255) / 256), a.parts);
-    if (dtype == VP_F32) hipLaunchKernelGGL(act_grad_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, a);
-    else if (dtype == VP_BF16) hipLaunchKernelGGL(act_grad_kernel<Bf16>, grid, dim3(256), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(act_grad_kernel<F16>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      const dim3 grid((unsigned)((N + 64 * Vec<T>::n - 1) / (64 * Vec<T>::n)), a.parts);
+      with_act(act, [&](auto f) {
+        hipLaunchKernelGGL((act_grad_kernel<T, decltype(f)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
+      });
+    });
     if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "activation gradient launch failed");
   }
-  return d_bias ? launch_column_sums(a.part, a.parts, N, d_bias, stream) : VP_OK;
+  return d_bias ? launch_column_sums(a.part, a.parts, N, N, d_bias, nullptr, stream) : VP_OK;
 }
 
 }  // namespace vp

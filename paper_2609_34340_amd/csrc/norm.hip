@@ -4,49 +4,335 @@
 //   u = (x - m) r, g = d_out w:  d_x = r (g - mean(g) - u mean(g u)) + residual
 //   d_w = sum over rows of d_out u,  d_b = sum over rows of d_out
 //
-// Statistics by two passes over the row: a mean m0, then d = x - m0 with sum(d) and sum(d^2), so that m = m0 + sum(d) / H
-// and the variance is (sum(d^2) - sum(d)^2 / H) / H: nothing large cancels whatever the rows' mean.
+// A row stays in the registers of its lanes (16 of them, a wavefront, or a workgroup), so it is read once; longer rows
+// are read again.  Statistics: every wavefront takes the mean of its values, then their deviations d from it, whose sum
+// corrects the mean and the sum of squares; a workgroup joins its wavefronts' by the formula for two groups' variances
+// (Chan, Golub, LeVeque 1979).  Means are kept as a base and a small shift, so nothing cancels however far from zero the
+// rows lie.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 
 #include "internal.h"
 #include "numeric.h"
+#include "rows.h"
 
 namespace vp {
 namespace {
 
-constexpr int kThreads = 256;
-
 struct NormArgs {
-  int64_t T, H;
+  int64_t T;
+  int32_t H;
   const unsigned char *x, *d_out, *residual;
   const void *weight, *bias;
-  bool wide;   // weight and bias are fp32
   bool center;
   int64_t x_stride, d_out_stride, residual_stride, out_stride;
   unsigned char* out;
   float* stats;
   const float* given;
   float eps;
-  float* part;   // [parts][d_weight, d_bias][H]
-  int parts;
+  float* part;   // gradient: [workgroup][d_weight, d_bias][H], or null
 };
 
-template <typename T> __device__ inline float param(const void* p, bool wide, int64_t c) {
-  return wide ? ((const float*)p)[c] : to_f32(((const T*)p)[c]);
+__device__ inline float plus(float p, float q) { return p + q; }
+
+// n neighbouring parameters, from column c of H on, as they lie in memory.
+template <typename P, int n> struct Params {
+  static constexpr int kVecs = n / Vec<P>::n;
+  u32x4 v[kVecs];
+  __device__ void load(const void* p, int c, int H) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) v[i] = load_piece((const P*)p + c + i * Vec<P>::n, H - c - i * Vec<P>::n);
+  }
+  __device__ void get(float* f) const {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) unpack16<P>(v[i], f + i * Vec<P>::n);
+  }
+};
+
+// LANES lanes to a row (16 or 64; 0: the workgroup), each with up to NV pieces of it.
+template <int LANES> struct RowOf {
+  int lane, lanes, group, groups;   // within the row; rows of the workgroup
+  __device__ RowOf() {
+    lanes = LANES ? LANES : blockDim.x;
+    lane = LANES ? threadIdx.x % LANES : threadIdx.x;
+    group = LANES ? threadIdx.x / LANES : 0;
+    groups = LANES ? blockDim.x / LANES : 1;
+  }
+};
+
+// How many of the row's values the lanes first .. first + 63 hold, of NV pieces of n each.
+template <int NV, int n> __device__ inline int held(int first, int lanes, int H) {
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) sum += min(max(H - (first + i * lanes) * n, 0), 64 * n);
+  return sum;
 }
 
-// Sums of a and b over the workgroup, in every thread.
+constexpr int kMaxWaves = 16;
+
+template <typename T, typename P, int LANES, int NV>
+__global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(NormArgs a) {
+  constexpr int n = Vec<T>::n, kSum = LANES == 16 ? 16 : 64;
+  __shared__ float from[2][3][kMaxWaves];   // base, shift and squares of each wavefront, for two rows in turn
+  const RowOf<LANES> row;
+  const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+  constexpr bool kKeep = NV == 2;   // parameters stay in registers; with four pieces of a lane these would spill
+  Params<P, n> w[kKeep ? NV : 1], b[kKeep ? NV : 1];
+#pragma unroll
+  for (int i = 0; i < (kKeep ? NV : 0); ++i) {
+    const int c = (row.lane + i * row.lanes) * n;
+    if (a.weight) w[i].load(a.weight, c, a.H);
+    if (a.bias) b[i].load(a.bias, c, a.H);
+  }
+  const float count = (float)a.H;
+  // of this wavefront's share of the row
+  const float mine = LANES ? count : (float)held<NV, n>(wave * 64, row.lanes, a.H);
+  const int64_t stride = (int64_t)gridDim.x * gridDim.y * row.groups;
+  int64_t t = block_index() * row.groups + row.group;
+  u32x4 next[NV];
+  const auto fetch = [&](int64_t at) {
+    const T* x = (const T*)(a.x + at * a.x_stride);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (row.lane + i * row.lanes) * n;
+      next[i] = load_piece(x + c, at < a.T ? a.H - c : 0);
+    }
+  };
+  fetch(t);
+  // every group of lanes goes on to the workgroup's last row, for the barriers and the exchanges between lanes
+  for (int64_t t0 = t - row.group, turn = 0; t0 < a.T; t0 += stride, t += stride, ++turn) {
+    u32x4 x[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) x[i] = next[i];
+    fetch(t + stride);
+    float base = 0.0f, s = 0.0f, squares = 0.0f, f[n];
+    if (a.center) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        unpack16<T>(x[i], f);   // zeros past the row's end
+#pragma unroll
+        for (int e = 0; e < n; ++e) base += f[e];
+      }
+      base = across<kSum>(base, plus) / fmaxf(mine, 1.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      unpack16<T>(x[i], f);
+      const int left = a.H - (row.lane + i * row.lanes) * n;
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        const float d = e < left ? f[e] - base : 0.0f;
+        s += d;
+        squares = __builtin_fmaf(d, d, squares);
+      }
+    }
+    squares = across<kSum>(squares, plus);
+    float shift = 0.0f;
+    if (a.center) {
+      s = across<kSum>(s, plus);
+      shift = s / fmaxf(mine, 1.0f);
+      squares -= s * shift;
+    }
+    if constexpr (LANES == 0) {
+      float (*all)[kMaxWaves] = from[turn & 1];
+      if (threadIdx.x % 64 == 0) {
+        all[0][wave] = base;
+        all[1][wave] = shift;
+        all[2][wave] = squares;
+      }
+      __syncthreads();
+      float first = all[0][0], sum = 0.0f, total = 0.0f;
+      for (int i = 0; i < waves; ++i) {
+        sum = __builtin_fmaf((float)held<NV, n>(i * 64, row.lanes, a.H), all[0][i] - first + all[1][i], sum);
+        total += all[2][i];
+      }
+      const float off = sum / count;   // of the row's mean from `first`
+      if (a.center) {
+        for (int i = 0; i < waves; ++i) {
+          const float d = all[0][i] - first + all[1][i] - off;
+          total = __builtin_fmaf((float)held<NV, n>(i * 64, row.lanes, a.H) * d, d, total);
+        }
+      }
+      base = first;
+      shift = a.center ? off : 0.0f;
+      squares = total;
+    }
+    const float r = 1.0f / sqrtf((squares < 0.0f ? 0.0f : squares / count) + a.eps);   // below 0 only by rounding
+    if (t >= a.T) continue;
+    if (a.stats && row.lane == 0) {
+      a.stats[2 * t] = base + shift;
+      a.stats[2 * t + 1] = r;
+    }
+    T* y = (T*)(a.out + t * a.out_stride);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (row.lane + i * row.lanes) * n;
+      if (c >= a.H) break;
+      float p[n];
+      unpack16<T>(x[i], f);
+#pragma unroll
+      for (int e = 0; e < n; ++e) f[e] = (f[e] - base - shift) * r;
+      constexpr auto at = [](int k) { return kKeep ? k : 0; };
+      if (a.weight) {
+        if (!kKeep) w[0].load(a.weight, c, a.H);
+        w[at(i)].get(p);
+#pragma unroll
+        for (int e = 0; e < n; ++e) f[e] *= p[e];
+      }
+      if (a.bias) {
+        if (!kKeep) b[0].load(a.bias, c, a.H);
+        b[at(i)].get(p);
+#pragma unroll
+        for (int e = 0; e < n; ++e) f[e] += p[e];
+      }
+      store_piece(y + c, pack16<T>(f), a.H - c);
+    }
+  }
+}
+
+// Two sums at a time.
 struct Pair { float a, b; };
+__device__ inline Pair wave_sum(Pair v) { return {across<64>(v.a, plus), across<64>(v.b, plus)}; }
+
+// The gradient.  A workgroup's row groups of `waves` wavefronts (or 16 lanes) each run through rows and keep the sums of
+// their columns' d_weight and d_bias in registers; at the end the groups' sums are joined in LDS, and the workgroups' by
+// column_sums_kernel: the same order at every call.
+constexpr int kGradThreads = 512;   // 1024 would leave 128 registers to a lane, and spill
+
+template <typename T, typename P, int LANES, int NV>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int waves) {
+  constexpr int n = Vec<T>::n, kSum = LANES == 16 ? 16 : 64;
+  __shared__ Pair from[2][kGradThreads / 64];
+  __shared__ float sums[kGradThreads * n];
+  const int lanes = LANES ? LANES : waves * 64, group = threadIdx.x / lanes, groups = blockDim.x / lanes;
+  const int lane = threadIdx.x % lanes, wave = threadIdx.x / 64;
+  constexpr bool kKeep = NV == 2;   // the weight stays in registers, and the residual is loaded ahead
+  constexpr auto at = [](int k) { return kKeep ? k : 0; };
+  Params<P, n> w[kKeep ? NV : 1];
+  float dw[NV][n] = {}, db[NV][n] = {};
+#pragma unroll
+  for (int i = 0; i < (kKeep ? NV : 0); ++i)
+    if (a.weight) w[i].load(a.weight, (lane + i * lanes) * n, a.H);
+  const float count = (float)a.H;
+  const int64_t stride = (int64_t)gridDim.x * groups;
+  int64_t t = (int64_t)blockIdx.x * groups + group;
+  u32x4 next_x[NV], next_d[NV], next_r[kKeep ? NV : 1];
+  float next_m, next_s;
+  const auto fetch = [&](int64_t to) {
+    const T *x = (const T*)(a.x + to * a.x_stride), *d = (const T*)(a.d_out + to * a.d_out_stride);
+    const bool in = to < a.T;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * lanes) * n;
+      next_x[i] = load_piece(x + c, in ? a.H - c : 0);
+      next_d[i] = load_piece(d + c, in ? a.H - c : 0);
+      if (kKeep && a.residual) next_r[at(i)] = load_piece((const T*)(a.residual + to * a.residual_stride) + c, in ? a.H - c : 0);
+    }
+    next_m = in ? a.given[2 * to] : 0.0f;
+    next_s = in ? a.given[2 * to + 1] : 0.0f;
+  };
+  fetch(t);
+  for (int64_t t0 = t - group, turn = 0; t0 < a.T; t0 += stride, t += stride, ++turn) {
+    u32x4 x[NV], d[NV], res[kKeep ? NV : 1];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      x[i] = next_x[i];
+      d[i] = next_d[i];
+      if (kKeep) res[at(i)] = next_r[at(i)];
+    }
+    const float m = next_m, r = next_s;
+    fetch(t + stride);
+    float f[n], g[n], p[n];
+    Pair s{0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int left = a.H - (lane + i * lanes) * n;
+      unpack16<T>(x[i], f);
+      unpack16<T>(d[i], g);
+      if (a.weight) {
+        if (!kKeep) w[0].load(a.weight, (lane + i * lanes) * n, a.H);
+        w[at(i)].get(p);
+      }
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        const float u = e < left ? (f[e] - m) * r : 0.0f;
+        dw[i][e] = __builtin_fmaf(g[e], u, dw[i][e]);
+        db[i][e] += g[e];
+        const float v = a.weight ? g[e] * p[e] : g[e];
+        s.a += v;
+        s.b = __builtin_fmaf(v, u, s.b);
+      }
+    }
+    s = {across<kSum>(s.a, plus), across<kSum>(s.b, plus)};
+    if constexpr (LANES == 0) {
+      Pair* all = from[turn & 1];
+      if (threadIdx.x % 64 == 0) all[wave] = s;
+      __syncthreads();
+      s = {0.0f, 0.0f};
+      for (int i = group * waves; i < (group + 1) * waves; ++i) {
+        s.a += all[i].a;
+        s.b += all[i].b;
+      }
+    }
+    if (t >= a.T) continue;
+    const float mg = a.center ? s.a / count : 0.0f, mgu = s.b / count;
+    T* out = (T*)(a.out + t * a.out_stride);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * lanes) * n;
+      if (c >= a.H) break;
+      unpack16<T>(x[i], f);
+      unpack16<T>(d[i], g);
+      if (a.weight) {
+        if (!kKeep) w[0].load(a.weight, c, a.H);
+        w[at(i)].get(p);
+#pragma unroll
+        for (int e = 0; e < n; ++e) g[e] *= p[e];
+      }
+#pragma unroll
+      for (int e = 0; e < n; ++e) f[e] = r * (g[e] - mg - (f[e] - m) * r * mgu);
+      if (a.residual) {
+        if (!kKeep) res[0] = load_piece((const T*)(a.residual + t * a.residual_stride) + c, a.H - c);
+        unpack16<T>(res[at(i)], g);
+#pragma unroll
+        for (int e = 0; e < n; ++e) f[e] += g[e];
+      }
+      store_piece(out + c, pack16<T>(f), a.H - c);
+    }
+  }
+  if (!a.part) return;
+  const auto join = [&](float (&mine)[NV][n], float* to) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < n; ++e) sums[e * blockDim.x + threadIdx.x] = mine[i][e];   // [element][group][lane]
+      __syncthreads();
+      for (int k = threadIdx.x; k < lanes * n; k += blockDim.x) {
+        const int e = k / lanes, l = k % lanes, c = (l + i * lanes) * n + e;
+        float s = 0.0f;
+        for (int q = 0; q < groups; ++q) s += sums[e * blockDim.x + q * lanes + l];
+        if (c < a.H) to[c] = s;
+      }
+    }
+  };
+  float* part = a.part + (int64_t)blockIdx.x * 2 * a.H;
+  join(dw, part);
+  join(db, part + a.H);
+}
+
+// ------------------------------------------------------------- long rows
+
+// Rows that no workgroup's registers hold: read again for every step, from the L2 as a rule.
+constexpr int kLong = 1024;
+
 __device__ inline Pair block_sum(Pair v, Pair* lds) {
-  const auto add = [](float p, float q) { return p + q; };
-  v.a = across<64>(v.a, add);
-  v.b = across<64>(v.b, add);
+  v = wave_sum(v);
   if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
   __syncthreads();
   Pair s{0.0f, 0.0f};
-  for (int w = 0; w < kThreads / 64; ++w) {
+  for (int w = 0; w < kLong / 64; ++w) {
     s.a += lds[w].a;
     s.b += lds[w].b;
   }
@@ -54,97 +340,198 @@ __device__ inline Pair block_sum(Pair v, Pair* lds) {
   return s;
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
-  __shared__ Pair lds[kThreads / 64];
+template <typename T, typename P> __global__ void __launch_bounds__(kLong) norm_long_kernel(NormArgs a) {
+  constexpr int n = Vec<T>::n;
+  __shared__ Pair lds[kLong / 64];
   const int64_t t = block_index();
   if (t >= a.T) return;
   const T* x = (const T*)(a.x + t * a.x_stride);
   T* y = (T*)(a.out + t * a.out_stride);
-  const float n = (float)a.H;
+  const float count = (float)a.H;
+  const auto each = [&](auto f) {   // f(column, values, how many of them)
+    for (int c = threadIdx.x * n; c < a.H; c += kLong * n) {
+      float v[n];
+      unpack16<T>(load_piece(x + c, a.H - c), v);
+      f(c, v, a.H - c);
+    }
+  };
   float m = 0.0f;
   if (a.center) {
     Pair s{0.0f, 0.0f};
-    for (int64_t c = threadIdx.x; c < a.H; c += kThreads) s.a += to_f32(x[c]);
-    m = block_sum(s, lds).a / n;
+    each([&](int, const float* v, int) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) s.a += v[e];
+    });
+    m = block_sum(s, lds).a / count;
   }
   Pair s{0.0f, 0.0f};
-  for (int64_t c = threadIdx.x; c < a.H; c += kThreads) {
-    const float d = to_f32(x[c]) - m;
-    s.a += d;
-    s.b += d * d;
-  }
+  each([&](int, const float* v, int left) {
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      const float d = e < left ? v[e] - m : 0.0f;
+      s.a += d;
+      s.b = __builtin_fmaf(d, d, s.b);
+    }
+  });
   s = block_sum(s, lds);
-  const float shift = a.center ? s.a / n : 0.0f;
-  const float left = s.b - s.a * shift;   // never below 0 but by rounding
-  const float r = 1.0f / sqrtf((left < 0.0f ? 0.0f : left / n) + a.eps);
+  const float shift = a.center ? s.a / count : 0.0f, squares = s.b - s.a * shift;
+  const float r = 1.0f / sqrtf((squares < 0.0f ? 0.0f : squares / count) + a.eps);
   if (a.stats && threadIdx.x == 0) {
     a.stats[2 * t] = m + shift;
     a.stats[2 * t + 1] = r;
   }
-  for (int64_t c = threadIdx.x; c < a.H; c += kThreads) {
-    float v = (to_f32(x[c]) - m - shift) * r;
-    if (a.weight) v *= param<T>(a.weight, a.wide, c);
-    if (a.bias) v += param<T>(a.bias, a.wide, c);
-    y[c] = from_f32<T>(v);
-  }
+  each([&](int c, float* v, int left) {
+    Params<P, n> p;
+    float f[n];
+#pragma unroll
+    for (int e = 0; e < n; ++e) v[e] = (v[e] - m - shift) * r;
+    if (a.weight) {
+      p.load(a.weight, c, a.H);
+      p.get(f);
+#pragma unroll
+      for (int e = 0; e < n; ++e) v[e] *= f[e];
+    }
+    if (a.bias) {
+      p.load(a.bias, c, a.H);
+      p.get(f);
+#pragma unroll
+      for (int e = 0; e < n; ++e) v[e] += f[e];
+    }
+    store_piece(y + c, pack16<T>(v), left);
+  });
 }
 
-// Rows' shares of d_weight and d_bias: workgroup (columns, part).
-template <typename T> __global__ void __launch_bounds__(kThreads) norm_params_kernel(NormArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (c >= a.H) return;
-  float dw = 0.0f, db = 0.0f;
-  for (int64_t t = blockIdx.y; t < a.T; t += a.parts) {
-    const float d = to_f32(((const T*)(a.d_out + t * a.d_out_stride))[c]);
-    dw += d * ((to_f32(((const T*)(a.x + t * a.x_stride))[c]) - a.given[2 * t]) * a.given[2 * t + 1]);
-    db += d;
-  }
-  a.part[(int64_t)blockIdx.y * a.H + c] = dw;
-  a.part[((int64_t)a.parts + blockIdx.y) * a.H + c] = db;
-}
-
-template <typename T> __global__ void __launch_bounds__(kThreads) norm_grad_kernel(NormArgs a) {
-  __shared__ Pair lds[kThreads / 64];
+// d_x of a long row.
+template <typename T, typename P> __global__ void __launch_bounds__(kLong) norm_grad_long_kernel(NormArgs a) {
+  constexpr int n = Vec<T>::n;
+  __shared__ Pair lds[kLong / 64];
   const int64_t t = block_index();
   if (t >= a.T) return;
   const T *x = (const T*)(a.x + t * a.x_stride), *d = (const T*)(a.d_out + t * a.d_out_stride);
-  const float m = a.given[2 * t], r = a.given[2 * t + 1], n = (float)a.H;
-  const auto grad = [&](int64_t c) { return to_f32(d[c]) * (a.weight ? param<T>(a.weight, a.wide, c) : 1.0f); };
+  const float m = a.given[2 * t], r = a.given[2 * t + 1], count = (float)a.H;
+  const auto each = [&](auto f) {   // f(column, u, g, how many of them)
+    for (int c = threadIdx.x * n; c < a.H; c += kLong * n) {
+      float u[n], g[n], p[n];
+      unpack16<T>(load_piece(x + c, a.H - c), u);
+      unpack16<T>(load_piece(d + c, a.H - c), g);
+#pragma unroll
+      for (int e = 0; e < n; ++e) u[e] = (u[e] - m) * r;
+      if (a.weight) {
+        Params<P, n> w;
+        w.load(a.weight, c, a.H);
+        w.get(p);
+#pragma unroll
+        for (int e = 0; e < n; ++e) g[e] *= p[e];
+      }
+      f(c, u, g, a.H - c);
+    }
+  };
   Pair s{0.0f, 0.0f};
-  for (int64_t c = threadIdx.x; c < a.H; c += kThreads) {
-    const float g = grad(c);
-    s.a += g;
-    s.b += g * ((to_f32(x[c]) - m) * r);
-  }
+  each([&](int, const float* u, const float* g, int left) {
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      s.a += g[e];
+      s.b = __builtin_fmaf(g[e], e < left ? u[e] : 0.0f, s.b);
+    }
+  });
   s = block_sum(s, lds);
-  const float mg = a.center ? s.a / n : 0.0f, mgu = s.b / n;
-  for (int64_t c = threadIdx.x; c < a.H; c += kThreads) {
-    float v = r * (grad(c) - mg - (to_f32(x[c]) - m) * r * mgu);
-    if (a.residual) v += to_f32(((const T*)(a.residual + t * a.residual_stride))[c]);
-    ((T*)(a.out + t * a.out_stride))[c] = from_f32<T>(v);
+  const float mg = a.center ? s.a / count : 0.0f, mgu = s.b / count;
+  each([&](int c, float* u, const float* g, int left) {
+    float res[n];
+#pragma unroll
+    for (int e = 0; e < n; ++e) u[e] = r * (g[e] - mg - u[e] * mgu);
+    if (a.residual) {
+      unpack16<T>(load_piece((const T*)(a.residual + t * a.residual_stride) + c, left), res);
+#pragma unroll
+      for (int e = 0; e < n; ++e) u[e] += res[e];
+    }
+    store_piece((T*)(a.out + t * a.out_stride) + c, pack16<T>(u), left);
+  });
+}
+
+// d_weight and d_bias of long rows: a thread takes a piece of the columns and every parts-th row.
+template <typename T> __global__ void __launch_bounds__(256) norm_params_long_kernel(NormArgs a, int parts) {
+  constexpr int n = Vec<T>::n;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * n;
+  if (c >= a.H) return;
+  float dw[n] = {}, db[n] = {};
+  for (int64_t t = blockIdx.y; t < a.T; t += parts) {
+    const float m = a.given[2 * t], r = a.given[2 * t + 1];
+    float x[n], d[n];
+    unpack16<T>(load_piece((const T*)(a.x + t * a.x_stride) + c, a.H - c), x);
+    unpack16<T>(load_piece((const T*)(a.d_out + t * a.d_out_stride) + c, a.H - c), d);
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      dw[e] = __builtin_fmaf(d[e], (x[e] - m) * r, dw[e]);
+      db[e] += d[e];
+    }
+  }
+  float* part = a.part + (int64_t)blockIdx.y * 2 * a.H;
+#pragma unroll
+  for (int e = 0; e < n; ++e) {
+    if (c + e < a.H) {
+      part[c + e] = dw[e];
+      part[a.H + c + e] = db[e];
+    }
   }
 }
 
-__global__ void __launch_bounds__(kThreads) column_sums_kernel(const float* part, int parts, int64_t H, float* out) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (c >= H) return;
-  float s = 0.0f;
-  for (int i = 0; i < parts; ++i) s += part[(int64_t)i * H + c];
-  out[c] = s;
+// ---------------------------------------------------------------- sums over rows
+
+// part [parts][width]: columns below `split` go to first, the others to second (either may be null).  A workgroup has 32
+// columns; a thread sums four of them over every 32nd part, and the threads' sums are added in order.
+constexpr int kSumCols = 32, kSumSlices = 32;
+
+__global__ void __launch_bounds__(256) column_sums_kernel(const float* part, int parts, int64_t width, int64_t split,
+                                                          float* first, float* second) {
+  __shared__ f32x4 lds[kSumSlices][kSumCols / 4];
+  const int quad = threadIdx.x % (kSumCols / 4), slice = threadIdx.x / (kSumCols / 4);
+  const int64_t c = (int64_t)blockIdx.x * kSumCols + quad * 4;
+  f32x4 s = {0, 0, 0, 0};
+  if (c < width) {
+#pragma unroll 4
+    for (int i = slice; i < parts; i += kSumSlices) {
+      const u32x4 v = load_piece(part + (int64_t)i * width + c, width - c);
+      s += __builtin_bit_cast(f32x4, v);
+    }
+  }
+  lds[slice][quad] = s;
+  __syncthreads();
+  if (threadIdx.x >= kSumCols) return;
+  const int64_t at = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
+  if (at >= width) return;
+  float sum = 0.0f;
+  for (int i = 0; i < kSumSlices; ++i) sum += lds[i][threadIdx.x / 4][threadIdx.x % 4];
+  float* to = at < split ? first : second;
+  if (to) to[at < split ? at : at - split] = sum;
 }
 
-int norm_parts(int64_t T) { return (int)std::min<int64_t>(T, 256); }
+// ------------------------------------------------------------------- host
+
+// Lanes of a row and pieces of a lane, from the row's pieces.
+struct NormPlan { int lanes, per; int waves; };   // lanes 0: `waves` wavefronts; per 0: a long row
+NormPlan plan_of(int64_t pieces, bool grad) {
+  const int most = (grad ? kGradThreads : 1024) / 64;   // wavefronts
+  const int64_t two = (pieces + 127) / 128, four = (pieces + 255) / 256;
+  if (pieces <= 32) return {16, 2, 0};
+  if (pieces <= 128) return {64, 2, 0};
+  if (two <= most) return {0, 2, (int)two};
+  if (four <= most) return {0, 4, (int)four};
+  return {0, 0, 0};
+}
+
+constexpr int kCus = 256;
+constexpr int kParts = kCus;   // workgroups of the gradient, at most: registers allow one or two on a CU
 
 NormArgs norm_args(const NormLaunch& p) {
   NormArgs a{};
   a.T = p.T;
-  a.H = p.H;
+  a.H = (int32_t)p.H;
   a.x = (const unsigned char*)p.x;
   a.d_out = (const unsigned char*)p.d_out;
   a.residual = (const unsigned char*)p.residual;
   a.weight = p.weight;
   a.bias = p.bias;
-  a.wide = p.param_dtype == VP_F32;
   a.center = p.center;
   a.x_stride = p.x_stride;
   a.d_out_stride = p.d_out_stride;
@@ -154,59 +541,91 @@ NormArgs norm_args(const NormLaunch& p) {
   a.stats = p.stats;
   a.given = p.given;
   a.eps = p.eps;
-  a.part = (float*)p.ws;
-  a.parts = norm_parts(p.T);
+  a.part = p.d_weight || p.d_bias ? (float*)p.ws : nullptr;
   return a;
 }
 
-template <typename F> void typed(int32_t dtype, F f) {
-  if (dtype == VP_F32) f(float{});
-  else if (dtype == VP_BF16) f(Bf16{});
-  else f(F16{});
+// Calls f with the rows' type and the parameters'.
+template <typename F> void with_types(const NormLaunch& p, F f) {
+  with_type(p.dtype, [&](auto t) {
+    if (p.param_dtype == VP_F32) f(t, float{});
+    else f(t, t);
+  });
+}
+
+// Calls f with the lanes and pieces as types.
+template <typename F> void with_plan(const NormPlan& p, F f) {
+  if (p.lanes == 16) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+  else if (p.lanes == 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+  else if (p.per == 2) f(std::integral_constant<int, 0>{}, std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
 }
 
 }  // namespace
 
-vp_status launch_column_sums(const float* part, int parts, int64_t H, float* out, void* stream) {
-  hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((H + kThreads - 1) / kThreads)), dim3(kThreads), 0, (hipStream_t)stream,
-                     part, parts, H, out);
+vp_status launch_column_sums(const float* part, int parts, int64_t width, int64_t split, float* first, float* second,
+                             void* stream) {
+  hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((width + kSumCols - 1) / kSumCols)), dim3(256), 0, (hipStream_t)stream,
+                     part, parts, width, split, first, second);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "column sum launch failed");
   return VP_OK;
 }
 
 vp_status launch_layer_norm(const NormLaunch& p, void* stream) {
   const NormArgs a = norm_args(p);
-  typed(p.dtype, [&](auto t) {
-    hipLaunchKernelGGL(norm_kernel<decltype(t)>, grid_of(a.T), dim3(kThreads), 0, (hipStream_t)stream, a);
+  const hipStream_t s = (hipStream_t)stream;
+  with_types(p, [&](auto t, auto q) {
+    using T = decltype(t);
+    using P = decltype(q);
+    const NormPlan plan = plan_of((p.H + Vec<T>::n - 1) / Vec<T>::n, false);
+    if (plan.per == 0) {
+      hipLaunchKernelGGL((norm_long_kernel<T, P>), grid_of(a.T), dim3(kLong), 0, s, a);
+      return;
+    }
+    with_plan(plan, [&](auto lanes, auto per) {
+      constexpr int L = decltype(lanes)::value, V = decltype(per)::value;
+      const int threads = L ? 256 : plan.waves * 64, rows = L ? 256 / std::max(L, 1) : 1;
+      // workgroups that keep their parameters over many rows
+      const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, kCus * 2048 / threads);
+      hipLaunchKernelGGL((norm_kernel<T, P, L, V>), grid_of(blocks), dim3(threads), 0, s, a);
+    });
   });
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "norm launch failed");
   return VP_OK;
 }
 
-size_t layer_norm_grad_workspace(int64_t T, int64_t H) { return (size_t)norm_parts(T) * 2 * H * 4; }
+size_t layer_norm_grad_workspace(int64_t T, int64_t H) { return (size_t)std::min<int64_t>(T, kParts) * 2 * H * 4; }
 
 vp_status launch_layer_norm_grad(const NormLaunch& p, void* stream) {
   const NormArgs a = norm_args(p);
-  if (p.d_weight || p.d_bias) {   // before d_x, which may take d_out's place
-    if (a.T > 0) {
-      typed(p.dtype, [&](auto t) {
-        hipLaunchKernelGGL(norm_params_kernel<decltype(t)>, dim3((unsigned)((a.H + kThreads - 1) / kThreads), a.parts),
-                           dim3(kThreads), 0, (hipStream_t)stream, a);
-      });
-    }
-    if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "norm gradient launch failed");
-    vp_status st = VP_OK;
-    if (p.d_weight) st = launch_column_sums(a.part, a.parts, a.H, p.d_weight, stream);
-    if (st == VP_OK && p.d_bias) st = launch_column_sums(a.part + a.parts * a.H, a.parts, a.H, p.d_bias, stream);
-    if (st != VP_OK) return st;
-  }
+  const hipStream_t s = (hipStream_t)stream;
+  int parts = (int)std::min<int64_t>(a.T, kParts);
   if (a.T > 0) {
-    typed(p.dtype, [&](auto t) {
-      hipLaunchKernelGGL(norm_grad_kernel<decltype(t)>, grid_of(a.T), dim3(kThreads), 0, (hipStream_t)stream, a);
+    with_types(p, [&](auto t, auto q) {
+      using T = decltype(t);
+      using P = decltype(q);
+      const int64_t pieces = (p.H + Vec<T>::n - 1) / Vec<T>::n;
+      const NormPlan plan = plan_of(pieces, true);
+      if (plan.per == 0) {
+        if (a.part) {   // before d_x, which may take d_out's place
+          hipLaunchKernelGGL((norm_params_long_kernel<T>), dim3((unsigned)((pieces + 255) / 256), parts), dim3(256), 0, s, a, parts);
+        }
+        hipLaunchKernelGGL((norm_grad_long_kernel<T, P>), grid_of(a.T), dim3(kLong), 0, s, a);
+        return;
+      }
+      with_plan(plan, [&](auto lanes, auto per) {
+        constexpr int L = decltype(lanes)::value, V = decltype(per)::value;
+        const int rows = L ? kGradThreads / std::max(L, 1) : std::max(1, kGradThreads / 64 / plan.waves);
+        const int threads = L ? kGradThreads : rows * plan.waves * 64;
+        parts = (int)std::min<int64_t>((a.T + rows - 1) / rows, kParts);
+        hipLaunchKernelGGL((norm_grad_kernel<T, P, L, V>), dim3(parts), dim3(threads), 0, s, a, plan.waves);
+      });
     });
   }
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "norm gradient launch failed");
-  return VP_OK;
+  return a.part || (a.T == 0 && (p.d_weight || p.d_bias))
+             ? launch_column_sums((const float*)p.ws, parts, 2 * p.H, p.H, p.d_weight, p.d_bias, stream)
+             : VP_OK;
 }
 
 }  // namespace vp
