@@ -55,70 +55,91 @@ template <typename T> __device__ inline void finish4(const DenseArgs& a, int64_t
 
 // ----------------------------------------------------------- few rows
 
-// Up to 64 rows by 32 columns, forward.  The weights' bytes bound it: they go
-// straight to registers, each read once.  A workgroup has one part of the
-// contraction, of which its four wavefronts take turns on 256-byte pieces,
-// loads one piece ahead; their sums are added in LDS in the wavefronts' order.
-// The rows of x come from the L2.
-constexpr int kFewRows = 64, kFewCols = 32, kPiece = 256;
+// Up to 64 rows by 64 columns of one part of the contraction, forward.  The
+// weights' bytes bound it: they go straight to registers, each read once.  The
+// rows of x would be read again for every 16 columns (64 rows by 4096 x 4096:
+// 64 MB from the L2, 7 us), so they go through LDS, a chunk of 256 values at a
+// time: two wavefronts for 32 columns each, and two more for the other half of
+// the chunk, whose sums are added in LDS at the end.  Loads run two chunks
+// ahead.  16-byte piece c of row r lies at place c ^ (r & 15), so that a
+// fragment's 16 rows meet no bank twice.
+constexpr int kFewRows = 64, kFewCols = 64, kFewChunk = 256;
 
-template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a, int64_t m0, int n0, int part, float* sums) {
+template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a, int64_t m0, int n0, int part, unsigned char* lds) {
 #ifdef __HIP_DEVICE_COMPILE__
+  constexpr int kRow = kFewChunk * 2, kBuffer = MT * 16 * kRow, kAhead = 2;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int r = lane % 16, q = lane / 16;
+  const int r = lane % 16, q = lane / 16, group = wave % 2, half = wave / 2;
   const int rows = (int)min((int64_t)(MT * 16), a.R - m0);
   const int c0 = part * a.chunk, bytes = min(a.chunk, a.C - c0) * 2;   // of the part
   const int sx = (int)a.a_stride, sw = (int)a.b_stride;
   const auto rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_stride + (int64_t)c0 * 2), 0, (rows - 1) * sx + bytes, 0x00020000);
   const auto weights = [&](int u) {
-    const int n = n0 + u * 16, valid = max(min(16, a.N - n), 0);
+    const int n = n0 + group * 32 + u * 16, valid = max(min(16, a.N - n), 0);
     return __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + (int64_t)n * a.b_stride + (int64_t)c0 * 2), 0,
                                              valid > 0 ? (valid - 1) * sw + bytes : 0, 0x00020000);
   };
   const auto rw0 = weights(0), rw1 = weights(1);
-  struct Piece { u32x4 w[2][4], x[MT][4]; };
-  const auto load = [&](Piece& p, int at) {   // `at`: the piece's first byte
+  struct Chunk { u32x4 w[2][4], x[2 * MT]; } ahead[kAhead];
+  const int row0 = threadIdx.x / 32, piece = threadIdx.x % 32;   // of x, as this thread brings it
+  const auto load_x = [&](Chunk& k, int at) {   // `at`: the chunk's first byte; past the part: zero
+    const uint32_t off = at + piece * 16 < bytes ? (uint32_t)(at + piece * 16) : 0x60000000u;
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) k.x[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, off + (row0 + 8 * i) * sx, 0, 0);
+  };
+  const auto load_w = [&](Chunk& k, int at) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const int byte = at + c * 64 + q * 16;
-      const uint32_t off = byte < bytes ? (uint32_t)byte : 0x60000000u;   // past the part: zero
-      p.w[0][c] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 0);
-      p.w[1][c] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 0);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) p.x[i][c] = __builtin_amdgcn_raw_buffer_load_b128(rx, off + (i * 16 + r) * sx, 0, 0);
+      const int byte = at + half * (kRow / 2) + c * 64 + q * 16;
+      const uint32_t off = byte < bytes ? (uint32_t)byte : 0x60000000u;
+      k.w[0][c] = __builtin_amdgcn_raw_buffer_load_b128(rw0, off + r * sw, 0, 0);
+      k.w[1][c] = __builtin_amdgcn_raw_buffer_load_b128(rw1, off + r * sw, 0, 0);
     }
   };
   f32x4 acc[2][MT] = {};
-  const auto multiply = [&](const Piece& p) {
+  const auto chunk = [&](Chunk& k, unsigned char* buffer, int at) {
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) {
+      const int row = row0 + 8 * i;
+      *(u32x4*)(buffer + row * kRow + (piece ^ (row & 15)) * 16) = k.x[i];
+    }
+    load_x(k, at + kAhead * kRow);
+    __syncthreads();   // one for each chunk: a wavefront here has read the chunk before the last, whose buffer this was
     using F = typename Frag<T>::type;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < 4; ++c) {
+      u32x4 x[MT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) x[i] = *(const u32x4*)(buffer + (i * 16 + r) * kRow + (((half * 4 + c) * 4 + q) ^ r) * 16);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) acc[u][i] = mma(__builtin_bit_cast(F, p.w[u][c]), __builtin_bit_cast(F, p.x[i][c]), acc[u][i]);
+        for (int u = 0; u < 2; ++u) acc[u][i] = mma(__builtin_bit_cast(F, k.w[u][c]), __builtin_bit_cast(F, x[i]), acc[u][i]);
+    }
+    load_w(k, at + kAhead * kRow);
   };
-  constexpr int kTurn = 4 * kPiece;
-  Piece p0, p1;
-  load(p0, wave * kPiece);
-  for (int at = wave * kPiece; at < bytes; at += 2 * kTurn) {
-    load(p1, at + kTurn);
-    multiply(p0);
-    load(p0, at + 2 * kTurn);
-    multiply(p1);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    load_x(ahead[i], i * kRow);
+    load_w(ahead[i], i * kRow);
   }
-  f32x4* each = (f32x4*)sums;   // [wavefront][column tile][row tile][lane]
+  for (int at = 0; at < bytes; at += kAhead * kRow) {
+    chunk(ahead[0], lds, at);
+    chunk(ahead[1], lds + kBuffer, at + kRow);   // past the part: zeros
+  }
+  __syncthreads();
+  f32x4* each = (f32x4*)lds;   // [wavefront][column tile][row tile][lane]
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int i = 0; i < MT; ++i) each[((wave * 2 + u) * MT + i) * 64 + lane] = acc[u][i];
   __syncthreads();
-  for (int f = wave; f < 2 * MT; f += 4) {   // a fragment to a wavefront
-    const int u = f % 2, i = f / 2, n = n0 + u * 16 + q * 4;
-    const int64_t m = m0 + i * 16 + r;
-    f32x4 z = {};
+  // the two halves' sums: a column tile to a wavefront
 #pragma unroll
-    for (int w = 0; w < 4; ++w) z += each[((w * 2 + u) * MT + i) * 64 + lane];
+  for (int i = 0; i < MT; ++i) {
+    const int n = n0 + group * 32 + half * 16 + q * 4;
+    const int64_t m = m0 + i * 16 + r;
+    const f32x4 z = each[((group * 2 + half) * MT + i) * 64 + lane] + each[(((group + 2) * 2 + half) * MT + i) * 64 + lane];
     if (m >= a.R || n >= a.N) continue;
     if (a.raw) *(f32x4*)(a.out + part * a.part_bytes + m * a.out_stride + (int64_t)n * 4) = z;
     else finish4<T>(a, m, n, z);
@@ -126,14 +147,9 @@ template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a
 #endif
 }
 
-template <typename T> __global__ void __launch_bounds__(256) linear_few(DenseArgs a) {
-  __shared__ float sums[4 * 2 * (kFewRows / 16) * 64 * 4];
-  const int n0 = blockIdx.x * kFewCols, part = blockIdx.y;
-  const int64_t m0 = (int64_t)blockIdx.z * kFewRows;
-  const int64_t rows = a.R - m0;
-  if (rows <= 16) few_rows<T, 1>(a, m0, n0, part, sums);
-  else if (rows <= 32) few_rows<T, 2>(a, m0, n0, part, sums);
-  else few_rows<T, 4>(a, m0, n0, part, sums);
+template <typename T, int MT> __global__ void __launch_bounds__(256, 2) linear_few(DenseArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * MT * 16 * kFewChunk * 2];
+  few_rows<T, MT>(a, (int64_t)blockIdx.z * kFewRows, blockIdx.x * kFewCols, blockIdx.y, lds);
 }
 
 // The parts' sums [parts][M][N] in their order, and the epilogue: four neighbouring results a thread.
@@ -273,7 +289,9 @@ template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPla
   if (p.kind == kFew) {
     if constexpr (MODE == kForward) {
       const dim3 grid((unsigned)((a.N + kFewCols - 1) / kFewCols), (unsigned)p.parts, (unsigned)((M + kFewRows - 1) / kFewRows));
-      hipLaunchKernelGGL(linear_few<T>, grid, dim3(256), 0, s, a);
+      if (M <= 16) hipLaunchKernelGGL((linear_few<T, 1>), grid, dim3(256), 0, s, a);
+      else if (M <= 32) hipLaunchKernelGGL((linear_few<T, 2>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((linear_few<T, 4>), grid, dim3(256), 0, s, a);
       if (hipGetLastError() != hipSuccess) st = set_error(VP_ERR_HIP, "dense product launch failed");
     }
   } else {

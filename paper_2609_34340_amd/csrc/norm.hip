@@ -35,6 +35,8 @@ struct NormArgs {
 };
 
 __device__ inline float plus(float p, float q) { return p + q; }
+// A value that a wavefront's lanes share, so that what follows from it (a row's address) takes scalar registers.
+__device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // n neighbouring parameters, from column c of H on, as they lie in memory.
 template <typename P, int n> struct Params {
@@ -56,7 +58,7 @@ template <int LANES> struct RowOf {
   __device__ RowOf() {
     lanes = LANES ? LANES : blockDim.x;
     lane = LANES ? threadIdx.x % LANES : threadIdx.x;
-    group = LANES ? threadIdx.x / LANES : 0;
+    group = LANES == 16 ? threadIdx.x / 16 : LANES ? same(threadIdx.x / 64) : 0;
     groups = LANES ? blockDim.x / LANES : 1;
   }
 };
@@ -71,12 +73,14 @@ template <int NV, int n> __device__ inline int held(int first, int lanes, int H)
 
 constexpr int kMaxWaves = 16;
 
+constexpr int kWaves = 5;   // wavefronts of a SIMD that the registers are kept to
+
 template <typename T, typename P, int LANES, int NV>
-__global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(NormArgs a) {
+__global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm_kernel(NormArgs a) {
   constexpr int n = Vec<T>::n, kSum = LANES == 16 ? 16 : 64;
   __shared__ float from[2][3][kMaxWaves];   // base, shift and squares of each wavefront, for two rows in turn
   const RowOf<LANES> row;
-  const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+  const int wave = same(threadIdx.x / 64), waves = blockDim.x / 64;
   constexpr bool kKeep = NV == 2;   // parameters stay in registers; with four pieces of a lane these would spill
   Params<P, n> w[kKeep ? NV : 1], b[kKeep ? NV : 1];
 #pragma unroll
@@ -87,7 +91,9 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(NormArgs a) {
   }
   const float count = (float)a.H;
   // of this wavefront's share of the row
-  const float mine = LANES ? count : (float)held<NV, n>(wave * 64, row.lanes, a.H);
+  const int mine = LANES ? a.H : held<NV, n>(wave * 64, row.lanes, a.H);
+  const bool full = mine == kSum * NV * n;   // no lane past the row's end
+  const float each = 1.0f / (float)max(mine, 1);
   const int64_t stride = (int64_t)gridDim.x * gridDim.y * row.groups;
   int64_t t = block_index() * row.groups + row.group;
   u32x4 next[NV];
@@ -102,38 +108,43 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(NormArgs a) {
   fetch(t);
   // every group of lanes goes on to the workgroup's last row, for the barriers and the exchanges between lanes
   for (int64_t t0 = t - row.group, turn = 0; t0 < a.T; t0 += stride, t += stride, ++turn) {
-    u32x4 x[NV];
+    float base = 0.0f, s = 0.0f, squares = 0.0f, d[NV][n];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) x[i] = next[i];
+    for (int i = 0; i < NV; ++i) unpack16<T>(next[i], d[i]);   // zeros past the row's end
     fetch(t + stride);
-    float base = 0.0f, s = 0.0f, squares = 0.0f, f[n];
     if (a.center) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        unpack16<T>(x[i], f);   // zeros past the row's end
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < n; ++e) base += f[e];
+        for (int e = 0; e < n; ++e) base += d[i][e];
+      base = across<kSum>(base, plus) * each;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < n; ++e) d[i][e] -= base;
+      if (!full) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int e = 0; e < n; ++e)
+            if (e >= a.H - (row.lane + i * row.lanes) * n) d[i][e] = 0.0f;
       }
-      base = across<kSum>(base, plus) / fmaxf(mine, 1.0f);
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      unpack16<T>(x[i], f);
-      const int left = a.H - (row.lane + i * row.lanes) * n;
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < n; ++e) {
-        const float d = e < left ? f[e] - base : 0.0f;
-        s += d;
-        squares = __builtin_fmaf(d, d, squares);
+        s += d[i][e];
+        squares = __builtin_fmaf(d[i][e], d[i][e], squares);
       }
-    }
     squares = across<kSum>(squares, plus);
     float shift = 0.0f;
     if (a.center) {
       s = across<kSum>(s, plus);
-      shift = s / fmaxf(mine, 1.0f);
+      shift = s * each;
       squares -= s * shift;
     }
+    const float mine_base = base;
     if constexpr (LANES == 0) {
       float (*all)[kMaxWaves] = from[turn & 1];
       if (threadIdx.x % 64 == 0) {
@@ -147,15 +158,15 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(NormArgs a) {
         sum = __builtin_fmaf((float)held<NV, n>(i * 64, row.lanes, a.H), all[0][i] - first + all[1][i], sum);
         total += all[2][i];
       }
-      const float off = sum / count;   // of the row's mean from `first`
+      const float delta = sum / count;   // of the row's mean from `first`
       if (a.center) {
         for (int i = 0; i < waves; ++i) {
-          const float d = all[0][i] - first + all[1][i] - off;
+          const float d = all[0][i] - first + all[1][i] - delta;
           total = __builtin_fmaf((float)held<NV, n>(i * 64, row.lanes, a.H) * d, d, total);
         }
       }
       base = first;
-      shift = a.center ? off : 0.0f;
+      shift = a.center ? delta : 0.0f;
       squares = total;
     }
     const float r = 1.0f / sqrtf((squares < 0.0f ? 0.0f : squares / count) + a.eps);   // below 0 only by rounding
@@ -164,16 +175,16 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(NormArgs a) {
       a.stats[2 * t] = base + shift;
       a.stats[2 * t + 1] = r;
     }
+    const float off = (mine_base - base - shift) * r;   // d is from this wavefront's mean
     T* y = (T*)(a.out + t * a.out_stride);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (row.lane + i * row.lanes) * n;
       if (c >= a.H) break;
-      float p[n];
-      unpack16<T>(x[i], f);
-#pragma unroll
-      for (int e = 0; e < n; ++e) f[e] = (f[e] - base - shift) * r;
+      float f[n], p[n];
       constexpr auto at = [](int k) { return kKeep ? k : 0; };
+#pragma unroll
+      for (int e = 0; e < n; ++e) f[e] = __builtin_fmaf(d[i][e], r, off);
       if (a.weight) {
         if (!kKeep) w[0].load(a.weight, c, a.H);
         w[at(i)].get(p);
@@ -205,8 +216,9 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int
   constexpr int n = Vec<T>::n, kSum = LANES == 16 ? 16 : 64;
   __shared__ Pair from[2][kGradThreads / 64];
   __shared__ float sums[kGradThreads * n];
-  const int lanes = LANES ? LANES : waves * 64, group = threadIdx.x / lanes, groups = blockDim.x / lanes;
-  const int lane = threadIdx.x % lanes, wave = threadIdx.x / 64;
+  const int wave = same(threadIdx.x / 64);
+  const int lanes = LANES ? LANES : waves * 64, groups = blockDim.x / lanes;
+  const int group = LANES == 16 ? threadIdx.x / 16 : LANES ? wave : wave / waves, lane = threadIdx.x - group * lanes;
   constexpr bool kKeep = NV == 2;   // the weight stays in registers, and the residual is loaded ahead
   constexpr auto at = [](int k) { return kKeep ? k : 0; };
   Params<P, n> w[kKeep ? NV : 1];
@@ -217,56 +229,61 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int
   const float count = (float)a.H;
   const int64_t stride = (int64_t)gridDim.x * groups;
   int64_t t = (int64_t)blockIdx.x * groups + group;
-  u32x4 next_x[NV], next_d[NV], next_r[kKeep ? NV : 1];
-  float next_m, next_s;
-  const auto fetch = [&](int64_t to) {
-    const T *x = (const T*)(a.x + to * a.x_stride), *d = (const T*)(a.d_out + to * a.d_out_stride);
-    const bool in = to < a.T;
+  // Two rows ahead where registers allow: one row's arithmetic is shorter than a load.
+  constexpr int kAhead = kKeep ? 2 : 1;
+  struct Row { u32x4 x[NV], d[NV], res[kKeep ? NV : 1]; float m, r; } next[kAhead];
+  const auto fetch = [&](Row& to, int64_t at_row) {
+    const T *x = (const T*)(a.x + at_row * a.x_stride), *d = (const T*)(a.d_out + at_row * a.d_out_stride);
+    const bool in = at_row < a.T;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * lanes) * n;
-      next_x[i] = load_piece(x + c, in ? a.H - c : 0);
-      next_d[i] = load_piece(d + c, in ? a.H - c : 0);
-      if (kKeep && a.residual) next_r[at(i)] = load_piece((const T*)(a.residual + to * a.residual_stride) + c, in ? a.H - c : 0);
+      to.x[i] = load_piece(x + c, in ? a.H - c : 0);
+      to.d[i] = load_piece(d + c, in ? a.H - c : 0);   // zeros past the row's end
+      if (kKeep && a.residual) to.res[at(i)] = load_piece((const T*)(a.residual + at_row * a.residual_stride) + c, in ? a.H - c : 0);
     }
-    next_m = in ? a.given[2 * to] : 0.0f;
-    next_s = in ? a.given[2 * to + 1] : 0.0f;
+    to.m = in ? a.given[2 * at_row] : 0.0f;
+    to.r = in ? a.given[2 * at_row + 1] : 0.0f;
   };
-  fetch(t);
-  for (int64_t t0 = t - group, turn = 0; t0 < a.T; t0 += stride, t += stride, ++turn) {
-    u32x4 x[NV], d[NV], res[kKeep ? NV : 1];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(next[i], t + i * stride);
+  int turn = 0;
+  const auto one_row = [&](Row& row) {
+    const float m = row.m, r = row.r;
+    float u[NV][n], g[NV][n], p[n];
+    u32x4 res[kKeep ? NV : 1];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      x[i] = next_x[i];
-      d[i] = next_d[i];
-      if (kKeep) res[at(i)] = next_r[at(i)];
+      unpack16<T>(row.x[i], u[i]);
+      unpack16<T>(row.d[i], g[i]);
+      if (kKeep) res[at(i)] = row.res[at(i)];
     }
-    const float m = next_m, r = next_s;
-    fetch(t + stride);
-    float f[n], g[n], p[n];
+    fetch(row, t + kAhead * stride);
     Pair s{0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int left = a.H - (lane + i * lanes) * n;
-      unpack16<T>(x[i], f);
-      unpack16<T>(d[i], g);
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        u[i][e] = (u[i][e] - m) * r;
+        dw[i][e] = __builtin_fmaf(g[i][e], u[i][e], dw[i][e]);
+        db[i][e] += g[i][e];
+      }
       if (a.weight) {
         if (!kKeep) w[0].load(a.weight, (lane + i * lanes) * n, a.H);
         w[at(i)].get(p);
+#pragma unroll
+        for (int e = 0; e < n; ++e) g[i][e] *= p[e];
       }
 #pragma unroll
       for (int e = 0; e < n; ++e) {
-        const float u = e < left ? (f[e] - m) * r : 0.0f;
-        dw[i][e] = __builtin_fmaf(g[e], u, dw[i][e]);
-        db[i][e] += g[e];
-        const float v = a.weight ? g[e] * p[e] : g[e];
-        s.a += v;
-        s.b = __builtin_fmaf(v, u, s.b);
+        s.a += g[i][e];
+        s.b = __builtin_fmaf(g[i][e], u[i][e], s.b);
       }
     }
     s = {across<kSum>(s.a, plus), across<kSum>(s.b, plus)};
     if constexpr (LANES == 0) {
       Pair* all = from[turn & 1];
+      ++turn;
       if (threadIdx.x % 64 == 0) all[wave] = s;
       __syncthreads();
       s = {0.0f, 0.0f};
@@ -275,30 +292,32 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int
         s.b += all[i].b;
       }
     }
-    if (t >= a.T) continue;
-    const float mg = a.center ? s.a / count : 0.0f, mgu = s.b / count;
+    if (t >= a.T) return;
+    const float mg = a.center ? -r * (s.a / count) : 0.0f, mgu = -r * (s.b / count);
     T* out = (T*)(a.out + t * a.out_stride);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * lanes) * n;
       if (c >= a.H) break;
-      unpack16<T>(x[i], f);
-      unpack16<T>(d[i], g);
-      if (a.weight) {
-        if (!kKeep) w[0].load(a.weight, c, a.H);
-        w[at(i)].get(p);
+      float f[n];
 #pragma unroll
-        for (int e = 0; e < n; ++e) g[e] *= p[e];
-      }
-#pragma unroll
-      for (int e = 0; e < n; ++e) f[e] = r * (g[e] - mg - (f[e] - m) * r * mgu);
+      for (int e = 0; e < n; ++e) f[e] = __builtin_fmaf(r, g[i][e], __builtin_fmaf(mgu, u[i][e], mg));
       if (a.residual) {
         if (!kKeep) res[0] = load_piece((const T*)(a.residual + t * a.residual_stride) + c, a.H - c);
-        unpack16<T>(res[at(i)], g);
+        unpack16<T>(res[at(i)], p);
 #pragma unroll
-        for (int e = 0; e < n; ++e) f[e] += g[e];
+        for (int e = 0; e < n; ++e) f[e] += p[e];
       }
       store_piece(out + c, pack16<T>(f), a.H - c);
+    }
+  };
+  // every group goes on to the workgroup's last row, for the barriers and the exchanges between lanes
+  for (int64_t t0 = t - group; t0 < a.T;) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (t0 < a.T) one_row(next[i]);
+      t0 += stride;
+      t += stride;
     }
   }
   if (!a.part) return;
@@ -489,7 +508,7 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const float* part, int
   const int64_t c = (int64_t)blockIdx.x * kSumCols + quad * 4;
   f32x4 s = {0, 0, 0, 0};
   if (c < width) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = slice; i < parts; i += kSumSlices) {
       const u32x4 v = load_piece(part + (int64_t)i * width + c, width - c);
       s += __builtin_bit_cast(f32x4, v);
@@ -585,8 +604,8 @@ vp_status launch_layer_norm(const NormLaunch& p, void* stream) {
     with_plan(plan, [&](auto lanes, auto per) {
       constexpr int L = decltype(lanes)::value, V = decltype(per)::value;
       const int threads = L ? 256 : plan.waves * 64, rows = L ? 256 / std::max(L, 1) : 1;
-      // workgroups that keep their parameters over many rows
-      const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, kCus * 2048 / threads);
+      // workgroups that keep their parameters over many rows: as many as are resident at once
+      const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, kCus * std::max(4 * (V == 2 ? kWaves : 4) * 64 / threads, 1));
       hipLaunchKernelGGL((norm_kernel<T, P, L, V>), grid_of(blocks), dim3(threads), 0, s, a);
     });
   });
