@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "act.h"
 #include "internal.h"
@@ -237,28 +238,53 @@ struct LinearPlan {
   int64_t chunk;   // of the contraction: a part's values
 };
 
+// Few rows: about one workgroup for each CU.  Measured, us in 1, 2, 4, 8 parts: 1
+// row by 4096 x 4096 19, 13.5, 10.4, 10.5; 61 rows 28, 19, 15.0, 16.7; 1 by 16384
+// x 4096 23, 26, 27, 28; 96 rows by 256 x 7168 in 4, 7, 14, 28 parts 17, 14, 11.6,
+// 11.7.  128 rows by 4096 x 4096 20.0, tiles 20.6.
+//
+// Tiles: the least of an estimate in us.  A step of 64 values takes 0.72 for a
+// 128 x 128 tile alone on its CU, 1.1 for two, 1.65 for a 256 x 256 tile; a round
+// of tiles ends with 3 or 9 for its results; joining parts takes 2.5 and the
+// sums' way out and back at 4 TB/s.  Measured, us (128 / 256 tiles, parts in
+// brackets): 16381 rows by 4096 x 4096 546 / 445; 2048 rows 71 / 96; 512 rows 46
+// [1], 35 [2], 34 [4] / 93 [1], 48 [4]; 256 rows 46 [1], 31 [2], 24 [4], 27 [8];
+// 16384 by 256 x 4096 50 [1], 51 [2] / 99 [1], 67 [4], its weights' gradient 172
+// [1], 58 [4], 54 [8], 65 [16] / 342 [1], 63 [16], its rows' gradient 59 / 70.
 LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
   const int64_t M = mode == kExpertGradW ? N_ : R, N = mode == kExpertForward ? N_ : K;
   const int64_t C = mode == kExpertForward ? K : mode == kExpertGradX ? N_ : R;
   const auto ceil_of = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  LinearPlan p{kTiles256, 1, std::max<int64_t>(C, 1)};
-  int64_t tiles, unit;
-  if (mode == kExpertForward && M <= 128) {
-    p.kind = kFew;
-    tiles = ceil_of(M, kFewRows) * ceil_of(N, kFewCols);
-    unit = 512;
-  } else {
-    const int64_t small = ceil_of(M, 128) * ceil_of(N, 128);
-    if (small <= kCus * 5 / 2) p.kind = kTiles128;
-    tiles = p.kind == kTiles128 ? small : ceil_of(M, 256) * ceil_of(N, 256);
-    unit = 256;
+  LinearPlan best{kTiles256, 1, std::max<int64_t>(C, 1)};
+  const auto in_parts = [&](LinearKind kind, int64_t parts) {
+    LinearPlan p{kind, 1, std::max<int64_t>(C, 1)};
+    if (parts > 1) {
+      p.chunk = ceil_of(ceil_of(C, parts), 64) * 64;
+      p.parts = (int)ceil_of(C, p.chunk);
+    }
+    return p;
+  };
+  if (mode == kExpertForward && M <= 2 * kFewRows) {
+    const int64_t tiles = std::max<int64_t>(ceil_of(M, kFewRows) * ceil_of(N, kFewCols), 1);
+    return in_parts(kFew, std::min(kCus / tiles, C / (2 * kFewChunk)));
   }
-  const int64_t parts = std::min<int64_t>(p.kind == kTiles256 ? 1 : 2 * kCus / std::max<int64_t>(tiles, 1), C / unit);
-  if (parts > 1) {
-    p.chunk = ceil_of(ceil_of(C, parts), 64) * 64;
-    p.parts = (int)ceil_of(C, p.chunk);
+  double least = 0.0;
+  for (const LinearKind kind : {kTiles256, kTiles128}) {
+    const int64_t side = kind == kTiles128 ? 128 : 256, tiles = ceil_of(M, side) * ceil_of(N, side);
+    for (int64_t parts = 1; parts == 1 || (parts <= 64 && C >= 128 * parts); parts *= 2) {
+      const LinearPlan p = in_parts(kind, parts);
+      const double steps = (double)ceil_of(p.chunk, 64), groups = (double)(tiles * p.parts);
+      const double rounds = std::max(1.0, std::ceil(groups / (kind == kTiles128 ? 2 * kCus : kCus)));
+      const double step = kind == kTiles256 ? 1.65 : groups > kCus ? 1.1 : 0.72;
+      double time = rounds * (step * steps + (kind == kTiles128 ? 3.0 : 9.0));
+      if (p.parts > 1) time += 2.5 + (double)p.parts * (double)M * (double)N * 8.0 / 4e6;
+      if (least == 0.0 || time < least) {
+        least = time;
+        best = p;
+      }
+    }
   }
-  return p;
+  return best;
 }
 
 template <typename T, int MODE, int WM, int WN, int MT, int NT> vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {

@@ -617,112 +617,124 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
       }
     }
   };
-  // The epilogue of a dense product, a row of fragments at a time (all of them
-  // through one step after the other would spill).  A lane's four results of
-  // fragment (i, j) are row (wm MT + i) 16 + r, columns (wn NT + j) 16 + 4 q on.
-  // 16-bit operands of the epilogue come as the stores go, 16 bytes a lane, and
-  // are brought to the fragments' places by the same exchange.
+  // The epilogue of a dense product, two neighbouring fragments at a time (all
+  // of them through one step after the other would spill; the bias is what the
+  // sums begin with).  A lane's four results of fragment (i, j) are row (wm MT +
+  // i) 16 + r, columns (wn NT + j) 16 + 4 q on.  16-bit operands of the epilogue
+  // come as the stores go, 16 bytes a lane for two fragments, and are brought to
+  // the fragments' places by the same exchange; their loads run kFar pairs ahead.
   const auto finish = [&](const TileTo& t) {
     if constexpr (kDense) {
       const auto resource = [&](const unsigned char* base, int64_t stride, int size) {
         return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, base ? (t.rows - 1) * (int)stride + t.cols * size : 0, 0x00020000);
       };
       const auto out = resource(t.out, a.out_stride, a.wide ? 4 : 2);
+      // (the compiler must not know these places: it would compute all rows' offsets before the first tile, and spill)
+      int row0 = wm * MT * 16 + r, quad = q;
+      asm volatile("" : "+v"(row0), "+v"(quad));
       const auto wide_at = [&](int i, int j, int64_t stride) -> uint32_t {   // of 32-bit values
-        const int n = (wn * NT + j) * 16 + q * 4;
-        return n < t.cols ? (uint32_t)(((wm * MT + i) * 16 + r) * (int)stride + n * 4) : 0x60000000u;
+        const int n = (wn * NT + j) * 16 + quad * 4;
+        return n < t.cols ? (uint32_t)(row0 * (int)stride + n * 4 + i * 16 * (int)stride) : 0x60000000u;
       };
-      const auto put_wide = [&](int i, const f32x4 (&v)[NT]) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[j]), out, wide_at(i, j, a.out_stride), 0, 0);
+      const auto put_wide = [&](int i, int j, const f32x4& v) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), out, wide_at(i, j, a.out_stride), 0, 0);
       };
-      if constexpr (MODE == kGradW) {
+      if (MODE == kGradW || a.raw) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) put_wide(i, acc[i]);
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) put_wide(i, j, acc[i][j]);
         return;
       }
-      const auto half_at = [&](int i, int j, int64_t stride) -> uint32_t {   // of 16-bit values, fragments j and j + 1
-        const int n = (wn * NT + j + (q & 1)) * 16 + (q >> 1) * 8;
-        return n < t.cols ? (uint32_t)(((wm * MT + i) * 16 + r) * (int)stride + n * 2) : 0x60000000u;
+      const auto half_at = [&](int p, int64_t stride) -> uint32_t {   // of pair p's 16-bit values
+        const int i = p / (NT / 2), j = p % (NT / 2) * 2, n = (wn * NT + j + (quad & 1)) * 16 + (quad >> 1) * 8;
+        return n < t.cols ? (uint32_t)(row0 * (int)stride + n * 2 + i * 16 * (int)stride) : 0x60000000u;
       };
-      const auto put_half = [&](const auto& to, int64_t stride, int i, const f32x4 (&v)[NT]) {
+      const auto put_half = [&](const auto& to, int64_t stride, int p, const f32x4 (&v)[2]) {
+        u32x2 h[2];
 #pragma unroll
-        for (int j = 0; j < NT; j += 2) {
-          u32x2 p[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            p[u].x = from_f32<Out>(v[j + u][0]).u | (uint32_t)from_f32<Out>(v[j + u][1]).u << 16;
-            p[u].y = from_f32<Out>(v[j + u][2]).u | (uint32_t)from_f32<Out>(v[j + u][3]).u << 16;
-          }
-          const auto x = __builtin_amdgcn_permlane16_swap(p[0].x, p[1].x, false, false);
-          const auto y = __builtin_amdgcn_permlane16_swap(p[0].y, p[1].y, false, false);
-          const u32x4 o = {x[0], y[0], x[1], y[1]};
-          __builtin_amdgcn_raw_buffer_store_b128(o, to, half_at(i, j, stride), 0, 0);
+        for (int u = 0; u < 2; ++u) {
+          h[u].x = from_f32<Out>(v[u][0]).u | (uint32_t)from_f32<Out>(v[u][1]).u << 16;
+          h[u].y = from_f32<Out>(v[u][2]).u | (uint32_t)from_f32<Out>(v[u][3]).u << 16;
         }
+        const auto x = __builtin_amdgcn_permlane16_swap(h[0].x, h[1].x, false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(h[0].y, h[1].y, false, false);
+        const u32x4 o = {x[0], y[0], x[1], y[1]};
+        __builtin_amdgcn_raw_buffer_store_b128(o, to, half_at(p, stride), 0, 0);
       };
-      const auto get_half = [&](const auto& from, int64_t stride, int i, f32x4 (&v)[NT]) {
+      const auto get_half = [&](const u32x4& o, f32x4 (&v)[2]) {
+        const auto x = __builtin_amdgcn_permlane16_swap(o[0], o[2], false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(o[1], o[3], false, false);
 #pragma unroll
-        for (int j = 0; j < NT; j += 2) {
-          const u32x4 o = __builtin_amdgcn_raw_buffer_load_b128(from, half_at(i, j, stride), 0, 0);
-          const auto x = __builtin_amdgcn_permlane16_swap(o[0], o[2], false, false);
-          const auto y = __builtin_amdgcn_permlane16_swap(o[1], o[3], false, false);
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            v[j + u] = f32x4{to_f32(Out{(uint16_t)(x[u] & 0xffffu)}), to_f32(Out{(uint16_t)(x[u] >> 16)}),
-                             to_f32(Out{(uint16_t)(y[u] & 0xffffu)}), to_f32(Out{(uint16_t)(y[u] >> 16)})};
-        }
+        for (int u = 0; u < 2; ++u)
+          v[u] = f32x4{to_f32(Out{(uint16_t)(x[u] & 0xffffu)}), to_f32(Out{(uint16_t)(x[u] >> 16)}),
+                       to_f32(Out{(uint16_t)(y[u] & 0xffffu)}), to_f32(Out{(uint16_t)(y[u] >> 16)})};
       };
       const auto before = resource(t.pre, a.pre_stride, 2);
       const auto slope = resource(a.slope ? a.slope + t.m0 * a.slope_stride + (int64_t)t.n0 * 2 : nullptr, a.slope_stride, 2);
       const int size = a.wide ? 4 : 2;
       const auto residual = resource(a.residual ? a.residual + t.m0 * a.residual_stride + (int64_t)t.n0 * size : nullptr, a.residual_stride, size);
-      f32x4 bias[NT] = {};
-      if (MODE == kForward && !a.raw && a.bias) {
+      const bool half_residual = a.residual && !a.wide;
+      constexpr int kPairs = MT * NT / 2, kFar = 2;
+      u32x4 far_slope[kFar], far_residual[kFar];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int n = t.n0 + (wn * NT + j) * 16 + q * 4;
-          if (n < a.N) bias[j] = bias4<Out>(a, n);
-        }
+      for (int p = 0; p < kFar; ++p) {
+        if (MODE == kGradX && a.slope) far_slope[p] = __builtin_amdgcn_raw_buffer_load_b128(slope, half_at(p, a.slope_stride), 0, 0);
+        if (half_residual) far_residual[p] = __builtin_amdgcn_raw_buffer_load_b128(residual, half_at(p, a.residual_stride), 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        f32x4 v[NT], z[NT];
+      for (int p = 0; p < kPairs; ++p) {
+        const int i = p / (NT / 2), j = p % (NT / 2) * 2;
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 v[2] = {acc[i][j], acc[i][j + 1]}, z[2];
+        if constexpr (MODE == kForward) {
+          if (t.pre) put_half(before, a.pre_stride, p, v);
+          with_act(a.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) v[j] = acc[i][j] + bias[j];
-        if (!a.raw) {
-          if constexpr (MODE == kForward) {
-            if (t.pre) put_half(before, a.pre_stride, i, v);
-            with_act(a.act, [&](auto act) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int j = 0; j < NT; ++j)
+              for (int c = 0; c < 4; ++c) v[u][c] = activation<decltype(act)::value>(v[u][c]);
+          });
+        } else if (a.slope) {
+          get_half(far_slope[p % kFar], z);
+          if (p + kFar < kPairs) far_slope[p % kFar] = __builtin_amdgcn_raw_buffer_load_b128(slope, half_at(p + kFar, a.slope_stride), 0, 0);
+          with_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[j][c] = activation<decltype(act)::value>(v[j][c]);
-            });
-          } else if (a.slope) {
-            get_half(slope, a.slope_stride, i, z);
-            with_act(a.act, [&](auto act) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[j][c] = through<decltype(act)::value>(v[j][c], z[j][c]);
-            });
-          }
-          if (a.residual) {
-            if (a.wide) {
-#pragma unroll
-              for (int j = 0; j < NT; ++j)
-                z[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(residual, wide_at(i, j, a.residual_stride), 0, 0));
-            } else {
-              get_half(residual, a.residual_stride, i, z);
-            }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) v[j] += z[j];
-          }
+              for (int c = 0; c < 4; ++c) v[u][c] = through<decltype(act)::value>(v[u][c], z[u][c]);
+          });
         }
-        if (a.wide) put_wide(i, v);
-        else put_half(out, a.out_stride, i, v);
+        if (a.wide) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if (a.residual)
+              v[u] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(residual, wide_at(i, j + u, a.residual_stride), 0, 0));
+            put_wide(i, j + u, v[u]);
+          }
+        } else {
+          if (half_residual) {
+            get_half(far_residual[p % kFar], z);
+            if (p + kFar < kPairs) far_residual[p % kFar] = __builtin_amdgcn_raw_buffer_load_b128(residual, half_at(p + kFar, a.residual_stride), 0, 0);
+            v[0] += z[0];
+            v[1] += z[1];
+          }
+          put_half(out, a.out_stride, p, v);
+        }
       }
+    }
+  };
+  // What a tile's sums begin with: zeros, or the bias of their columns.
+  const auto first_sums = [&](const TileTo& t) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      f32x4 v = {0, 0, 0, 0};
+      if constexpr (kDense && MODE == kForward) {
+        const int n = t.n0 + (wn * NT + j) * 16 + q * 4;
+        if (a.bias && !a.raw && n < a.N) v = bias4<Out>(a, n);
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[i][j] = v;
     }
   };
   const auto write = [&](const TileTo& t) {
@@ -774,6 +786,7 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   for (int i = 0; i < MT; ++i) sa[i] = read_power(0, 0, (wm * MT + i) * 16);
 #pragma unroll
   for (int i = 0; i < NT; ++i) sb[i] = read_power(0, 0, BM + (wn * NT + i) * 16);
+  if constexpr (kDense && MODE == kForward) first_sums(cur);
   bool stored = false;
   for (int pos = 0;; ++pos) {
 #pragma unroll
@@ -847,10 +860,14 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
       next = after;
       --begun;
       step = 0;
+      if constexpr (kDense && MODE == kForward) {
+        first_sums(cur);
+      } else {
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+          for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+      }
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last loads end before the LDS is another workgroup's
