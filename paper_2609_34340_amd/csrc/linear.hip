@@ -236,6 +236,8 @@ struct LinearPlan {
   LinearKind kind;
   int parts;
   int64_t chunk;   // of the contraction: a part's values
+  // 128 x 128 tiles of M by N results, at most one for each CU
+  bool alone(int64_t M, int64_t N) const { return ((M + 127) / 128) * ((N + 127) / 128) * parts <= kCus; }
 };
 
 // Few rows: about one workgroup for each CU.  Measured, us in 1, 2, 4, 8 parts: 1
@@ -287,14 +289,18 @@ LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
   return best;
 }
 
-template <typename T, int MODE, int WM, int WN, int MT, int NT> vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
+template <typename T, int MODE, int WM, int WN, int MT, int NT, int STAGES = 2> vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
   constexpr int BM = WM * MT * 16, BN = WN * NT * 16;
   const int64_t mt = ((MODE == kGradW ? a.M : a.R) + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
   const int64_t tiles = mt * nt * a.parts;
   if (tiles >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
   int64_t per = MODE == kGradW ? (mt * nt + 7) / 8 * a.parts : (tiles + 7) / 8;
-  per = std::min<int64_t>(per, kCus / 8 * (BM == 128 ? 2 : 1));
-  hipLaunchKernelGGL((product_tiled<T, MODE, false, WM, WN, MT, NT, DenseArgs>), dim3((unsigned)(per * 8)), dim3(WM * WN * 64), 0, s, a);
+  per = std::min<int64_t>(per, kCus / 8 * (BM == 128 && STAGES == 2 ? 2 : 1));
+  const auto kernel = product_tiled<T, MODE, false, WM, WN, MT, NT, DenseArgs, STAGES>;
+  const int lds = STAGES == 2 ? 0 : STAGES * (BM + BN) * kStep;
+  if (lds && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    return set_error(VP_ERR_HIP, "dense product launch failed");
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(per * 8)), dim3(WM * WN * 64), lds, s, a);
   if (hipGetLastError() != hipSuccess) return set_error(VP_ERR_HIP, "dense product launch failed");
   return VP_OK;
 }
@@ -321,7 +327,9 @@ template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPla
       if (hipGetLastError() != hipSuccess) st = set_error(VP_ERR_HIP, "dense product launch failed");
     }
   } else {
-    st = p.kind == kTiles128 ? launch_dense_tiled<T, MODE, 2, 2, 4, 4>(a, s) : launch_dense_tiled<T, MODE, 2, 4, 8, 4>(a, s);
+    st = p.kind == kTiles256  ? launch_dense_tiled<T, MODE, 2, 4, 8, 4>(a, s)
+         : p.alone(M, a.N) ? launch_dense_tiled<T, MODE, 2, 2, 4, 4, 4>(a, s)
+                           : launch_dense_tiled<T, MODE, 2, 2, 4, 4>(a, s);
   }
   if (st != VP_OK || p.parts == 1) return st;
   hipLaunchKernelGGL(linear_join<T>, grid_of((M * (a.N / 4) + 255) / 256), dim3(256), 0, s, whole, (const float*)ws, p.parts, M);

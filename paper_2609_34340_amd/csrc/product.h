@@ -273,7 +273,12 @@ template <typename Out> struct TileIn : Out {
   int a_left, a_width, b_left, b_width;
 };
 
-// Wavefronts that a SIMD has registers for at least: of the dense products' 128 x 128 tiles two workgroups share a CU.
+// The steps of a kernel that holds more than two come with the launch: knowing their size the compiler would give the one
+// workgroup that a CU then holds both register files, and move sums between them.
+extern __shared__ __attribute__((aligned(1024))) unsigned char more_steps[];
+
+// Wavefronts that a SIMD has registers for at least: of the dense products' 128 x 128 tiles two workgroups share a CU (and
+// with the registers of one, sums move between the two register files).
 template <typename Args> constexpr int waves_of() { return std::is_same_v<Args, DenseArgs> ? 2 : 1; }
 
 // Measured: 32768 rows by 4096 x 4096, bf16 0.83-0.88 ms (1.25-1.33 PFLOP/s; the
@@ -288,9 +293,9 @@ template <typename Args> constexpr int waves_of() { return std::is_same_v<Args, 
 //
 // WM x WN wavefronts, each with MT x NT fragments of 16 x 16 results.  A
 // workgroup takes every gridDim / 8-th tile of its XCD's and runs through
-// their steps as one stream: the loads are two steps ahead, so that the next
+// their steps as one stream: the loads are two steps ahead (STAGES), so that the next
 // tile's first steps arrive while this one's results are written.
-template <typename T, int MODE, bool GATED, int WM, int WN, int MT, int NT, typename Args = ProductArgs>
+template <typename T, int MODE, bool GATED, int WM, int WN, int MT, int NT, typename Args = ProductArgs, int STAGES = 2>
 __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(Args a) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host's pass knows none of the builtins below
   using Out = typename Elem<T>::out;
@@ -301,7 +306,8 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   constexpr int BM = WM * MT * 16, BN = WN * NT * 16, kWaves = WM * WN;
   constexpr int kTileN = GATED ? BN / 2 : BN;   // output columns
   constexpr int kSize = MODE == kGradW ? 4 : 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2][(BM + BN) * kStep];
+  constexpr bool kFixed = STAGES == 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kFixed ? STAGES : 1][kFixed ? (BM + BN) * kStep : 16];
   // 4-bit blocks: the powers of two of four steps, 32 bytes a row, double buffered
   __shared__ __attribute__((aligned(1024))) unsigned char powers[kMx ? 2 : 1][kMx ? (BM + BN) * 32 : 16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -362,7 +368,7 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
           t.b_width = depth * 2;
         }
       }
-      t.steps = max(t.steps, 2);   // steps past the last add zeros
+      t.steps = max(t.steps, STAGES);   // steps past the last add zeros
       t.m0 = m0;
       t.n0 = n0;
       t.out = a.out + part * a.part_bytes + m0 * a.out_stride + (int64_t)n0 * (a.wide ? 4 : 2);
@@ -429,7 +435,7 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     return false;
   };
 
-  // what is loaded, two steps ahead of what is multiplied
+  // what is loaded, STAGES steps ahead of what is multiplied
   Operand<BM, kColsA, kWaves> oa;
   Operand<BN, kColsB, kWaves> ob;
   TileAt ahead;
@@ -437,7 +443,7 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   int load_step = 0, load_group = 0;
   if (!find(load_idx, ahead)) return;
   TileTo cur = ahead, next = ahead, after = ahead;   // of the multiplied tile and those begun since
-  int begun = 0;   // how many of these: a tile has two steps at least, so at most two
+  int begun = 0;   // how many of these: a tile has STAGES steps at least, so at most two
   const auto begin = [&] {
     oa.start(ahead.a, ahead.a_left, ahead.a_width, lane);
     ob.start(ahead.b, ahead.b_left, ahead.b_width, lane);
@@ -466,6 +472,10 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     }
   };
 
+  const auto stage = [&](int pos) -> unsigned char* {
+    if constexpr (kFixed) return lds[pos & 1];
+    else return more_steps + (pos & (STAGES - 1)) * ((BM + BN) * kStep);
+  };
   // places of this lane's fragments in LDS
   const auto chunk = [=](int kk) { return kMx ? 2 * q + kk : 4 * kk + q; };
   uint32_t pa[kColsA ? MT : 1], pb[kColsB ? NT : 1];
@@ -495,10 +505,10 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     }
   };
   const auto read_a = [&](int pos, int kk, int i) {
-    return frag(lds[pos & 1], std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
+    return frag(stage(pos), std::bool_constant<kColsA>{}, std::integral_constant<int, BM>{}, pa[kColsA ? i : 0], i, kk);
   };
   const auto read_b = [&](int pos, int kk, int i) {
-    return frag(lds[pos & 1] + BM * kStep, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
+    return frag(stage(pos) + BM * kStep, std::bool_constant<kColsB>{}, std::integral_constant<int, BN>{}, pb[kColsB ? i : 0], i, kk);
   };
 
   // 4-bit blocks: a load covers 32 rows' powers of four steps, first their
@@ -546,8 +556,8 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   // middle of the step if there are rows enough, else all after it
   constexpr bool kEarly = MT == NT + 4;
   static_assert((kEarly || MT == 4) && kLoadsA == 4 && kLoadsB == 4, "the loads' places among the rows of products");
-  const auto issue_a = [&](int pos, int j) { oa.issue(lds[pos & 1], wave, j); };
-  const auto issue_b = [&](int pos, int j) { ob.issue(lds[pos & 1] + BM * kStep, wave, j); };
+  const auto issue_a = [&](int pos, int j) { oa.issue(stage(pos), wave, j); };
+  const auto issue_b = [&](int pos, int j) { ob.issue(stage(pos) + BM * kStep, wave, j); };
   const auto load = [&](int pos) {
     load_powers();
 #pragma unroll
@@ -773,9 +783,14 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   i32x4 fa[MT], fb0[NT], fb1[NT];
   int sa[MT] = {}, sb[NT] = {};
   int step = 0, group = 0;
+  static_assert(STAGES == 2 || (!kEarly && !kMx && STAGES == 4), "places of the steps ahead");
   load(0);
   load(1);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if constexpr (STAGES == 4) {
+    load(2);
+    load(3);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES == 2 ? 0 : (STAGES - 1) * (kLoadsA + kLoadsB)) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
@@ -788,15 +803,17 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   for (int i = 0; i < NT; ++i) sb[i] = read_power(0, 0, BM + (wn * NT + i) * 16);
   if constexpr (kDense && MODE == kForward) first_sums(cur);
   bool stored = false;
+  // loads that were started after the next step's: of the steps after it, and those of this step's first half
+  constexpr int kYounger = (STAGES - 2) * (kLoadsA + kLoadsB) + (kEarly ? kLoadsB : 0);
   for (int pos = 0;; ++pos) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if (i < NT) fb1[i] = read_b(pos, 1, i);
       if (kEarly && i == NT + 1) {
-        issue_b(pos + 2, 0);
-        issue_b(pos + 2, 1);
+        issue_b(pos + STAGES, 0);
+        issue_b(pos + STAGES, 1);
       } else if (kEarly && i > NT + 1) {
-        issue_b(pos + 2, i - NT);
+        issue_b(pos + STAGES, i - NT);
       }
       multiply(kFirst, i, fa[i], fb0, sa[i], sb);
       if (kEarly && i == NT) {   // every wavefront has read the step's columns
@@ -809,8 +826,8 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     multiply(kSecond, 0, fa[0], fb1, sa[0], sb);
     // the next step has arrived (the stores of the tile before may be on
     // their way), and no wavefront reads this step's half any more
-    if (stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kStores + (kEarly ? kLoadsB : 0)) : "memory");
-    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kEarly ? kLoadsB : 0) : "memory");
+    if (stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kStores + kYounger) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kYounger) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const bool end = step + 1 == cur.steps;
@@ -821,20 +838,20 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     fa[0] = read_a(pos + 1, 0, 0);
     sa[0] = read_power(group, next_step, wm * MT * 16);
     if (!kEarly) {
-      issue_b(pos + 2, 0);
-      issue_b(pos + 2, 1);
+      issue_b(pos + STAGES, 0);
+      issue_b(pos + STAGES, 1);
     }
 #pragma unroll
     for (int i = 1; i < MT; ++i) {
       if (kEarly) {
-        if (i % 2) issue_a(pos + 2, i / 2);
+        if (i % 2) issue_a(pos + STAGES, i / 2);
       } else {
         if (i == 1) {
-          issue_b(pos + 2, 2);
-          issue_b(pos + 2, 3);
+          issue_b(pos + STAGES, 2);
+          issue_b(pos + STAGES, 3);
         } else {
-          issue_a(pos + 2, 2 * i - 4);
-          issue_a(pos + 2, 2 * i - 3);
+          issue_a(pos + STAGES, 2 * i - 4);
+          issue_a(pos + STAGES, 2 * i - 3);
         }
       }
       const auto column = [&](int j) {
