@@ -328,7 +328,7 @@ template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPla
     }
   } else {
     st = p.kind == kTiles256  ? launch_dense_tiled<T, MODE, 2, 4, 8, 4>(a, s)
-         : p.alone(M, a.N) ? launch_dense_tiled<T, MODE, 2, 2, 4, 4, 4>(a, s)
+         : p.alone(M, a.N) ? launch_dense_tiled<T, MODE, 2, 4, 4, 2, 4>(a, s)
                            : launch_dense_tiled<T, MODE, 2, 2, 4, 4>(a, s);
   }
   if (st != VP_OK || p.parts == 1) return st;

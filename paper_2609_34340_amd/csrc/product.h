@@ -555,15 +555,16 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   // where the loads go among the rows of products: the columns' before the
   // middle of the step if there are rows enough, else all after it
   constexpr bool kEarly = MT == NT + 4;
-  static_assert((kEarly || MT == 4) && kLoadsA == 4 && kLoadsB == 4, "the loads' places among the rows of products");
+  constexpr bool kTwo = kLoadsA == 2;   // loads of each operand: two, or four
+  static_assert((kEarly || MT == 4) && kLoadsA == kLoadsB && (kLoadsA == 4 || (kTwo && !kEarly)), "the loads' places among the rows of products");
   const auto issue_a = [&](int pos, int j) { oa.issue(stage(pos), wave, j); };
   const auto issue_b = [&](int pos, int j) { ob.issue(stage(pos) + BM * kStep, wave, j); };
   const auto load = [&](int pos) {
     load_powers();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) issue_b(pos, j);
+    for (int j = 0; j < kLoadsB; ++j) issue_b(pos, j);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) issue_a(pos, j);
+    for (int j = 0; j < kLoadsA; ++j) issue_a(pos, j);
     advance();
   };
 
@@ -845,6 +846,8 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     for (int i = 1; i < MT; ++i) {
       if (kEarly) {
         if (i % 2) issue_a(pos + STAGES, i / 2);
+      } else if constexpr (kTwo) {
+        if (i <= 2) issue_a(pos + STAGES, i - 1);
       } else {
         if (i == 1) {
           issue_b(pos + STAGES, 2);
@@ -859,7 +862,7 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
         sb1[j] = read_power(group, next_step, BM + (wn * NT + j) * 16);
       };
       if (i <= NT) column(i - 1);
-      if (!kEarly && i == MT - 1) column(NT - 1);
+      if (!kEarly && NT == MT && i == MT - 1) column(NT - 1);
       multiply(kSecond, i, fa[i], fb1, sa[i], sb);
       fa[i] = read_a(pos + 1, 0, i);
       sa[i] = read_power(group, next_step, (wm * MT + i) * 16);
