@@ -766,6 +766,19 @@ vp_status vp_linear_grad_x(const void* d_y, int64_t d_y_stride, int32_t dtype, c
 vp_status vp_linear_grad_w(const void* d_y, int64_t d_y_stride, const void* x, int64_t x_stride, int32_t dtype,
                            int64_t R, int32_t N, int32_t K, float* d_w, void* ws, size_t ws_bytes, void* stream);
 
+/* Which kernel a dense product's sizes select, for tests and profiles (host
+ * only; negative for sizes that the calls refuse), and in how many parts the
+ * contraction is taken (parts may be NULL).  `direction` as in
+ * vp_linear_workspace; of tiles of 128 x 128 results at most one is on each CU
+ * at a time (ALONE), or two. */
+typedef enum {
+  VP_LINEAR_FEW_ROWS = 0,
+  VP_LINEAR_TILES_128 = 1,
+  VP_LINEAR_TILES_256 = 2,
+  VP_LINEAR_TILES_ALONE = 3
+} vp_linear_kind;
+int32_t vp_linear_kernel(int32_t direction, int64_t R, int32_t N, int32_t K, int32_t* parts);
+
 /* --------------------------------------------------------------- helpers */
 
 /* Modeled completion time of a schedule, Eq. (2), as the exact fraction

@@ -756,4 +756,4 @@ from .layer import (expert_gate_grad, expert_kernel, expert_matmul, expert_matmu
 from . import dense  # noqa: E402
 from .dense import (dropout, layer_norm, layer_norm_grad, layer_norm_grad_workspace_bytes, linear,  # noqa: E402,F401
                     linear_act_grad, linear_act_grad_workspace_bytes, linear_grad_w, linear_grad_x,
-                    linear_workspace_bytes)
+                    linear_kernel, linear_workspace_bytes)

@@ -165,6 +165,11 @@ size_t vp_linear_workspace(int32_t direction, int64_t R, int32_t N, int32_t K) {
   return vp::linear_workspace(direction, R, N, K);
 }
 
+int32_t vp_linear_kernel(int32_t direction, int64_t R, int32_t N, int32_t K, int32_t* parts) {
+  if (direction < vp::kExpertForward || direction > vp::kExpertGradW || check_product(VP_BF16, R, N, K) != VP_OK) return -1;
+  return vp::linear_kind(direction, R, N, K, parts);
+}
+
 vp_status vp_linear(const void* x, int64_t x_stride, int32_t dtype, const void* w, int64_t w_stride, int64_t R,
                     int32_t N, int32_t K, const void* bias, int32_t bias_dtype, int32_t act, const void* residual,
                     int64_t residual_stride, void* y, int32_t out_dtype, int64_t y_stride, void* pre,

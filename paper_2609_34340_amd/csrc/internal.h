@@ -282,6 +282,7 @@ struct LinearLaunch {
   void* ws;
 };
 size_t linear_workspace(int mode, int64_t R, int32_t N, int32_t K);
+vp_linear_kind linear_kind(int mode, int64_t R, int32_t N, int32_t K, int32_t* parts);
 vp_status launch_linear(const LinearLaunch& p, void* stream);
 size_t act_grad_workspace(int64_t R, int64_t N);
 vp_status launch_act_grad(const void* d_y, int64_t d_y_stride, const void* pre, int64_t pre_stride, int32_t dtype,

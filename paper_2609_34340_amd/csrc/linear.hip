@@ -125,8 +125,8 @@ template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a
     load_w(ahead[i], i * kRow);
   }
   for (int at = 0; at < bytes; at += kAhead * kRow) {
-    chunk(ahead[0], lds, at);
-    chunk(ahead[1], lds + kBuffer, at + kRow);   // past the part: zeros
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) chunk(ahead[i], lds + (i & 1) * kBuffer, at + i * kRow);   // past the part: zeros
   }
   __syncthreads();
   f32x4* each = (f32x4*)lds;   // [wavefront][column tile][row tile][lane]
@@ -231,34 +231,28 @@ int act_grad_parts(int64_t R, int64_t N) {
 }
 
 // How a product is computed, from its sizes alone: M rows and N columns of results, a contraction of C.
-enum LinearKind { kFew, kTiles128, kTiles256 };
 struct LinearPlan {
-  LinearKind kind;
+  vp_linear_kind kind;
   int parts;
   int64_t chunk;   // of the contraction: a part's values
-  // 128 x 128 tiles of M by N results, at most one for each CU
-  bool alone(int64_t M, int64_t N) const { return ((M + 127) / 128) * ((N + 127) / 128) * parts <= kCus; }
 };
 
-// Few rows: about one workgroup for each CU.  Measured, us in 1, 2, 4, 8 parts: 1
-// row by 4096 x 4096 19, 13.5, 10.4, 10.5; 61 rows 28, 19, 15.0, 16.7; 1 by 16384
-// x 4096 23, 26, 27, 28; 96 rows by 256 x 7168 in 4, 7, 14, 28 parts 17, 14, 11.6,
-// 11.7.  128 rows by 4096 x 4096 20.0, tiles 20.6.
+// Few rows: about one workgroup for each CU.  Measured, us in 1, 2, 4, 8 parts, weights from memory: 1 row by 4096 x 4096
+// 20, 15, 12.5, 12.0; 61 rows 31, 22, 16.8, 18.0; 128 rows 31, 22.0, 22.8 (tiles in 8 parts 21.2); 1 by 16384 x 4096 30, 34;
+// 96 rows by 256 x 7168 in 4, 7, 14, 28 parts 18, 14, 11.9, 11.9.
 //
-// Tiles: the least of an estimate in us.  A step of 64 values takes 0.72 for a
-// 128 x 128 tile alone on its CU, 1.1 for two, 1.65 for a 256 x 256 tile; a round
-// of tiles ends with 3 or 9 for its results; joining parts takes 2.5 and the
-// sums' way out and back at 4 TB/s.  Measured, us (128 / 256 tiles, parts in
-// brackets): 16381 rows by 4096 x 4096 546 / 445; 2048 rows 71 / 96; 512 rows 46
-// [1], 35 [2], 34 [4] / 93 [1], 48 [4]; 256 rows 46 [1], 31 [2], 24 [4], 27 [8];
-// 16384 by 256 x 4096 50 [1], 51 [2] / 99 [1], 67 [4], its weights' gradient 172
-// [1], 58 [4], 54 [8], 65 [16] / 342 [1], 63 [16], its rows' gradient 59 / 70.
+// Tiles: the least of an estimate in us.  A step of 64 values takes 0.72 for a 128 x 128 tile alone on its CU, 1.1 for two,
+// 1.65 for a 256 x 256 tile; a round of tiles ends with 3 or 9 for its results; joining parts takes 2.5 and the sums' way
+// out and back at 3 TB/s.  Measured, us (128 / 256 tiles, parts in brackets): 16381 rows by 4096 x 4096 546 / 417; 2048
+// rows 71 / 96; 512 rows 46 [1], 36.0 [2], 36.7 [4] / 93 [1], 48 [4]; 256 rows 32 [2], 25.5 [4], 29 [8]; 16384 by 256 x 4096
+// 58-62 [1], 67 [2] / 99 [1], 67 [4], its weights' gradient 60 [4], 66 [8], 74 [16] / 342 [1], 63 [16], its rows' gradient
+// 59 / 70; rows' gradient of 96 rows by 4096 x 4096 45 [1], 21.6 [4], 19.6 [8], 22.5 [16].
 LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
   const int64_t M = mode == kExpertGradW ? N_ : R, N = mode == kExpertForward ? N_ : K;
   const int64_t C = mode == kExpertForward ? K : mode == kExpertGradX ? N_ : R;
   const auto ceil_of = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  LinearPlan best{kTiles256, 1, std::max<int64_t>(C, 1)};
-  const auto in_parts = [&](LinearKind kind, int64_t parts) {
+  LinearPlan best{VP_LINEAR_TILES_256, 1, std::max<int64_t>(C, 1)};
+  const auto in_parts = [&](vp_linear_kind kind, int64_t parts) {
     LinearPlan p{kind, 1, std::max<int64_t>(C, 1)};
     if (parts > 1) {
       p.chunk = ceil_of(ceil_of(C, parts), 64) * 64;
@@ -268,18 +262,19 @@ LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
   };
   if (mode == kExpertForward && M <= 2 * kFewRows) {
     const int64_t tiles = std::max<int64_t>(ceil_of(M, kFewRows) * ceil_of(N, kFewCols), 1);
-    return in_parts(kFew, std::min(kCus / tiles, C / (2 * kFewChunk)));
+    return in_parts(VP_LINEAR_FEW_ROWS, std::min(kCus / tiles, C / (2 * kFewChunk)));
   }
   double least = 0.0;
-  for (const LinearKind kind : {kTiles256, kTiles128}) {
-    const int64_t side = kind == kTiles128 ? 128 : 256, tiles = ceil_of(M, side) * ceil_of(N, side);
+  for (const bool large : {true, false}) {
+    const int64_t side = large ? 256 : 128, tiles = ceil_of(M, side) * ceil_of(N, side);
     for (int64_t parts = 1; parts == 1 || (parts <= 64 && C >= 128 * parts); parts *= 2) {
-      const LinearPlan p = in_parts(kind, parts);
+      LinearPlan p = in_parts(VP_LINEAR_TILES_256, parts);
       const double steps = (double)ceil_of(p.chunk, 64), groups = (double)(tiles * p.parts);
-      const double rounds = std::max(1.0, std::ceil(groups / (kind == kTiles128 ? 2 * kCus : kCus)));
-      const double step = kind == kTiles256 ? 1.65 : groups > kCus ? 1.1 : 0.72;
-      double time = rounds * (step * steps + (kind == kTiles128 ? 3.0 : 9.0));
-      if (p.parts > 1) time += 2.5 + (double)p.parts * (double)M * (double)N * 8.0 / 4e6;
+      if (!large) p.kind = groups <= kCus ? VP_LINEAR_TILES_ALONE : VP_LINEAR_TILES_128;
+      const double rounds = std::max(1.0, std::ceil(groups / (large ? kCus : 2 * kCus)));
+      const double step = large ? 1.65 : p.kind == VP_LINEAR_TILES_ALONE ? 0.72 : 1.1;
+      double time = rounds * (step * steps + (large ? 9.0 : 3.0));
+      if (p.parts > 1) time += 2.5 + (double)p.parts * (double)M * (double)N * 8.0 / 3e6;
       if (least == 0.0 || time < least) {
         least = time;
         best = p;
@@ -318,7 +313,7 @@ template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPla
     a.pre = nullptr;
   }
   vp_status st = VP_OK;
-  if (p.kind == kFew) {
+  if (p.kind == VP_LINEAR_FEW_ROWS) {
     if constexpr (MODE == kForward) {
       const dim3 grid((unsigned)((a.N + kFewCols - 1) / kFewCols), (unsigned)p.parts, (unsigned)((M + kFewRows - 1) / kFewRows));
       if (M <= 16) hipLaunchKernelGGL((linear_few<T, 1>), grid, dim3(256), 0, s, a);
@@ -327,9 +322,9 @@ template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPla
       if (hipGetLastError() != hipSuccess) st = set_error(VP_ERR_HIP, "dense product launch failed");
     }
   } else {
-    st = p.kind == kTiles256  ? launch_dense_tiled<T, MODE, 2, 4, 8, 4>(a, s)
-         : p.alone(M, a.N) ? launch_dense_tiled<T, MODE, 2, 4, 4, 2, 4>(a, s)
-                           : launch_dense_tiled<T, MODE, 2, 2, 4, 4>(a, s);
+    st = p.kind == VP_LINEAR_TILES_256     ? launch_dense_tiled<T, MODE, 2, 4, 8, 4>(a, s)
+         : p.kind == VP_LINEAR_TILES_ALONE ? launch_dense_tiled<T, MODE, 2, 4, 4, 2, 4>(a, s)
+                                           : launch_dense_tiled<T, MODE, 2, 2, 4, 4>(a, s);
   }
   if (st != VP_OK || p.parts == 1) return st;
   hipLaunchKernelGGL(linear_join<T>, grid_of((M * (a.N / 4) + 255) / 256), dim3(256), 0, s, whole, (const float*)ws, p.parts, M);
@@ -338,6 +333,12 @@ template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPla
 }
 
 }  // namespace
+
+vp_linear_kind linear_kind(int mode, int64_t R, int32_t N, int32_t K, int32_t* parts) {
+  const LinearPlan p = plan_of(mode, R, N, K);
+  if (parts) *parts = p.parts;
+  return p.kind;
+}
 
 size_t linear_workspace(int mode, int64_t R, int32_t N, int32_t K) {
   const LinearPlan p = plan_of(mode, R, N, K);

@@ -6,6 +6,8 @@ reuse buffers, and so may the workspace `ws` (uint8), which calls that can overl
 from __future__ import annotations
 
 import ctypes as C
+import functools
+from operator import index
 from typing import Optional
 
 import torch
@@ -26,6 +28,7 @@ def declare(L) -> None:
     L.vp_dropout.argtypes = [vp, i32, i64, i64, i64, C.c_double, C.c_uint64, vp, vp, i64, vp, i64, vp]
     L.vp_linear_workspace.argtypes = [i32, i64, i32, i32]
     L.vp_linear_workspace.restype = sz
+    L.vp_linear_kernel.argtypes = [i32, i64, i32, i32, C.POINTER(i32)]
     L.vp_linear.argtypes = [vp, i64, i32, vp, i64, i64, i32, i32, vp, i32, i32, vp, i64, vp, i32, i64, vp, i64, vp, sz, vp]
     L.vp_linear_act_grad_workspace.argtypes = [i64, i64]
     L.vp_linear_act_grad_workspace.restype = sz
@@ -128,6 +131,7 @@ def dropout(x: torch.Tensor, p: float, seed: int, *, step: Optional[torch.Tensor
     the gradient is dropout(d_out, p, seed, step=step) with the same values.  out may be x or residual."""
     ld, dt = _matrix(x, "x"), _float_dtype(x, "x")
     T, H = x.shape
+    seed = index(seed)
     if not 0 <= seed < 1 << 64:
         raise ValueError("seed must be of 64 bits and not negative")   # ctypes would keep the low bits
     if step is not None:
@@ -149,9 +153,27 @@ def _weights2(w: torch.Tensor, dtype) -> int:
     return _matrix(w, "w", dtype=dtype)
 
 
+_DIRECTIONS = ("forward", "grad_x", "grad_w")
+
+
+@functools.lru_cache(maxsize=256)
+def _linear_bytes(direction: int, R: int, N: int, K: int) -> int:
+    return int(lib().vp_linear_workspace(direction, R, N, K))
+
+
 def linear_workspace_bytes(R: int, N: int, K: int, direction: str = "forward") -> int:
     """vp_linear_workspace; direction "forward", "grad_x" or "grad_w"."""
-    return int(lib().vp_linear_workspace(("forward", "grad_x", "grad_w").index(direction), R, N, K))
+    return _linear_bytes(_DIRECTIONS.index(direction), R, N, K)
+
+
+def linear_kernel(R: int, N: int, K: int, direction: str = "forward"):
+    """vp_linear_kernel: ("few_rows", "tiles_128", "tiles_256" or "tiles_alone", parts of the contraction), by which a
+    product of these sizes is computed."""
+    parts = C.c_int32()
+    kind = lib().vp_linear_kernel(_DIRECTIONS.index(direction), R, N, K, C.byref(parts))
+    if kind < 0:
+        raise ValueError("no product has these sizes")
+    return ("few_rows", "tiles_128", "tiles_256", "tiles_alone")[kind], parts.value
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, *, act: str = "none",
@@ -174,7 +196,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     ldo, do, size = _matrix(out, "out", cols=N, rows=R), _float_dtype(out, "out"), out.element_size()
     ldr = 0 if residual is None else _matrix(residual, "residual", cols=N, dtype=out.dtype, rows=R)
     ldp = 0 if pre is None else _matrix(pre, "pre", cols=N, dtype=x.dtype, rows=R)
-    ws = _workspace(ws, lib().vp_linear_workspace(0, R, N, K), x.device, stream)
+    ws = _workspace(ws, _linear_bytes(0, R, N, K), x.device, stream)
     queue = _queue(stream, x, w, bias, residual, out, pre, ws)
     _check(lib().vp_linear(_ptr(x), 2 * ldx, dt, _ptr(w), 2 * ldw, R, N, K, _ptr(bias), pb, _act(act), _ptr(residual),
                            size * ldr, _ptr(out), do, size * ldo, _ptr(pre), 2 * ldp, _ptr(ws),
@@ -234,7 +256,7 @@ def linear_grad_x(d_y: torch.Tensor, w: torch.Tensor, *, act: str = "none", pre:
     if out is None:
         out = _from(stream, torch.empty, (R, K), dtype=d_y.dtype, device=d_y.device)
     ldo = _matrix(out, "out", cols=K, dtype=d_y.dtype, rows=R)
-    ws = _workspace(ws, lib().vp_linear_workspace(1, R, N, K), d_y.device, stream)
+    ws = _workspace(ws, _linear_bytes(1, R, N, K), d_y.device, stream)
     queue = _queue(stream, d_y, w, pre, residual, out, ws)
     _check(lib().vp_linear_grad_x(_ptr(d_y), 2 * ldd, dt, _ptr(w), 2 * ldw, R, N, K, code, _ptr(pre), 2 * ldp,
                                   _ptr(residual), 2 * ldr, _ptr(out), 2 * ldo, _ptr(ws), 0 if ws is None else ws.numel(),
@@ -253,7 +275,7 @@ def linear_grad_w(d_y: torch.Tensor, x: torch.Tensor, *, out: Optional[torch.Ten
     if out is None:
         out = _from(stream, torch.empty, (N, K), dtype=torch.float32, device=d_y.device)
     _whole(out, torch.float32, (N, K), "out")
-    ws = _workspace(ws, lib().vp_linear_workspace(2, R, N, K), d_y.device, stream)
+    ws = _workspace(ws, _linear_bytes(2, R, N, K), d_y.device, stream)
     queue = _queue(stream, d_y, x, out, ws)
     _check(lib().vp_linear_grad_w(_ptr(d_y), 2 * ldd, _ptr(x), 2 * ldx, dt, R, N, K, _ptr(out), _ptr(ws),
                                   0 if ws is None else ws.numel(), queue), "vp_linear_grad_w")
