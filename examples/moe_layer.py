@@ -7,6 +7,7 @@ the transfers between ranks are emulated, by copying each step's slices from the
 
     python examples/moe_layer.py            # bf16, forward and backward, against torch in 32 bits
     python examples/moe_layer.py --mx       # forward with rows and weights in 4-bit blocks
+    python examples/moe_layer.py --block    # the layer inside its block: norm before, shared expert beside, dropout after it
 """
 import argparse
 import os
@@ -132,12 +133,13 @@ class Layer:
         return w[r * n:(r + 1) * n]
 
     def _routing(self, x):
-        logits = [(t @ self.router.t()).float() for t in x]
+        logits = [vp.linear(t, self.router, dtype=torch.float32) for t in x]
         routed = [vp.route(z, self.k, bias=self.bias, **self.how) for z in logits]
         return logits, routed, torch.stack([q["ids"] for q in routed]).contiguous()
 
-    def forward(self, x):
-        """x[r]: rank r's tokens [T, hidden] bf16.  Every rank's output, and what backward() needs."""
+    def forward(self, x, residual=None):
+        """x[r]: rank r's tokens [T, hidden] bf16.  Every rank's output, with x or residual[r] added, and what backward()
+        needs."""
         logits, routed, routing = self._routing(x)
         ex = Exchange(self.cat, routing, self.experts, 2 * self.hidden)
         kept, results = [], []
@@ -150,7 +152,7 @@ class Layer:
             kept.append((rows, pre, h))
             results.append(y_raw)
         returned = [as_rows(c, self.hidden) for c in ex.combine(results)]
-        out = [vp.merge(c, q["weights"], residual=t) for c, q, t in zip(returned, routed, x)]
+        out = [vp.merge(c, q["weights"], residual=t) for c, q, t in zip(returned, routed, residual or x)]
         assert vp.read_status(ex.status) == 0
         return out, (x, logits, routed, routing, kept, returned)
 
@@ -170,8 +172,9 @@ class Layer:
         assert vp.read_status(there.status) == 0 and vp.read_status(back.status) == 0
         return [vp.merge(c, q["weights"], residual=t) for c, q, t in zip(returned, routed, x)]
 
-    def backward(self, d_out, saved):
-        """Gradients of the tokens (without the router's share), of the logits, and of the experts' weights."""
+    def backward(self, d_out, saved, residual=None):
+        """Gradients of the tokens (without the router's share, with d_out or residual[r] added), of the logits, and of the
+        experts' weights."""
         x, logits, routed, routing, kept, returned = saved
         # every (token, slot) has a gradient row of its own: the same exchange with one expert for each
         ex = Exchange(self.cat, routing.view(self.N, -1, 1), self.experts, 2 * self.hidden)
@@ -193,9 +196,80 @@ class Layer:
             vp.expert_matmul_grad_x(d_pre, self._local(self.up, r), off, out=dx, status=ex.status)
             back.append(dx_raw)
         ones = torch.ones((x[0].shape[0], self.k), device="cuda")
-        dx = [vp.merge(as_rows(c, self.hidden), ones, residual=d) for c, d in zip(ex.combine(back), d_out)]
+        dx = [vp.merge(as_rows(c, self.hidden), ones, residual=d) for c, d in zip(ex.combine(back), residual or d_out)]
         assert vp.read_status(ex.status) == 0
         return dx, d_logits, torch.cat(d_up), torch.cat(d_down)
+
+
+class Block:
+    """x + dropout(layer(n) + shared(n)) with n = norm(x) and a shared expert down(gelu(up(n) + bias))."""
+
+    def __init__(self, layer, p=0.1, seed=0):
+        g = torch.Generator(device="cuda").manual_seed(seed + 100)
+        rand = lambda *s, std: torch.randn(*s, generator=g, device="cuda") * std  # noqa: E731
+        hidden, inner = layer.hidden, layer.inner
+        self.layer, self.p, self.seed = layer, p, seed
+        self.norm_w, self.norm_b = 1 + rand(hidden, std=0.1), rand(hidden, std=0.1)
+        self.up, self.up_b = rand(inner, hidden, std=hidden ** -0.5).bfloat16(), rand(inner, std=0.1)
+        self.down = rand(hidden, inner, std=inner ** -0.5).bfloat16()
+        self.step = torch.zeros(1, dtype=torch.int64, device="cuda")   # counts the training steps: a new mask each
+
+    def forward(self, x):
+        saved, normed, shared = [], [], []
+        for t in x:
+            stats = torch.empty((len(t), 2), device="cuda")
+            n = vp.layer_norm(t, self.norm_w, self.norm_b, stats=stats)
+            pre = torch.empty((len(t), self.up.shape[0]), dtype=t.dtype, device="cuda")
+            h = vp.linear(n, self.up, self.up_b, act="gelu", pre=pre)
+            normed.append(n)
+            shared.append(vp.linear(h, self.down))
+            saved.append((t, stats, n, pre, h))
+        y, layer_saved = self.layer.forward(normed, residual=shared)
+        out = [vp.dropout(m, self.p, self.seed + r, step=self.step, residual=t) for r, (m, t) in enumerate(zip(y, x))]
+        return out, (saved, layer_saved)
+
+    def backward(self, d_out, kept):
+        """Gradients of the tokens, then a dict of the weights'."""
+        saved, layer_saved = kept
+        d_y = [vp.dropout(d, self.p, self.seed + r, step=self.step) for r, d in enumerate(d_out)]
+        grads = dict.fromkeys(("norm_w", "norm_b", "up", "up_b", "down", "router"), 0.0)
+        d_n = []
+        for d, (_, _, n, pre, h) in zip(d_y, saved):
+            grads["down"] = grads["down"] + vp.linear_grad_w(d, h)
+            d_pre = vp.linear_grad_x(d, self.down, act="gelu", pre=pre)
+            grads["up_b"] = grads["up_b"] + vp.linear_act_grad(d_pre)[1]
+            grads["up"] = grads["up"] + vp.linear_grad_w(d_pre, n)
+            d_n.append(vp.linear_grad_x(d_pre, self.up))
+        d_n, d_logits, d_up, d_down = self.layer.backward(d_y, layer_saved, residual=d_n)
+        d_x = []
+        for d, g, z, (t, stats, n, _, _) in zip(d_out, d_n, d_logits, saved):
+            z = z.bfloat16()
+            grads["router"] = grads["router"] + vp.linear_grad_w(z, n)
+            g = vp.linear_grad_x(z, self.layer.router, residual=g)
+            dx, dw, db = vp.layer_norm_grad(g, t, stats, self.norm_w, residual=d)
+            grads["norm_w"], grads["norm_b"] = grads["norm_w"] + dw, grads["norm_b"] + db
+            d_x.append(dx)
+        return d_x, dict(grads, experts_up=d_up, experts_down=d_down)
+
+
+def block_errors(layer, x, d_out):
+    """The block's output and gradients against torch in 32 bits, with the experts that it chose and the values it kept."""
+    block = Block(layer)
+    out, kept = block.forward(x)
+    d_x, grads = block.backward(d_out, kept)
+    names = dict(norm_w=block.norm_w, norm_b=block.norm_b, up=block.up, up_b=block.up_b, down=block.down, router=layer.router,
+                 experts_up=layer.up, experts_down=layer.down)
+    leaf = {k: v.float().requires_grad_() for k, v in names.items()}
+    tokens, want = [t.float().requires_grad_() for t in x], []
+    for r, (t, q) in enumerate(zip(tokens, kept[1][2])):
+        n = torch.nn.functional.layer_norm(t, (layer.hidden,), leaf["norm_w"], leaf["norm_b"], 1e-5)
+        s = torch.nn.functional.gelu(n @ leaf["up"].t() + leaf["up_b"]) @ leaf["down"].t()
+        y = reference(layer, n, n @ leaf["router"].t(), q["ids"], leaf["experts_up"], leaf["experts_down"]) - n + s
+        mask = vp.dropout(torch.ones_like(t), block.p, block.seed + r, step=block.step)   # the factor, or 0
+        want.append(t + y * mask)
+    sum((w * d.float()).sum() for w, d in zip(want, d_out)).backward()
+    return dict(out=relative(torch.cat(out), torch.cat(want).detach()), dx=relative(torch.cat(d_x), torch.cat([t.grad for t in tokens])),
+                **{"d_" + k: relative(grads[k], leaf[k].grad) for k in names})
 
 
 def reference(layer, x, logits, ids, up, down):
@@ -223,12 +297,16 @@ def main(argv=None):
     ap.add_argument("--experts", type=int, default=32)
     ap.add_argument("--top-k", type=int, default=2)
     ap.add_argument("--mx", action="store_true")
+    ap.add_argument("--block", action="store_true")
     a = ap.parse_args(argv)
     N = 8
     layer = Layer(a.hidden, a.inner, a.experts, a.top_k, N)
     g = torch.Generator(device="cuda").manual_seed(1)
     x = [torch.randn(a.tokens, a.hidden, generator=g, device="cuda").bfloat16() for _ in range(N)]
-    if a.mx:
+    if a.block:
+        d_out = [torch.randn(a.tokens, a.hidden, generator=g, device="cuda").bfloat16() for _ in range(N)]
+        errors = block_errors(layer, x, d_out)
+    elif a.mx:
         up, down = vp.mx_quantize(layer.up), vp.mx_quantize(layer.down)
         out = layer.forward_mx(x, up, down)
         logits, routed, _ = layer._routing(x)
