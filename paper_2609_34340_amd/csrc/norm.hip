@@ -38,6 +38,15 @@ __device__ inline float plus(float p, float q) { return p + q; }
 // A value that a wavefront's lanes share, so that what follows from it (a row's address) takes scalar registers.
 __device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// To one unit of the last place.
+__device__ inline float inverse_root(float v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_amdgcn_rsqf(v);
+#else
+  return v;
+#endif
+}
+
 // n neighbouring parameters, from column c of H on, as they lie in memory.
 template <typename P, int n> struct Params {
   static constexpr int kVecs = n / Vec<P>::n;
@@ -93,16 +102,19 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm
   // of this wavefront's share of the row
   const int mine = LANES ? a.H : held<NV, n>(wave * 64, row.lanes, a.H);
   const bool full = mine == kSum * NV * n;   // no lane past the row's end
-  const float each = 1.0f / (float)max(mine, 1);
+  const float each = 1.0f / (float)max(mine, 1), part_of_row = 1.0f / count;
+  // of wavefront lane % 16, for the joint statistics
+  const float theirs = LANES == 0 && (threadIdx.x & 15) < waves ? (float)held<NV, n>((threadIdx.x & 15) * 64, row.lanes, a.H) : 0.0f;
   const int64_t stride = (int64_t)gridDim.x * gridDim.y * row.groups;
   int64_t t = block_index() * row.groups + row.group;
   u32x4 next[NV];
   const auto fetch = [&](int64_t at) {
+    if (at >= a.T) return;   // what is there stays, and goes nowhere
     const T* x = (const T*)(a.x + at * a.x_stride);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (row.lane + i * row.lanes) * n;
-      next[i] = load_piece(x + c, at < a.T ? a.H - c : 0);
+      next[i] = full ? *(const u32x4_any*)(x + c) : load_piece(x + c, a.H - c);
     }
   };
   fetch(t);
@@ -153,23 +165,23 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm
         all[2][wave] = squares;
       }
       __syncthreads();
-      float first = all[0][0], sum = 0.0f, total = 0.0f;
-      for (int i = 0; i < waves; ++i) {
-        sum = __builtin_fmaf((float)held<NV, n>(i * 64, row.lanes, a.H), all[0][i] - first + all[1][i], sum);
-        total += all[2][i];
-      }
-      const float delta = sum / count;   // of the row's mean from `first`
+      // lane l of every 16 has wavefront l's
+      const int l = threadIdx.x & 15;
+      const bool in = l < waves;
+      const float first = all[0][0], theirs_mean = in ? all[0][l] - first + all[1][l] : 0.0f;
+      float total = in ? all[2][l] : 0.0f, delta = 0.0f;   // delta: of the row's mean from `first`
       if (a.center) {
-        for (int i = 0; i < waves; ++i) {
-          const float d = all[0][i] - first + all[1][i] - delta;
-          total = __builtin_fmaf((float)held<NV, n>(i * 64, row.lanes, a.H) * d, d, total);
-        }
+        delta = across<16>(theirs * theirs_mean, plus) * part_of_row;
+        const float d = theirs_mean - delta;
+        total = __builtin_fmaf(theirs * d, d, total);
       }
+      total = across<16>(total, plus);
       base = first;
-      shift = a.center ? delta : 0.0f;
+      shift = delta;
       squares = total;
     }
-    const float r = 1.0f / sqrtf((squares < 0.0f ? 0.0f : squares / count) + a.eps);   // below 0 only by rounding
+    // (below 0 only by rounding; the hardware's root is as near as a rounded one and a division)
+    const float r = inverse_root((squares < 0.0f ? 0.0f : squares * part_of_row) + a.eps);
     if (t >= a.T) continue;
     if (a.stats && row.lane == 0) {
       a.stats[2 * t] = base + shift;
@@ -180,7 +192,7 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (row.lane + i * row.lanes) * n;
-      if (c >= a.H) break;
+      if (!full && c >= a.H) break;
       float f[n], p[n];
       constexpr auto at = [](int k) { return kKeep ? k : 0; };
 #pragma unroll
@@ -197,7 +209,8 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm
 #pragma unroll
         for (int e = 0; e < n; ++e) f[e] += p[e];
       }
-      store_piece(y + c, pack16<T>(f), a.H - c);
+      if (full) *(u32x4_any*)(y + c) = pack16<T>(f);
+      else store_piece(y + c, pack16<T>(f), a.H - c);
     }
   }
 }
