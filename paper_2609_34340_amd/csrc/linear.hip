@@ -4,6 +4,10 @@
 //   grad x    d_x = (d_y W) act'(pre) + residual     (over N)
 //   grad w    d_w = d_y^T x                          (over the rows, in 32 bits)
 //   d_pre = d_y act'(pre), d_b = sum over rows of it
+//
+// Many rows go through product.h's tiles, of 128 x 128 or 256 x 256 results,
+// few through linear_few.  Where the results are too few for 256 CUs the
+// contraction is taken in parts, whose sums linear_join adds in their order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -63,7 +67,12 @@ template <typename T> __device__ inline void finish4(const DenseArgs& a, int64_t
 // time: two wavefronts for 32 columns each, and two more for the other half of
 // the chunk, whose sums are added in LDS at the end.  Loads run two chunks
 // ahead.  16-byte piece c of row r lies at place c ^ (r & 15), so that a
-// fragment's 16 rows meet no bank twice.
+// fragment's 16 rows meet no bank twice.  61 rows by 4096 x 4096, weights from
+// memory, in four parts: 13 us, and 4 for the join; 96 by 256 x 7168 in 14: 7.5
+// and 4.5.  Tried and dropped: four chunks ahead for up to 32 rows (12.5 -> 13.0
+// us at one row: the weights' rate bounds it, not their latency), up to 16 rows
+// by 16 columns without parts (10.4 -> 8.6 us at one row by 4096 x 4096, 11.0 ->
+// 11.4 at 16 rows, 17 -> 20 at 16 by 8192 x 4096).
 constexpr int kFewRows = 64, kFewCols = 64, kFewChunk = 256;
 
 template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a, int64_t m0, int n0, int part, unsigned char* lds) {
@@ -167,7 +176,9 @@ template <typename T> __global__ void __launch_bounds__(256) linear_join(DenseAr
 
 // Through the activation, and the columns' sums.  A wavefront has 64 pieces of
 // 16 bytes of a row; the workgroup's four take turns on the rows of one part,
-// kAhead rows' loads at a time, and join their columns' sums in LDS.
+// kActAhead rows' loads at a time, and join their columns' sums in LDS.  HBM
+// bounds it: gelu's of 8191 rows of 4096, bf16, 42 us, 4.8 TB/s, and 4.7 for the
+// parts' sums.
 struct ActGradArgs {
   const unsigned char *d_y, *pre;
   int64_t d_y_stride, pre_stride, d_pre_stride;

@@ -9,6 +9,16 @@
 // corrects the mean and the sum of squares; a workgroup joins its wavefronts' by the formula for two groups' variances
 // (Chan, Golub, LeVeque 1979).  Means are kept as a base and a small shift, so nothing cancels however far from zero the
 // rows lie.
+//
+// HBM bounds both directions, and first the instructions had to become few enough: workgroups run through rows with their
+// parameters in registers and the next row's loads on the way, pieces of rows that are whole carry no checks, and the
+// wavefronts' statistics are joined across lanes (in a loop over the wavefronts by every lane they were more instructions
+// than the row's values: 16384 rows of 7168, bf16, 414 a wavefront and row, 98.7 us; now 240 and 90 us, 5.2 TB/s, where a
+// 1 GiB copy reaches 4.8 to 5.2).  96 rows of 4096 take 3.5 us, about a launch.  The gradient of 8192 rows of 4096 with a
+// residual: 57 us, 4.7 TB/s, and 5 for the sums of its 256 workgroups; its registers (an output's sums for every column)
+// leave a CU one workgroup, and two rows' loads ahead make up for it (one: 62 us; 128 registers and two workgroups spill:
+// 122).  Rows that begin at any element cost little in 32 bits (4095 rows of 2047: 27 us, of 2048 22), twice the time in
+// 16 (8192 rows of 4095: 104, of 4096 53).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -82,7 +92,7 @@ template <int NV, int n> __device__ inline int held(int first, int lanes, int H)
 
 constexpr int kMaxWaves = 16;
 
-constexpr int kWaves = 5;   // wavefronts of a SIMD that the registers are kept to
+constexpr int kWaves = 6;   // wavefronts of a SIMD that the registers are kept to
 
 template <typename T, typename P, int LANES, int NV>
 __global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm_kernel(NormArgs a) {
@@ -107,7 +117,7 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024, NV == 2 ? kWaves : 4) norm
   const float theirs = LANES == 0 && (threadIdx.x & 15) < waves ? (float)held<NV, n>((threadIdx.x & 15) * 64, row.lanes, a.H) : 0.0f;
   const int64_t stride = (int64_t)gridDim.x * gridDim.y * row.groups;
   int64_t t = block_index() * row.groups + row.group;
-  u32x4 next[NV];
+  u32x4 next[NV] = {};
   const auto fetch = [&](int64_t at) {
     if (at >= a.T) return;   // what is there stays, and goes nowhere
     const T* x = (const T*)(a.x + at * a.x_stride);

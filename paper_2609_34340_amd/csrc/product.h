@@ -634,6 +634,9 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   // i) 16 + r, columns (wn NT + j) 16 + 4 q on.  16-bit operands of the epilogue
   // come as the stores go, 16 bytes a lane for two fragments, and are brought to
   // the fragments' places by the same exchange; their loads run kFar pairs ahead.
+  // 16381 rows by 4096 x 4096: 417-435 us without, 495-510 with bias, gelu, kept
+  // values and residual (of which the residual and the kept values, 268 MB, 50 and
+  // gelu 10-20); row by row of fragments, with the spilled registers, 560.
   const auto finish = [&](const TileTo& t) {
     if constexpr (kDense) {
       const auto resource = [&](const unsigned char* base, int64_t stride, int size) {
