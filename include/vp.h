@@ -679,7 +679,8 @@ int32_t vp_route_lanes(int64_t T, int32_t E);
  *   weight, bias  device [H] of param_dtype, which is VP_F32 or x's type;
  *           either may be NULL (ones, zeros)
  *   stats   device float32 [T, 2], (m, r) for the gradient, or NULL
- * A row with an infinity or NaN becomes NaN and touches no other.  H <= 2^20, T
+ * A row with an infinity or NaN becomes NaN and touches no other (without
+ * `center` an infinity makes r 0: zeros, and NaN in its own place).  H <= 2^20, T
  * < 2^31; strides and addresses are multiples of the element (of 16 bytes for
  * full speed), eps >= 0 and finite. */
 vp_status vp_layer_norm(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, const void* weight,

@@ -14,6 +14,7 @@
 #include <cmath>
 
 #include "act.h"
+#include "divide.h"
 #include "internal.h"
 #include "numeric.h"
 #include "product.h"
@@ -167,7 +168,7 @@ template <typename T> __global__ void __launch_bounds__(256) linear_join(DenseAr
   const int64_t i = block_index() * 256 + threadIdx.x;
   const int quads = a.N / 4;
   if (i >= M * quads) return;
-  const int64_t m = i / quads;
+  const int64_t m = fdiv53(i, quads);
   f32x4 v = {};
 #pragma unroll 8
   for (int p = 0; p < parts; ++p) v += *(const f32x4*)(sums + (p * M * quads + i) * 4);

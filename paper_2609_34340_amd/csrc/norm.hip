@@ -48,10 +48,10 @@ __device__ inline float plus(float p, float q) { return p + q; }
 // A value that a wavefront's lanes share, so that what follows from it (a row's address) takes scalar registers.
 __device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// To one unit of the last place.
+// To one unit of the last place; the hardware's takes the smallest numbers for 0, so these are scaled.
 __device__ inline float inverse_root(float v) {
 #ifdef __HIP_DEVICE_COMPILE__
-  return __builtin_amdgcn_rsqf(v);
+  return v < 0x1p-100f ? __builtin_amdgcn_rsqf(v * 0x1p100f) * 0x1p50f : __builtin_amdgcn_rsqf(v);
 #else
   return v;
 #endif
@@ -417,7 +417,7 @@ template <typename T, typename P> __global__ void __launch_bounds__(kLong) norm_
   });
   s = block_sum(s, lds);
   const float shift = a.center ? s.a / count : 0.0f, squares = s.b - s.a * shift;
-  const float r = 1.0f / sqrtf((squares < 0.0f ? 0.0f : squares / count) + a.eps);
+  const float r = inverse_root((squares < 0.0f ? 0.0f : squares / count) + a.eps);
   if (a.stats && threadIdx.x == 0) {
     a.stats[2 * t] = m + shift;
     a.stats[2 * t + 1] = r;

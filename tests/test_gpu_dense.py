@@ -165,6 +165,10 @@ def test_layer_norm_of_infinities_and_nan(vp):
         got = vp.layer_norm(x.cuda())
         assert got[1:4].isnan().all()
         near_rounded(got[::4], y[::4], err[::4])
+        square = vp.layer_norm(x.cuda(), center=False)
+        assert square[2].isnan().all()
+        for row, place in ((1, 3), (3, 0)):
+            assert square[row, place].isnan() and (square[row].nan_to_num(0.0) == 0).all() and int(square[row].isnan().sum()) == 1
         stats = ref.norm(torch.where(x.isfinite(), x, 0.0), None, None, 1e-5, True)[2].float()
         dx, e_x, dw, _, _, _ = ref.norm_grad(torch.ones_like(x), x, stats, None, True)
         got = vp.layer_norm_grad(torch.ones_like(x).cuda(), x.cuda(), stats.cuda())
@@ -189,6 +193,36 @@ def test_layer_norm_in_place_and_empty(vp):
     assert vp.layer_norm(none).shape == (0, 16)
     got = vp.layer_norm_grad(none, none, torch.empty(0, 2, device="cuda"), d_weight=torch.ones(16, device="cuda"))
     assert (got[1] == 0).all() and (got[2] == 0).all()   # sums over no rows
+
+
+def test_layer_norm_without_eps(vp):
+    """Tiny rows, whose squares are next to the smallest numbers, and rows of one value (0 / 0)."""
+    for H in (64, 4096, 40000):
+        x = normal((3, H), 1)
+        x[1] *= 2.0 ** -50
+        x[2] = 0.0
+        y, err, stats, stats_err = ref.norm(x[:2], None, None, 0.0, True)
+        st = torch.empty(3, 2, device="cuda")
+        got = vp.layer_norm(x.cuda(), eps=0.0, stats=st)
+        near_rounded(got[:2], y, err)
+        near(st[:2], stats, stats_err + 1e-30)
+        assert got[2].isnan().all()
+
+
+def test_layer_norm_grad_of_one_parameter(vp):
+    """The library's call with only d_weight or only d_bias asked for."""
+    L, T, H = vp.lib(), 37, 200
+    x, d = normal((T, H), 1).cuda(), normal((T, H), 2).cuda()
+    st = torch.rand(T, 2, device="cuda")
+    want = vp.layer_norm_grad(d, x, st)
+    for which in (0, 1):
+        dx, one = torch.empty_like(x), torch.full((H,), math.nan, device="cuda")
+        ws = torch.empty(vp.layer_norm_grad_workspace_bytes(T, H), dtype=torch.uint8, device="cuda")
+        p = lambda t: t.data_ptr()  # noqa: E731
+        assert L.vp_layer_norm_grad(p(d), 4 * H, p(x), 4 * H, 0, T, H, p(st), None, 0, 1, None, 0, p(dx), 4 * H,
+                                    None if which else p(one), p(one) if which else None, p(ws), ws.numel(),
+                                    torch.cuda.current_stream().cuda_stream) == vp.OK
+        assert torch.equal(dx, want[0]) and torch.equal(one, want[1 + which])
 
 
 @pytest.mark.parametrize("center", [True, False])
@@ -607,3 +641,11 @@ def test_launches_of_more_than_2_to_the_32_threads(vp):
         near_rounded(vp.dropout(x, 0.5, 4)[first:first + 5], want, err)
     d, e, _, _ = ref.act_grad(last, last, "silu")
     near_rounded(vp.linear_act_grad(x, x, act="silu")[0][-5:], d, e)
+    w = normal((8, 8), 3, torch.bfloat16)
+    for got, (want, e) in ((vp.linear(x, w.cuda(), act="silu"), ref.linear(last, w, None, "silu")[:2]),
+                           (vp.linear_grad_x(x, w.cuda()), ref.linear_grad_x(last, w))):
+        near_rounded(got[-5:], want, e)
+        near_rounded(got[:5], want, e)
+        assert (got[5:-5] == 0).all()
+    want, e = ref.linear_grad_w(last, last)
+    near(vp.linear_grad_w(x, x), 2 * want, 4 * e + 1e-30)
