@@ -21,8 +21,8 @@
 
 #include "internal.h"
 #include "numeric.h"
-#include "product.h"
 #include "report.h"
+#include "product.h"
 
 namespace vp {
 namespace {

@@ -2,9 +2,9 @@
 // dense ones share.
 //
 // Each step of the contraction brings 128 bytes of every row of both operands
-// to LDS (64 16-bit values, or 256 4-bit ones) by direct loads, double
-// buffered.  Both operands are read through buffer descriptors that end with
-// the expert's last row: what lies outside reads as zero, so no neighbour's
+// to LDS (64 16-bit values, or 256 4-bit ones) by direct loads, two or four
+// steps ahead.  Both operands are read through buffer descriptors that end with
+// the operand's last row: what lies outside reads as zero, so no neighbour's
 // row (which may hold anything) enters a sum.  The places in LDS are permuted
 // so that the matrix fragments' reads meet no bank twice (in 4-bit blocks, whose
 // lanes take neighbouring chunks, some do):
@@ -14,7 +14,8 @@
 //                         piece p of contraction row c at place p ^ f(c), read
 //                         through the transposing LDS load
 // The product is computed as its transpose, so that a lane's four results are
-// neighbours in the output row.
+// neighbours in the output row.  (The experts' products report offsets out of
+// order: their source includes report.h before this.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -25,7 +26,6 @@
 #include "act.h"
 #include "internal.h"
 #include "numeric.h"
-#include "report.h"
 
 namespace vp {
 namespace {
