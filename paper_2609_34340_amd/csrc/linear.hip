@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "act.h"
 #include "divide.h"
@@ -76,7 +77,8 @@ template <typename T> __device__ inline void finish4(const DenseArgs& a, int64_t
 // 11.4 at 16 rows, 17 -> 20 at 16 by 8192 x 4096).
 constexpr int kFewRows = 64, kFewCols = 64, kFewChunk = 256;
 
-template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a, int64_t m0, int n0, int part, unsigned char* lds) {
+template <typename T, int MT>
+__device__ inline void few_rows(const DenseArgs& a, int64_t m0, int n0, int part, unsigned char* lds) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int kRow = kFewChunk * 2, kBuffer = MT * 16 * kRow, kAhead = 2;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -84,7 +86,8 @@ template <typename T, int MT> __device__ inline void few_rows(const DenseArgs& a
   const int rows = (int)min((int64_t)(MT * 16), a.R - m0);
   const int c0 = part * a.chunk, bytes = min(a.chunk, a.C - c0) * 2;   // of the part
   const int sx = (int)a.a_stride, sw = (int)a.b_stride;
-  const auto rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_stride + (int64_t)c0 * 2), 0, (rows - 1) * sx + bytes, 0x00020000);
+  const auto rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_stride + (int64_t)c0 * 2), 0,
+                                                    (rows - 1) * sx + bytes, 0x00020000);
   const auto weights = [&](int u) {
     const int n = n0 + group * 32 + u * 16, valid = max(min(16, a.N - n), 0);
     return __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + (int64_t)n * a.b_stride + (int64_t)c0 * 2), 0,
@@ -249,34 +252,57 @@ struct LinearPlan {
   int64_t chunk;   // of the contraction: a part's values
 };
 
-// Few rows: about one workgroup for each CU.  Measured, us in 1, 2, 4, 8 parts, weights from memory: 1 row by 4096 x 4096
-// 20, 15, 12.5, 12.0; 61 rows 31, 22, 16.8, 18.0; 128 rows 31, 22.0, 22.8 (tiles in 8 parts 21.2); 1 by 16384 x 4096 30, 34;
-// 96 rows by 256 x 7168 in 4, 7, 14, 28 parts 18, 14, 11.9, 11.9.
+// The least of an estimate in us.  Few rows: a chunk of 256 values takes 1.06 with up to 16 rows, 1.25 with 32, 1.7
+// with 64, (four fifths more where two workgroups share a CU), or its weights' time at 5.2 TB/s for all of them; 3
+// around them, and for parts 6 for the second launch (on the device 4, but a call of two launches takes the host 3
+// longer) and the sums' way out and back at 3 TB/s.  Measured in 1, 2, 4, 8 parts, weights from memory: 1 row by 4096
+// x 4096 20, 15, 12.5, 12.0; 61 rows 31, 22, 16.8, 18.0; 128 rows 31, 22.0, 22.8 (tiles in 8 parts 21.2); 1 by 16384 x
+// 4096 30, 34; 96 rows by 256 x 7168 in 4, 7, 14, 28 parts 18, 14, 11.9, 11.9; 1 by 512 x 512 4.8, 6.3, by 512 x 1536
+// 8.7, 8.3, by 2048 x 2048 11.4, 10.0, 8.3, 7.6.
 //
-// Tiles: the least of an estimate in us.  A step of 64 values takes 0.72 for a 128 x 128 tile alone on its CU, 1.1 for two,
-// 1.65 for a 256 x 256 tile; a round of tiles ends with 3 or 9 for its results; joining parts takes 2.5 and the sums' way
-// out and back at 3 TB/s.  Measured, us (128 / 256 tiles, parts in brackets): 16381 rows by 4096 x 4096 546 / 417; 2048
-// rows 71 / 96; 512 rows 46 [1], 36.0 [2], 36.7 [4] / 93 [1], 48 [4]; 256 rows 32 [2], 25.5 [4], 29 [8]; 16384 by 256 x 4096
-// 58-62 [1], 67 [2] / 99 [1], 67 [4], its weights' gradient 60 [4], 66 [8], 74 [16] / 342 [1], 63 [16], its rows' gradient
-// 59 / 70; rows' gradient of 96 rows by 4096 x 4096 45 [1], 21.6 [4], 19.6 [8], 22.5 [16].
+// Tiles: a step of 64 values takes 0.72 for a 128 x 128 tile alone on its CU, 1.1 for two, 1.65 for a 256 x 256 tile;
+// a round of tiles ends with 3 or 9 for its results; parts as above.  Measured, us (128 / 256 tiles, parts in
+// brackets): 16381 rows by 4096 x 4096 546 / 417; 2048 rows 71 / 96; 512 rows 46 [1], 36.0 [2], 36.7 [4] / 93 [1], 48
+// [4]; 256 rows 32 [2], 25.5 [4], 29 [8]; 16384 by 256 x 4096 58-62 [1], 67 [2] / 99 [1], 67 [4], its weights'
+// gradient 60 [4], 66 [8], 74 [16] / 342 [1], 63 [16], its rows' gradient 59 / 70; rows' gradient of 96 rows by 4096 x
+// 4096 45 [1], 21.6 [4], 19.6 [8], 22.5 [16].
 LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
   const int64_t M = mode == kExpertGradW ? N_ : R, N = mode == kExpertForward ? N_ : K;
   const int64_t C = mode == kExpertForward ? K : mode == kExpertGradX ? N_ : R;
   const auto ceil_of = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  LinearPlan best{VP_LINEAR_TILES_256, 1, std::max<int64_t>(C, 1)};
   const auto in_parts = [&](vp_linear_kind kind, int64_t parts) {
     LinearPlan p{kind, 1, std::max<int64_t>(C, 1)};
     if (parts > 1) {
-      p.chunk = ceil_of(ceil_of(C, parts), 64) * 64;
+      const int64_t unit = kind == VP_LINEAR_FEW_ROWS ? kFewChunk : 64;
+      p.chunk = ceil_of(ceil_of(C, parts), unit) * unit;
       p.parts = (int)ceil_of(C, p.chunk);
     }
     return p;
   };
-  if (mode == kExpertForward && M <= 2 * kFewRows) {
-    const int64_t tiles = std::max<int64_t>(ceil_of(M, kFewRows) * ceil_of(N, kFewCols), 1);
-    return in_parts(VP_LINEAR_FEW_ROWS, std::min(kCus / tiles, C / (2 * kFewChunk)));
-  }
+  const auto join = [&](const LinearPlan& p) {
+    return p.parts > 1 ? 6.0 + (double)p.parts * (double)M * (double)N * 8.0 / 3e6 : 0.0;
+  };
+  LinearPlan best{VP_LINEAR_FEW_ROWS, 1, std::max<int64_t>(C, 1)};
   double least = 0.0;
+  const auto take = [&](const LinearPlan& p, double time) {
+    if (least == 0.0 || time < least) {
+      least = time;
+      best = p;
+    }
+  };
+  if (mode == kExpertForward && M <= 2 * kFewRows) {
+    const int64_t tiles = ceil_of(M, kFewRows) * ceil_of(N, kFewCols), most = C / kFewChunk;
+    const double chunk = M <= 16 ? 1.06 : M <= 32 ? 1.25 : 1.7;
+    const int64_t one_each = kCus / std::max<int64_t>(tiles, 1);
+    for (const int64_t parts : std::initializer_list<int64_t>{1, 2, 4, 8, 16, 32, one_each, most}) {
+      if (parts > std::max<int64_t>(most, 1) || parts > 64) continue;
+      const LinearPlan p = in_parts(VP_LINEAR_FEW_ROWS, parts);
+      const double bytes = (double)(ceil_of(N, kFewCols) * p.parts) * (kFewCols * kFewChunk * 2);
+      const double crowd = std::max(1.0, 0.8 * (double)(tiles * p.parts) / kCus);
+      take(p, 3.0 + (double)ceil_of(p.chunk, kFewChunk) * std::max(chunk * crowd, bytes / 5.2e6) + join(p));
+    }
+    return best;
+  }
   for (const bool large : {true, false}) {
     const int64_t side = large ? 256 : 128, tiles = ceil_of(M, side) * ceil_of(N, side);
     for (int64_t parts = 1; parts == 1 || (parts <= 64 && C >= 128 * parts); parts *= 2) {
@@ -285,18 +311,14 @@ LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
       if (!large) p.kind = groups <= kCus ? VP_LINEAR_TILES_ALONE : VP_LINEAR_TILES_128;
       const double rounds = std::max(1.0, std::ceil(groups / (large ? kCus : 2 * kCus)));
       const double step = large ? 1.65 : p.kind == VP_LINEAR_TILES_ALONE ? 0.72 : 1.1;
-      double time = rounds * (step * steps + (large ? 9.0 : 3.0));
-      if (p.parts > 1) time += 2.5 + (double)p.parts * (double)M * (double)N * 8.0 / 3e6;
-      if (least == 0.0 || time < least) {
-        least = time;
-        best = p;
-      }
+      take(p, rounds * (step * steps + (large ? 9.0 : 3.0)) + join(p));
     }
   }
   return best;
 }
 
-template <typename T, int MODE, int WM, int WN, int MT, int NT, int STAGES = 2> vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
+template <typename T, int MODE, int WM, int WN, int MT, int NT, int STAGES = 2>
+vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
   constexpr int BM = WM * MT * 16, BN = WN * NT * 16;
   const int64_t mt = ((MODE == kGradW ? a.M : a.R) + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
   const int64_t tiles = mt * nt * a.parts;

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 # direction, R, N, K, kernel, parts: None where any number does
 PRODUCTS = [
-    ("forward", 1, 8, 8, "few_rows", 1), ("forward", 17, 72, 2056, "few_rows", 4), ("forward", 128, 264, 4096, "few_rows", 8),
+    ("forward", 1, 8, 8, "few_rows", 1), ("forward", 17, 72, 2056, "few_rows", None), ("forward", 128, 264, 4096, "few_rows", None), ("forward", 40, 520, 1000, "few_rows", 1),
     ("forward", 33, 16384, 512, "few_rows", 1),
     ("forward", 129, 8, 8, "tiles_alone", 1), ("forward", 130, 136, 64, "tiles_alone", 1), ("forward", 1000, 1032, 200, "tiles_alone", 1),
     ("forward", 140, 264, 4104, "tiles_alone", None), ("forward", 3000, 2056, 72, "tiles_128", 1), ("forward", 6100, 4104, 40, "tiles_128", 1),
