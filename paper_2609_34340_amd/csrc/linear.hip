@@ -253,7 +253,7 @@ struct LinearPlan {
 };
 
 // The least of an estimate in us.  Few rows: a chunk of 256 values takes 1.06 with up to 16 rows, 1.25 with 32, 1.7
-// with 64, (four fifths more where two workgroups share a CU), or its weights' time at 5.2 TB/s for all of them; 3
+// with 64 (1.6 times that where two workgroups share a CU), or its weights' time at 5.2 TB/s for all of them; 3
 // around them, and for parts 6 for the second launch (on the device 4, but a call of two launches takes the host 3
 // longer) and the sums' way out and back at 3 TB/s.  Measured in 1, 2, 4, 8 parts, weights from memory: 1 row by 4096
 // x 4096 20, 15, 12.5, 12.0; 61 rows 31, 22, 16.8, 18.0; 128 rows 31, 22.0, 22.8 (tiles in 8 parts 21.2); 1 by 16384 x
