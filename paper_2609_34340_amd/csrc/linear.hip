@@ -323,8 +323,7 @@ vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
   const int64_t mt = ((MODE == kGradW ? a.M : a.R) + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
   const int64_t tiles = mt * nt * a.parts;
   if (tiles >= (int64_t)1 << 31) return set_error(VP_ERR_UNSUPPORTED, "more than 2^31 tiles");
-  int64_t per = MODE == kGradW ? (mt * nt + 7) / 8 * a.parts : (tiles + 7) / 8;
-  per = std::min<int64_t>(per, kCus / 8 * (BM == 128 && STAGES == 2 ? 2 : 1));
+  const int64_t per = std::min<int64_t>((tiles + 7) / 8, kCus / 8 * (BM == 128 && STAGES == 2 ? 2 : 1));
   const auto kernel = product_tiled<T, MODE, false, WM, WN, MT, NT, DenseArgs, STAGES>;
   const int lds = STAGES == 2 ? 0 : STAGES * (BM + BN) * kStep;
   if (lds && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
@@ -337,7 +336,7 @@ vp_status launch_dense_tiled(const DenseArgs& a, hipStream_t s) {
 template <typename T, int MODE> vp_status launch_as(DenseArgs a, const LinearPlan& p, float* ws, hipStream_t s) {
   const DenseArgs whole = a;
   const int64_t M = MODE == kGradW ? a.M : a.R;
-  a.parts = a.L = p.parts;
+  a.parts = p.parts;
   a.chunk = (int32_t)p.chunk;
   if (p.parts > 1) {   // raw sums to the workspace
     a.raw = a.wide = true;

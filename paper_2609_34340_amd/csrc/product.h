@@ -333,13 +333,13 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
   int64_t slots = mt;   // row tiles (dense: of every part)
   int64_t high_slots = 0;   // dense: of one part
   if constexpr (kDense) {
-    high_slots = (a.R + BM - 1) / BM;
-    if (MODE != kGradW) slots = high_slots * a.parts;
+    high_slots = MODE == kGradW ? mt : (a.R + BM - 1) / BM;
+    slots = high_slots * a.parts;
   } else if constexpr (MODE != kGradW) {
     slots = row_tiles.total;
   }
   const uint32_t all = (uint32_t)(slots * nt), per = (all + 7) / 8;   // tiles, below 2^31; this XCD's
-  const uint32_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW ? per * a.L : per;   // (dense: L is the parts)
+  const uint32_t first = blockIdx.x >> 3, stride = gridDim.x >> 3, last = MODE == kGradW && !kDense ? per * a.L : per;
   const auto dense_tile = [&](TileAt& t, int part, int64_t m0, int n0) {
     if constexpr (kDense) {
       const int64_t c0 = (int64_t)part * a.chunk;
@@ -376,15 +376,15 @@ __global__ void __launch_bounds__(WM * WN * 64, waves_of<Args>()) product_tiled(
     }
   };
   const auto tile_at = [&](uint32_t idx, TileAt& t) -> bool {
-    const uint32_t in_xcd = MODE == kGradW ? idx % per : idx, at = (blockIdx.x & 7) * per + in_xcd;
+    const uint32_t in_xcd = MODE == kGradW && !kDense ? idx % per : idx, at = (blockIdx.x & 7) * per + in_xcd;
     if (at >= all) return false;
     const uint32_t band = at / (uint32_t)(kBand * nt), in = at - band * (kBand * nt);
     const uint32_t high = min((uint32_t)kBand, (uint32_t)slots - band * kBand);
     const int64_t slot = band * kBand + in % high;
     const int n0 = (int)(in / high) * kTileN;
     if constexpr (kDense) {
-      const int part = MODE == kGradW ? (int)(idx / per) : (int)((uint32_t)slot / (uint32_t)high_slots);
-      dense_tile(t, part, (MODE == kGradW ? slot : slot - part * high_slots) * BM, n0);
+      const int part = (int)((uint32_t)slot / (uint32_t)high_slots);
+      dense_tile(t, part, (slot - part * high_slots) * BM, n0);
       return true;
     }
     Group g;
