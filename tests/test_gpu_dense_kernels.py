@@ -216,3 +216,49 @@ def test_more_rows_than_workgroups_hold_at_once(vp):  # noqa: F811
         u = (x.double() - st[:, :1].double()) * st[:, 1:].double()
         assert_near(dw, (d.double() * u).sum(0), (T + 8) * ref.U * (d.double() * u).abs().sum(0))
         assert_near(db, d.double().sum(0), (T + 8) * ref.U * d.double().abs().sum(0))
+
+
+@pytest.mark.parametrize("case", [("forward", 2, 8, 1 << 20), ("forward", 200, 8, 1 << 20), ("forward", 2, 1 << 20, 8), ("forward", 130, 1 << 20, 8),
+                                  ("grad_x", 200, 1 << 20, 8), ("grad_x", 2, 8, 1 << 20), ("grad_w", 3, 1 << 20, 8), ("grad_w", 200, 8, 1 << 20)], ids=str)
+def test_the_widest_products(vp, case):  # noqa: F811
+    direction, R, N, K = case
+    check(vp, direction, R, N, K, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+def test_the_longest_rows(vp, dtype):  # noqa: F811
+    """2^20 values, the limit, and one less; every call on rows."""
+    for H in (1 << 20, (1 << 20) - 1):
+        x, w, dy = normal((3, H), 1, dtype), normal((H,), 2, dtype, 0.2, 1.0), normal((3, H), 3, dtype)
+        y, err, stats, _ = ref.norm(x, w, w, 1e-5, True)
+        near_rounded(vp.layer_norm(x.cuda(), w.cuda(), w.cuda()), y, err)
+        stats = stats.float()
+        dx, e_x, dw, e_w, db, e_b = ref.norm_grad(dy, x, stats, w, True, x)
+        got = vp.layer_norm_grad(dy.cuda(), x.cuda(), stats.cuda(), w.cuda(), residual=x.cuda())
+        near_rounded(got[0], dx, e_x)
+        near(got[1], dw, e_w + 1e-30)
+        near(got[2], db, e_b + 1e-30)
+        mask, scale = ref.kept(3, H, 0.1, 5, 6)
+        want, e = ref.dropout(x, mask, scale, dy)
+        near_rounded(vp.dropout(x.cuda(), 0.1, 5, step=torch.tensor([6]).cuda(), residual=dy.cuda()), want, e)
+        d, e, db, e_b = ref.act_grad(dy, x, "gelu")
+        got, got_b = vp.linear_act_grad(dy.cuda(), x.cuda(), act="gelu")
+        near_rounded(got, d, e)
+        near(got_b, db, e_b + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+def test_rows_more_than_4_mib_apart(vp, dtype):  # noqa: F811
+    def far(T, H, seed):
+        wide = torch.full((T, (5 << 20) // dtype.itemsize), math.nan, dtype=dtype, device="cuda")
+        wide[:, 3:3 + H] = normal((T, H), seed, dtype).cuda()
+        return wide[:, 3:3 + H]
+    x, dy, res, st = far(6, 200, 1), far(6, 200, 2), far(6, 200, 3), torch.rand(6, 2, device="cuda")
+    near_x, near_dy, near_res = x.contiguous(), dy.contiguous(), res.contiguous()
+    out = far(6, 200, 4)
+    assert torch.equal(vp.layer_norm(x, out=out), vp.layer_norm(near_x))
+    assert all(torch.equal(a, b) for a, b in zip(vp.layer_norm_grad(dy, x, st, residual=res, d_x=out),
+                                                 vp.layer_norm_grad(near_dy, near_x, st, residual=near_res)))
+    assert torch.equal(vp.dropout(x, 0.3, 1, residual=res, out=out), vp.dropout(near_x, 0.3, 1, residual=near_res))
+    got, want = vp.linear_act_grad(dy, x, act="silu", out=out), vp.linear_act_grad(near_dy, near_x, act="silu")
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
