@@ -747,7 +747,8 @@ vp_status vp_linear(const void* x, int64_t x_stride, int32_t dtype, const void* 
  * vp_dtype), and the bias's gradient d_bias = sum over rows (device float32
  * [N]; of the values before d_pre's rounding).  d_pre or d_bias may be NULL, not
  * both; pre is NULL exactly for VP_ACT_NONE; d_pre may be d_y itself.  relu's
- * slope at 0 is 0.  N <= 2^20, R < 2^31; strides and addresses as for the norm.
+ * slope at 0 is 0; slopes at infinities, to which a kept 16-bit value may
+ * round, are their limits 1 and 0.  N <= 2^20, R < 2^31; strides and addresses as for the norm.
  * The workspace is needed for d_bias. */
 size_t vp_linear_act_grad_workspace(int64_t R, int64_t N);
 vp_status vp_linear_act_grad(const void* d_y, int64_t d_y_stride, const void* pre, int64_t pre_stride, int32_t dtype,

@@ -18,11 +18,12 @@ __device__ inline float logistic(float v) {
   return v;
 #endif
 }
-// And 1 less it, as exact.  exp(-v) ends at 2^120 here, so that its product with the reciprocal stays 1.
+// And 1 less it, as exact.  exp(-v) ends at 2^120 here (a NaN stays), so that its product with the reciprocal stays 1.
 struct Logistic { float s, rest; };
 __device__ inline Logistic logistic_pair(float v) {
 #ifdef __HIP_DEVICE_COMPILE__
-  const float e = __builtin_fminf(__builtin_amdgcn_exp2f(v * -1.44269504089f), 0x1p120f);
+  float e = __builtin_amdgcn_exp2f(v * -1.44269504089f);
+  e = e > 0x1p120f ? 0x1p120f : e;
   const float s = __builtin_amdgcn_rcpf(1.0f + e);
   return {s, e * s};
 #else
@@ -67,22 +68,32 @@ template <int ACT> __device__ inline float activation(float v) {
   return v;
 }
 
-// gradient * activation'(v).  Below -100 and -20 the derivatives are those there, less than 1e-32 (where the factor of the
-// logistic would outgrow what its end at 2^-120 leaves).
+// v, no further from 0 than `most` (one instruction, which loses a NaN).
+__device__ inline float within(float v, float most) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_amdgcn_fmed3f(v, -most, most);
+#else
+  return v;
+#endif
+}
+
+// gradient * activation'(v).  Past 100 and 20 the factors of the logistic and the bell are those there, and the derivatives
+// 1, or less than 1e-32: below, the factor would outgrow what the logistic's end at 2^-120 leaves; above, it would be an
+// infinity times 0, v^2 from 5e19 on and v itself where a kept 16-bit value rounded to infinity.  A NaN comes from the
+// logistic or the distribution, which take v itself.
 template <int ACT> __device__ inline float through(float gradient, float v) {
   if constexpr (ACT == VP_ACT_RELU) return v <= 0.0f ? 0.0f : gradient;
   if constexpr (ACT == VP_ACT_SILU) {
-    v = v < -100.0f ? -100.0f : v;
     const Logistic q = logistic_pair(v);
-    return gradient * q.s * __builtin_fmaf(v, q.rest, 1.0f);
+    return gradient * q.s * __builtin_fmaf(within(v, 100.0f), q.rest, 1.0f);
   }
   if constexpr (ACT == VP_ACT_GELU) {
     const Normal n = normal(v);
-    return gradient * __builtin_fmaf(v * 0.398942280401f, n.bell, n.cdf);
+    return gradient * __builtin_fmaf(within(v, 20.0f) * 0.398942280401f, n.bell, n.cdf);
   }
   if constexpr (ACT == VP_ACT_GELU_TANH) {
-    v = v < -20.0f ? -20.0f : v;
     const Logistic q = logistic_pair(kTanhSlope * v * __builtin_fmaf(kTanhCube * v, v, 1.0f));
+    v = within(v, 20.0f);
     return gradient * q.s * __builtin_fmaf(v * q.rest, kTanhSlope * __builtin_fmaf(3.0f * kTanhCube * v, v, 1.0f), 1.0f);
   }
   return gradient;
