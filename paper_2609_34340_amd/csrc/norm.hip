@@ -252,6 +252,10 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int
   const float count = (float)a.H;
   const int64_t stride = (int64_t)gridDim.x * groups;
   int64_t t = (int64_t)blockIdx.x * groups + group;
+  // Past the row's end g is 0, but u of a zero would be -m r, which may pass 32 bits.  Lanes that hold nothing take x from
+  // the row's beginning, and a partial piece goes on with its last value (16 bits), or its u are 0 (32 bits: 33.8 us for
+  // 4095 rows of 2047, with the loads 34.8; every place checked in a branch costs whole rows 1 to 2%).
+  constexpr bool kLast = n == 8;
   // Two rows ahead where registers allow: one row's arithmetic is shorter than a load.
   constexpr int kAhead = kKeep ? 2 : 1;
   struct Row { u32x4 x[NV], d[NV], res[kKeep ? NV : 1]; float m, r; } next[kAhead];
@@ -260,8 +264,8 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int
     const bool in = at_row < a.T;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * lanes) * n;
-      to.x[i] = load_piece(x + c, in ? a.H - c : 0);
+      const int c = (lane + i * lanes) * n, cx = c < a.H ? c : 0;
+      to.x[i] = load_piece<T, kLast>(x + cx, in ? a.H - cx : 0);
       to.d[i] = load_piece(d + c, in ? a.H - c : 0);   // zeros past the row's end
       if (kKeep && a.residual) to.res[at(i)] = load_piece((const T*)(a.residual + at_row * a.residual_stride) + c, in ? a.H - c : 0);
     }
@@ -288,6 +292,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormArgs a, int
 #pragma unroll
       for (int e = 0; e < n; ++e) {
         u[i][e] = (u[i][e] - m) * r;
+        if (!kLast && e > 0) u[i][e] = e < a.H - (lane + i * lanes) * n ? u[i][e] : 0.0f;
         dw[i][e] = __builtin_fmaf(g[i][e], u[i][e], dw[i][e]);
         db[i][e] += g[i][e];
       }

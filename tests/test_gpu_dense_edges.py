@@ -4,7 +4,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_dense import normal, vp  # noqa: F401
+import dense_reference as ref
+from test_gpu_dense import near, near_rounded, normal, vp  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +32,24 @@ def test_slopes_of_the_largest_values(vp, act, dtype):  # noqa: F811
         d, w = normal((R, K), 2, dtype).cuda(), normal((K, 24), 3, dtype, 0.1).cuda()
         got, plain = vp.linear_grad_x(d, w, act=act, pre=pre), vp.linear_grad_x(d, w)
         assert torch.equal(got[:, :n], plain[:, :n]) and (got[:, n:2 * n].abs() <= 1e-28).all()
+
+
+@pytest.mark.parametrize("H", [61, 64, 250, 256, 1277, 1280, 32768])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+def test_gradient_of_equal_values_far_from_zero(vp, H, dtype):  # noqa: F811
+    """Rows of one value 2^80 and a tiny eps: m r passes 32 bits, where a row's lanes hold nothing as well, but u is 0 and
+    the gradient r (g - mean(g))."""
+    x = torch.full((3, H), 2.0 ** 80, dtype=dtype)
+    x[1] = 1.0
+    want = torch.tensor([[2.0 ** 80, 1e15], [1.0, 1e15], [2.0 ** 80, 1e15]], dtype=torch.float64)
+    stats = want.float().cuda()
+    # the mean is exact where every wavefront holds a power of two values (of 1280 in 16 bits one holds 768, and 1 / 768 rounds)
+    if H in (64, 256, 32768) or (H == 1280 and dtype == torch.float32):
+        assert (vp.layer_norm(x.cuda(), eps=1e-30, stats=stats.fill_(math.nan)) == 0).all()
+        near(stats, want, 8 * ref.U * want)
+    d = normal((3, H), 1, dtype)
+    dx, e, dw, e_w, db, e_b = ref.norm_grad(d, x, stats.cpu(), None, True)
+    got = vp.layer_norm_grad(d.cuda(), x.cuda(), stats)
+    near_rounded(got[0], dx, e)
+    near(got[1], dw, e_w + 1e-30)
+    near(got[2], db, e_b + 1e-30)
