@@ -156,9 +156,13 @@ def _weights2(w: torch.Tensor, dtype) -> int:
 _DIRECTIONS = ("forward", "grad_x", "grad_w")
 
 
+def _fits(R: int, N: int, K: int) -> bool:
+    return abs(R) < 1 << 63 and max(abs(N), abs(K)) < 1 << 31   # ctypes would keep the low bits
+
+
 @functools.lru_cache(maxsize=256)
 def _linear_bytes(direction: int, R: int, N: int, K: int) -> int:
-    return int(lib().vp_linear_workspace(direction, R, N, K))
+    return int(lib().vp_linear_workspace(direction, R, N, K)) if _fits(R, N, K) else 0
 
 
 def linear_workspace_bytes(R: int, N: int, K: int, direction: str = "forward") -> int:
@@ -170,7 +174,7 @@ def linear_kernel(R: int, N: int, K: int, direction: str = "forward"):
     """vp_linear_kernel: ("few_rows", "tiles_128", "tiles_256" or "tiles_alone", parts of the contraction), by which a
     product of these sizes is computed."""
     parts = C.c_int32()
-    kind = lib().vp_linear_kernel(_DIRECTIONS.index(direction), R, N, K, C.byref(parts))
+    kind = lib().vp_linear_kernel(_DIRECTIONS.index(direction), R, N, K, C.byref(parts)) if _fits(R, N, K) else -1
     if kind < 0:
         raise ValueError("no product has these sizes")
     return ("few_rows", "tiles_128", "tiles_256", "tiles_alone")[kind], parts.value
