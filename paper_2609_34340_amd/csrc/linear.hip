@@ -6,7 +6,7 @@
 //   d_pre = d_y act'(pre), d_b = sum over rows of it
 //
 // Many rows go through product.h's tiles, of 128 x 128 or 256 x 256 results,
-// few through linear_few.  Where the results are too few for 256 CUs the
+// few through linear_few (up to 32, and up to 128 by fewer columns).  Where the results are too few for 256 CUs the
 // contraction is taken in parts, whose sums linear_join adds in their order.
 #include <hip/hip_runtime.h>
 
@@ -253,12 +253,19 @@ struct LinearPlan {
 };
 
 // The least of an estimate in us.  Few rows: a chunk of 256 values takes 1.06 with up to 16 rows, 1.25 with 32, 1.7
-// with 64 (1.6 times that where two workgroups share a CU), or its weights' time at 5.2 TB/s for all of them; 3
-// around them, and for parts 6 for the second launch (on the device 4, but a call of two launches takes the host 3
+// with 64 (1.6 times that where two workgroups share a CU), or its weights' time at 5.2 TB/s for all of them (once for
+// every 64 rows); 3 around them, and for parts 6 for the second launch (on the device 4, but a call of two launches takes the host 3
 // longer) and the sums' way out and back at 3 TB/s.  Measured in 1, 2, 4, 8 parts, weights from memory: 1 row by 4096
 // x 4096 20, 15, 12.5, 12.0; 61 rows 31, 22, 16.8, 18.0; 128 rows 31, 22.0, 22.8 (tiles in 8 parts 21.2); 1 by 16384 x
 // 4096 30, 34; 96 rows by 256 x 7168 in 4, 7, 14, 28 parts 18, 14, 11.9, 11.9; 1 by 512 x 512 4.8, 6.3, by 512 x 1536
 // 8.7, 8.3, by 2048 x 2048 11.4, 10.0, 8.3, 7.6.
+//
+// Tiles read the weights once for 128 rows, so from 33 rows on the two are compared, in parts of 16 steps or more (of
+// fewer the estimate of tiles says too little), neither faster than its weights come: at 4.2 TB/s through few rows, 4.4
+// through tiles alone, 5.2 through the others.  Measured, weights from memory, us (few rows / tiles): 33 rows by 28672 x
+// 4096 65 / 64; 64 rows 70 / 66, by 57344 x 4096 127 / 109, by 131072 x 4096 257 / 196; 65 rows by 4096 x 4096 22 / 21,
+// by 14336 x 4096 52 / 36, by 28672 x 4096 105 / 60, by 131072 x 4096 466 / 192; of 414 sizes that go through tiles
+// for this, or by other parts, the worst is 64 by 32768 x 8192, 132 / 139.  With up to 32 rows tiles take 0.8 to 1.7 times as long.
 //
 // Tiles: a step of 64 values takes 0.72 for a 128 x 128 tile alone on its CU, 1.1 for two, 1.65 for a 256 x 256 tile;
 // a round of tiles ends with 3 or 9 for its results; parts as above.  Measured, us (128 / 256 tiles, parts in
@@ -290,18 +297,21 @@ LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
       best = p;
     }
   };
-  if (mode == kExpertForward && M <= 2 * kFewRows) {
+  const bool few = mode == kExpertForward && M <= 2 * kFewRows;
+  const double weights = few ? 2.0 * (double)N * (double)K : 0.0;   // bytes that bound a product of few rows
+  if (few) {
     const int64_t tiles = ceil_of(M, kFewRows) * ceil_of(N, kFewCols), most = C / kFewChunk;
     const double chunk = M <= 16 ? 1.06 : M <= 32 ? 1.25 : 1.7;
     const int64_t one_each = kCus / std::max<int64_t>(tiles, 1);
     for (const int64_t parts : std::initializer_list<int64_t>{1, 2, 4, 8, 16, 32, one_each, most}) {
       if (parts > std::max<int64_t>(most, 1) || parts > 64) continue;
       const LinearPlan p = in_parts(VP_LINEAR_FEW_ROWS, parts);
-      const double bytes = (double)(ceil_of(N, kFewCols) * p.parts) * (kFewCols * kFewChunk * 2);
+      const double bytes = (double)(tiles * p.parts) * (kFewCols * kFewChunk * 2);
       const double crowd = std::max(1.0, 0.8 * (double)(tiles * p.parts) / kCus);
       take(p, 3.0 + (double)ceil_of(p.chunk, kFewChunk) * std::max(chunk * crowd, bytes / 5.2e6) + join(p));
     }
-    return best;
+    if (M <= 32) return best;
+    least = std::max(least, 3.0 + weights * (double)ceil_of(M, kFewRows) / 4.2e6);   // tiles follow
   }
   for (const bool large : {true, false}) {
     const int64_t side = large ? 256 : 128, tiles = ceil_of(M, side) * ceil_of(N, side);
@@ -311,7 +321,9 @@ LinearPlan plan_of(int mode, int64_t R, int32_t N_, int32_t K) {
       if (!large) p.kind = groups <= kCus ? VP_LINEAR_TILES_ALONE : VP_LINEAR_TILES_128;
       const double rounds = std::max(1.0, std::ceil(groups / (large ? kCus : 2 * kCus)));
       const double step = large ? 1.65 : p.kind == VP_LINEAR_TILES_ALONE ? 0.72 : 1.1;
-      take(p, rounds * (step * steps + (large ? 9.0 : 3.0)) + join(p));
+      const double stream = 3.0 + weights / (p.kind == VP_LINEAR_TILES_ALONE ? 4.4e6 : 5.2e6);
+      if (few && steps < 16) break;
+      take(p, std::max(rounds * (step * steps + (large ? 9.0 : 3.0)), stream) + join(p));
     }
   }
   return best;

@@ -1,4 +1,5 @@
-"""What the questions about dense products make of sizes that the calls refuse (no GPU)."""
+"""What the questions about dense products answer: the kernels of few rows by wide outputs, and sizes that the calls refuse
+(no GPU)."""
 import pytest
 
 
@@ -20,3 +21,13 @@ def test_sizes_past_32_bits_have_no_kernel(vp, direction):
         with pytest.raises(ValueError):
             vp.linear_kernel(*sizes, direction)
         assert vp.linear_workspace_bytes(*sizes, direction) == 0
+
+
+def test_wide_outputs_read_their_weights_once(vp):
+    """From 65 rows on few_rows goes through the weights twice, and tiles do not; up to 32 rows it stays."""
+    for R, N, K in ((65, 14336, 4096), (96, 28672, 4096), (128, 28672, 8192), (128, 131072, 4096), (65, 1 << 20, 2048)):
+        assert vp.linear_kernel(R, N, K)[0] in ("tiles_alone", "tiles_128"), (R, N, K)
+    for R, N, K in ((64, 131072, 4096), (48, 57344, 4096)):
+        assert vp.linear_kernel(R, N, K) == ("tiles_128", 1), (R, N, K)
+    for R, N, K in ((1, 28672, 4096), (32, 131072, 4096), (61, 4096, 4096), (96, 256, 7168), (128, 1024, 4096)):
+        assert vp.linear_kernel(R, N, K)[0] == "few_rows", (R, N, K)

@@ -6,6 +6,7 @@ import torch
 
 import dense_reference as ref
 from test_gpu_dense import near, near_rounded, normal, vp  # noqa: F401
+from test_gpu_dense_kernels import check
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +54,16 @@ def test_gradient_of_equal_values_far_from_zero(vp, H, dtype):  # noqa: F811
     near_rounded(got[0], dx, e)
     near(got[1], dw, e_w + 1e-30)
     near(got[2], db, e_b + 1e-30)
+
+
+# R, N, K, kernel, parts: None where any number above one does
+WIDE = [(33, 57344, 1024, "tiles_128", 1), (64, 28680, 1032, "tiles_alone", 1), (65, 16384, 1024, "tiles_alone", 1), (127, 65544, 1024, "tiles_128", 1),
+        (100, 8192, 4104, "tiles_alone", None), (97, 4096, 8192, "tiles_alone", None), (32, 57344, 1024, "few_rows", 1)]
+
+
+@pytest.mark.parametrize("case", WIDE, ids=lambda c: "-".join(map(str, c)))
+def test_few_rows_by_wide_outputs(vp, case):  # noqa: F811
+    R, N, K, kernel, parts = case
+    kind, n = vp.linear_kernel(R, N, K)
+    assert kind == kernel and (n == parts if parts else n > 1)
+    check(vp, "forward", R, N, K, torch.bfloat16)
