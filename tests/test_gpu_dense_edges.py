@@ -1,4 +1,4 @@
-"""Norm, dropout and dense products where values leave the usual range."""
+"""Norm and dense products where values leave the usual range, few rows by wide outputs, and results over their residual."""
 import math
 
 import pytest
@@ -67,3 +67,53 @@ def test_few_rows_by_wide_outputs(vp, case):  # noqa: F811
     kind, n = vp.linear_kernel(R, N, K)
     assert kind == kernel and (n == parts if parts else n > 1)
     check(vp, "forward", R, N, K, torch.bfloat16)
+
+
+@pytest.mark.parametrize("H", [100, 4096, 20000])
+def test_gradient_of_rows_far_from_zero(vp, H):  # noqa: F811
+    """Forward statistics into the gradient, against the statistics of 64 bits.  The mean in 32 bits is off by up to half
+    a unit of its last place and by the forward's own bound: every u of the row moves by that times r, which the result
+    takes once through u and once through mean(g u); r's bound counts three times."""
+    x = normal((4, H), 1)
+    x[0] += 5000.0
+    x[2] -= 3e4
+    d = normal((4, H), 2)
+    _, _, stats, stats_err = ref.norm(x, None, None, 1e-5, True)
+    st = torch.empty(4, 2, device="cuda")
+    vp.layer_norm(x.cuda(), stats=st)
+    dx, e, dw, e_w, db, e_b = ref.norm_grad(d, x, stats, None, True)
+    m, r = stats[:, :1], stats[:, 1:]
+    e_r, off = stats_err[:, 1:], stats_err[:, :1] * r   # of r, and of u
+    u, g = (x.double() - m) * r, d.double()
+    e_u = (off + u.abs() * e_r / r) * 1.01
+    mean = lambda v: v.mean(1, keepdim=True)  # noqa: E731
+    moved = r * (e_u * mean(g * u).abs() + (u.abs() + e_u) * mean(g.abs() * e_u))
+    got = vp.layer_norm_grad(d.cuda(), x.cuda(), st)
+    near_rounded(got[0], dx, 1.01 * (e + dx.abs() * e_r / r + moved))
+    near(got[1], dw, 1.01 * e_w + (g.abs() * e_u).sum(0))
+    near(got[2], db, e_b)
+
+
+# direction, R, N, K, kernel, parts: None where any number above one does
+OVER = [("forward", 3, 136, 72, "few_rows", 1), ("forward", 40, 520, 4096, "few_rows", None), ("forward", 200, 136, 72, "tiles_alone", 1),
+        ("forward", 140, 264, 4104, "tiles_alone", None), ("forward", 3000, 2056, 72, "tiles_128", 1), ("forward", 4090, 4088, 392, "tiles_256", 1),
+        ("grad_x", 130, 72, 136, "tiles_alone", 1), ("grad_x", 96, 2056, 520, "tiles_alone", None), ("grad_x", 3000, 72, 2056, "tiles_128", 1),
+        ("grad_x", 4090, 392, 4088, "tiles_256", 1)]
+
+
+@pytest.mark.parametrize("case", OVER, ids=lambda c: "-".join(map(str, c)))
+def test_results_over_their_residual(vp, case):  # noqa: F811
+    """Every kernel writes over the residual what it writes beside it (which other tests hold to 64 bits)."""
+    direction, R, N, K, kernel, parts = case
+    kind, n = vp.linear_kernel(R, N, K, direction)
+    assert kind == kernel and (n == parts if parts else n > 1)
+    x, w, dy = (normal(s, i, torch.bfloat16, std).cuda() for i, (s, std) in enumerate((((R, K), 1.0), ((N, K), 0.1), ((R, N), 1.0))))
+    if direction == "forward":
+        for dtype in (torch.bfloat16, torch.float32):
+            res = normal((R, N), 5, dtype).cuda()
+            want = vp.linear(x, w, act="gelu", residual=res, dtype=dtype)
+            assert vp.linear(x, w, act="gelu", residual=res, out=res) is res and torch.equal(res, want)
+    else:
+        res, pre = normal((R, K), 5, torch.bfloat16).cuda(), normal((R, K), 6, torch.bfloat16).cuda()
+        want = vp.linear_grad_x(dy, w, act="silu", pre=pre, residual=res)
+        assert vp.linear_grad_x(dy, w, act="silu", pre=pre, residual=res, out=res) is res and torch.equal(res, want)
