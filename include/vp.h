@@ -680,9 +680,12 @@ int32_t vp_route_lanes(int64_t T, int32_t E);
  *           either may be NULL (ones, zeros)
  *   stats   device float32 [T, 2], (m, r) for the gradient, or NULL
  * A row with an infinity or NaN becomes NaN and touches no other (without
- * `center` an infinity makes r 0: zeros, and NaN in its own place).  H <= 2^20, T
- * < 2^31; strides and addresses are multiples of the element (of 16 bytes for
- * full speed), eps >= 0 and finite. */
+ * `center` an infinity makes r 0: zeros, and NaN in its own place).  Sums are of
+ * 32 bits' range as well: where a row's sum or its deviations' squares pass
+ * 2^128, r is 0 or NaN; where these fall below 2^-149, as if they were 0.  m is
+ * rounded to 32 bits for the gradient, not for y.  H <= 2^20, T < 2^31; strides
+ * and addresses are multiples of the element (of 16 bytes for full speed), eps
+ * >= 0 and finite. */
 vp_status vp_layer_norm(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t x_stride, const void* weight,
                         const void* bias, int32_t param_dtype, float eps, int32_t center, void* y, int64_t y_stride,
                         float* stats, void* stream);
@@ -720,7 +723,8 @@ vp_status vp_dropout(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t
                      int64_t out_stride, void* stream);
 
 /* Activations: x; max(x, 0); x s(x) with the logistic s; x Phi(x) with the
- * normal distribution; x s(2 sqrt(2 / pi) (x + 0.044715 x^3)). */
+ * normal distribution; x s(2 sqrt(2 / pi) (x + 0.044715 x^3)).  Of minus
+ * infinity the last three are NaN, as the product says. */
 enum { VP_ACT_NONE = 0, VP_ACT_RELU = 1, VP_ACT_SILU = 2, VP_ACT_GELU = 3, VP_ACT_GELU_TANH = 4 };
 
 /* Dense products: y = act(x W^T + bias) + residual.
@@ -748,8 +752,8 @@ vp_status vp_linear(const void* x, int64_t x_stride, int32_t dtype, const void* 
  * [N]; of the values before d_pre's rounding).  d_pre or d_bias may be NULL, not
  * both; pre is NULL exactly for VP_ACT_NONE; d_pre may be d_y itself.  relu's
  * slope at 0 is 0; slopes at infinities, to which a kept 16-bit value may
- * round, are their limits 1 and 0.  N <= 2^20, R < 2^31; strides and addresses as for the norm.
- * The workspace is needed for d_bias. */
+ * round, are their limits 1 and 0.  N <= 2^20, R < 2^31; strides and addresses
+ * as for the norm.  The workspace is needed for d_bias. */
 size_t vp_linear_act_grad_workspace(int64_t R, int64_t N);
 vp_status vp_linear_act_grad(const void* d_y, int64_t d_y_stride, const void* pre, int64_t pre_stride, int32_t dtype,
                              int64_t R, int64_t N, int32_t act, void* d_pre, int64_t d_pre_stride, float* d_bias,

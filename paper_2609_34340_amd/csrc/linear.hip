@@ -63,15 +63,17 @@ template <typename T> __device__ inline void finish4(const DenseArgs& a, int64_t
 // ----------------------------------------------------------- few rows
 
 // Up to 64 rows by 64 columns of one part of the contraction, forward.  The
-// weights' bytes bound it: they go straight to registers, each read once.  The
-// rows of x would be read again for every 16 columns (64 rows by 4096 x 4096:
-// 64 MB from the L2, 7 us), so they go through LDS, a chunk of 256 values at a
-// time: two wavefronts for 32 columns each, and two more for the other half of
-// the chunk, whose sums are added in LDS at the end.  Loads run two chunks
-// ahead.  16-byte piece c of row r lies at place c ^ (r & 15), so that a
-// fragment's 16 rows meet no bank twice.  61 rows by 4096 x 4096, weights from
-// memory, in four parts: 13 us, and 4 for the join; 96 by 256 x 7168 in 14: 7.5
-// and 4.5.  Tried and dropped: four chunks ahead for up to 32 rows (12.5 -> 13.0
+// weights go straight to registers, each read once.  The rows of x would be
+// read again for every 16 columns (64 rows by 4096 x 4096: 64 MB from the L2, 7
+// us), so they go through LDS, a chunk of 256 values at a time: two wavefronts
+// for 32 columns each, and two more for the other half of the chunk, whose sums
+// are added in LDS at the end.  Loads run two chunks ahead.  16-byte piece c of
+// row r lies at place c ^ (r & 15), so that a fragment's 16 rows meet no bank
+// twice.  Few rows are bound by the weights' bytes (one row by 16384 x 4096 at
+// 4.4 TB/s), 64 by a chunk's way through LDS and its barrier, 1.7 us against
+// 1.06 with up to 16: 61 rows by 4096 x 4096, weights from memory, in four
+// parts: 13 us (2.6 TB/s), and 4 for the join; 96 by 256 x 7168 in 14: 7.5 and
+// 4.5.  Tried and dropped: four chunks ahead for up to 32 rows (12.5 -> 13.0
 // us at one row: the weights' rate bounds it, not their latency), up to 16 rows
 // by 16 columns without parts (10.4 -> 8.6 us at one row by 4096 x 4096, 11.0 ->
 // 11.4 at 16 rows, 17 -> 20 at 16 by 8192 x 4096).

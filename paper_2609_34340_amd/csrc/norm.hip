@@ -7,8 +7,9 @@
 // A row stays in the registers of its lanes (16 of them, a wavefront, or a workgroup), so it is read once; longer rows
 // are read again.  Statistics: every wavefront takes the mean of its values, then their deviations d from it, whose sum
 // corrects the mean and the sum of squares; a workgroup joins its wavefronts' by the formula for two groups' variances
-// (Chan, Golub, LeVeque 1979).  Means are kept as a base and a small shift, so nothing cancels however far from zero the
-// rows lie.
+// (Chan, Golub, LeVeque 1979).  Means are kept as a base and a small shift, so nothing cancels in the results however far
+// from zero the rows lie.  The statistics hold their sum, rounded: the gradient's u are off by up to half a unit of m's
+// last place times r, all of a row by the same (2e-4 where m is 5000 times the deviation).
 //
 // HBM bounds both directions, and first the instructions had to become few enough: workgroups run through rows with their
 // parameters in registers and the next row's loads on the way, pieces of rows that are whole carry no checks, and the
@@ -17,8 +18,9 @@
 // 1 GiB copy reaches 4.8 to 5.2).  96 rows of 4096 take 3.5 us, about a launch.  The gradient of 8192 rows of 4096 with a
 // residual: 57 us, 4.7 TB/s, and 5 for the sums of its 256 workgroups; its registers (an output's sums for every column)
 // leave a CU one workgroup, and two rows' loads ahead make up for it (one: 62 us; 128 registers and two workgroups spill:
-// 122).  Rows that begin at any element cost little in 32 bits (4095 rows of 2047: 27 us, of 2048 22), twice the time in
-// 16 (8192 rows of 4095: 104, of 4096 53).
+// 122).  Rows that begin at any element cost little in 32 bits (4095 rows of 2047: 27 us, of 2048 22; forward 17.0, 15.6),
+// in 16 half as much again forward (8192 rows of 4095: 42, of 4096 29) and nearly twice the time in the gradient (with its
+// sums 93, 53).  Rows that are read again: 2048 of 32768 in 32 bits 170 us, their gradient 340; of 65536 in 16 bits 182, 422.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

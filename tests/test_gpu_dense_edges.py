@@ -1,4 +1,5 @@
-"""Norm and dense products where values leave the usual range, few rows by wide outputs, and results over their residual."""
+"""Norm and dense products where values leave the usual range, few rows by wide outputs, and results over their
+residual."""
 import math
 
 import pytest
@@ -117,3 +118,33 @@ def test_results_over_their_residual(vp, case):  # noqa: F811
         res, pre = normal((R, K), 5, torch.bfloat16).cuda(), normal((R, K), 6, torch.bfloat16).cuda()
         want = vp.linear_grad_x(dy, w, act="silu", pre=pre, residual=res)
         assert vp.linear_grad_x(dy, w, act="silu", pre=pre, residual=res, out=res) is res and torch.equal(res, want)
+
+
+def test_infinite_sums_through_activations(vp):  # noqa: F811
+    """Plus infinity stays, minus infinity is relu's 0 and NaN where it meets a factor of 0, and columns keep to themselves."""
+    for R, N in ((3, 64), (200, 136)):
+        x, w, b = torch.zeros(R, 72, dtype=torch.bfloat16), normal((N, 72), 1, torch.bfloat16), normal((N,), 2)
+        b[3], b[N - 1] = math.inf, -math.inf
+        for act in ref.ACTS:
+            for dtype in (torch.bfloat16, torch.float32):
+                got = vp.linear(x.cuda(), w.cuda(), b.cuda(), act=act, dtype=dtype).cpu()
+                assert (got[:, 3] == math.inf).all()
+                last = got[:, N - 1]
+                assert (last == -math.inf).all() if act == "none" else (last == 0).all() if act == "relu" else last.isnan().all()
+                assert got[:, :3].isfinite().all() and got[:, 4:N - 1].isfinite().all()
+
+
+@pytest.mark.parametrize("H", [40, 200, 3000, 40000])
+def test_rows_past_the_range_keep_to_themselves(vp, H):  # noqa: F811
+    """Finite rows whose squares, or whose sum, pass 2^128: r is 0 or NaN, and the rows beside them are what they were."""
+    x = normal((5, H), 1)
+    x[1] *= 1e25
+    x[3] = 3e38
+    for center in (True, False):
+        y, err, stats, stats_err = ref.norm(x[::2], None, None, 1e-5, center)
+        st = torch.empty(5, 2, device="cuda")
+        got = vp.layer_norm(x.cuda(), center=center, stats=st)
+        near_rounded(got[::2], y, err)
+        near(st[::2], stats, stats_err + 1e-30)
+        r = st[1::2, 1]
+        assert (r.isnan() | (r == 0)).all()
