@@ -13,19 +13,20 @@ namespace vp {
 
 typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
-// Vec<T>::n elements from p on, of which `left` (maybe none, or more than these) exist; past them zeros, or the LAST of them.
+// Vec<T>::n elements from p on, of which `left` (maybe none, or more than these) exist; past them zeros, or (of 16-bit
+// ones) the LAST of them.
 template <typename T, bool LAST = false> __device__ inline u32x4 load_piece(const T* p, int64_t left) {
   constexpr int n = Vec<T>::n;
   if (left >= n) return *(const u32x4_any*)p;
   u32x4 v = {0, 0, 0, 0};
-  if (LAST) {
+  if constexpr (LAST) {
+    static_assert(n == 8, "16-bit elements");
     if (left <= 0) return v;
     const int last = (int)left - 1;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
       const int at = i < last ? i : last;
-      if constexpr (n == 8) v[i / 2] |= (uint32_t)((const uint16_t*)p)[at] << (16 * (i % 2));
-      else v[i] = ((const uint32_t*)p)[at];
+      v[i / 2] |= (uint32_t)((const uint16_t*)p)[at] << (16 * (i % 2));
     }
     return v;
   }
